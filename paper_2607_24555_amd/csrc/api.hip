@@ -13,36 +13,6 @@ thread_local int g_last_hip_error = 0;
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
-int validate(const locks_cfg_t* c) {
-  if (!c) return LOCKS_E_INVAL;
-  if (c->head_dim != kDim) return LOCKS_E_UNSUPPORTED;
-  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64) return LOCKS_E_UNSUPPORTED;
-  if ((c->kv_dtype != LOCKS_BF16 && c->kv_dtype != LOCKS_FP32) ||
-      (c->q_dtype != LOCKS_BF16 && c->q_dtype != LOCKS_FP32))
-    return LOCKS_E_UNSUPPORTED;
-  if (c->num_seqs < 0 || c->num_kv_heads < 1 || c->num_q_heads < 1) return LOCKS_E_INVAL;
-  if (c->num_q_heads % c->num_kv_heads) return LOCKS_E_INVAL;
-  if (c->num_q_heads / c->num_kv_heads > kMaxGroup) return LOCKS_E_UNSUPPORTED;
-  if (c->rank < 1 || c->rank > kMaxRank) return LOCKS_E_INVAL;
-  if (c->basis < LOCKS_BASIS_INT4 || c->basis > LOCKS_BASIS_BF16) return LOCKS_E_INVAL;
-  if (c->basis != LOCKS_BASIS_INT4 && c->rank != 2 && c->rank != 4 && c->rank != 8)
-    return LOCKS_E_UNSUPPORTED;
-  if (c->basis != LOCKS_BASIS_INT4 && c->page_size != kPage) return LOCKS_E_UNSUPPORTED;
-  if (c->budget_tokens < 1 || (c->budget_tokens + c->page_size - 1) / c->page_size < 2)
-    return LOCKS_E_INVAL;
-  if (c->max_pages_per_seq < 1 || c->num_blocks < 1) return LOCKS_E_INVAL;
-  if ((long)c->num_seqs * c->num_q_heads > 0x7fffffffL / kDim) return LOCKS_E_INVAL;
-  // record offsets are 32-bit: the summary store must stay below 4 GiB
-  if (summary_store_bytes(*c) > 0xffffffffull) return LOCKS_E_UNSUPPORTED;
-  return LOCKS_OK;
-}
-
-int hip_status(hipError_t e) {
-  if (e == hipSuccess) return LOCKS_OK;
-  g_last_hip_error = (int)e;
-  return LOCKS_E_HIP;
-}
-
 struct Ws {
   float* s_hat;
   float2* part;
@@ -124,31 +94,6 @@ hipError_t scratch_ptr(void** out) {
 
 // Table checks (locks_set_table_checks), process-wide.
 std::atomic<int> g_table_checks{0};
-
-// With table checks on: validates page_table / seq_lens into the workspace's
-// checked copies (clamping what is out of range, setting the error word) on `st`
-// and points the two at the copies, which every later launch of the call reads.
-int checked_tables(const locks_cfg_t& c, void* ws, const int32_t*& page_table,
-                   const int32_t*& seq_lens, hipStream_t st) {
-  if (!g_table_checks.load(std::memory_order_relaxed)) return LOCKS_OK;
-  const WsPlan p = plan_workspace(c);
-  char* b = static_cast<char*>(ws);
-  int32_t* pt = reinterpret_cast<int32_t*>(b + p.chk_pt_off);
-  int32_t* sl = reinterpret_cast<int32_t*>(b + p.chk_sl_off);
-  int32_t* err = reinterpret_cast<int32_t*>(b + p.chk_err_off);
-  const int rc = hip_status(launch_check_tables(c, page_table, seq_lens, pt, sl, err, err + 1, st));
-  if (rc) return rc;
-  page_table = pt;
-  seq_lens = sl;
-  return LOCKS_OK;
-}
-
-int check_ws(const locks_cfg_t* c, void* ws, size_t ws_bytes) {
-  const WsPlan p = plan_workspace(*c);
-  if (!ws || ws_bytes < p.total) return LOCKS_E_WORKSPACE;
-  if (reinterpret_cast<uintptr_t>(ws) & 255) return LOCKS_E_WORKSPACE;
-  return LOCKS_OK;
-}
 
 // Table entries per attention block: 4 (one page per wave), doubled while the
 // grid would exceed ~512 blocks, so large batches stream several pages per
@@ -234,6 +179,58 @@ hipError_t build_pages(const locks_cfg_t& c, const void* k_cache, const int32_t*
 }
 
 }  // namespace
+
+int validate(const locks_cfg_t* c) {
+  if (!c) return LOCKS_E_INVAL;
+  if (c->head_dim != kDim) return LOCKS_E_UNSUPPORTED;
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64) return LOCKS_E_UNSUPPORTED;
+  if ((c->kv_dtype != LOCKS_BF16 && c->kv_dtype != LOCKS_FP32) ||
+      (c->q_dtype != LOCKS_BF16 && c->q_dtype != LOCKS_FP32))
+    return LOCKS_E_UNSUPPORTED;
+  if (c->num_seqs < 0 || c->num_kv_heads < 1 || c->num_q_heads < 1) return LOCKS_E_INVAL;
+  if (c->num_q_heads % c->num_kv_heads) return LOCKS_E_INVAL;
+  if (c->num_q_heads / c->num_kv_heads > kMaxGroup) return LOCKS_E_UNSUPPORTED;
+  if (c->rank < 1 || c->rank > kMaxRank) return LOCKS_E_INVAL;
+  if (c->basis < LOCKS_BASIS_INT4 || c->basis > LOCKS_BASIS_BF16) return LOCKS_E_INVAL;
+  if (c->basis != LOCKS_BASIS_INT4 && c->rank != 2 && c->rank != 4 && c->rank != 8)
+    return LOCKS_E_UNSUPPORTED;
+  if (c->basis != LOCKS_BASIS_INT4 && c->page_size != kPage) return LOCKS_E_UNSUPPORTED;
+  if (c->budget_tokens < 1 || (c->budget_tokens + c->page_size - 1) / c->page_size < 2)
+    return LOCKS_E_INVAL;
+  if (c->max_pages_per_seq < 1 || c->num_blocks < 1) return LOCKS_E_INVAL;
+  if ((long)c->num_seqs * c->num_q_heads > 0x7fffffffL / kDim) return LOCKS_E_INVAL;
+  // record offsets are 32-bit: the summary store must stay below 4 GiB
+  if (summary_store_bytes(*c) > 0xffffffffull) return LOCKS_E_UNSUPPORTED;
+  return LOCKS_OK;
+}
+
+int hip_status(hipError_t e) {
+  if (e == hipSuccess) return LOCKS_OK;
+  g_last_hip_error = (int)e;
+  return LOCKS_E_HIP;
+}
+
+int checked_tables(const locks_cfg_t& c, void* ws, const int32_t*& page_table,
+                   const int32_t*& seq_lens, hipStream_t st) {
+  if (!g_table_checks.load(std::memory_order_relaxed)) return LOCKS_OK;
+  const WsPlan p = plan_workspace(c);
+  char* b = static_cast<char*>(ws);
+  int32_t* pt = reinterpret_cast<int32_t*>(b + p.chk_pt_off);
+  int32_t* sl = reinterpret_cast<int32_t*>(b + p.chk_sl_off);
+  int32_t* err = reinterpret_cast<int32_t*>(b + p.chk_err_off);
+  const int rc = hip_status(launch_check_tables(c, page_table, seq_lens, pt, sl, err, err + 1, st));
+  if (rc) return rc;
+  page_table = pt;
+  seq_lens = sl;
+  return LOCKS_OK;
+}
+
+int check_ws(const locks_cfg_t* c, void* ws, size_t ws_bytes) {
+  const WsPlan p = plan_workspace(*c);
+  if (!ws || ws_bytes < p.total) return LOCKS_E_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(ws) & 255) return LOCKS_E_WORKSPACE;
+  return LOCKS_OK;
+}
 
 int page_budget(const locks_cfg_t& c) { return (c.budget_tokens + c.page_size - 1) / c.page_size; }
 

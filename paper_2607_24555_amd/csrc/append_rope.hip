@@ -1,0 +1,125 @@
+// New tokens of a step, rotated and appended to the paged caches (locks_rope_append_kv):
+// query rows from q to q_out, key and value rows into their slots, in one launch.
+//
+// A wave moves rows of one token, four at a time: 16 lanes a row, eight elements a lane
+// (16-byte accesses for bf16).  The angles of a lane's elements are loaded once and serve
+// every row of the wave; a pair half a row apart is exchanged between lanes.  Bound: HBM
+// for prompts, the chain length -> table entry -> store for a few tokens.
+#include "rope.h"
+
+namespace locks {
+namespace {
+
+constexpr int kRows = 4;  // rows in flight per 16 lanes
+
+// Rows [r0, r1) of a token, 4 at a time, from `src(r)` to `dst(r)` (null: not stored).
+template <typename T, typename Src>
+__device__ __forceinline__ void load_rows(Row8<T> (&w)[kRows], int r, int r1, Src src) {
+#pragma unroll
+  for (int u = 0; u < kRows; ++u) w[u].load(src(min(r + 4 * u, r1 - 1)));
+}
+
+template <typename T, typename Src, typename Dst>
+__device__ __forceinline__ void move_rows(const RopeArgs& rope, const Angles& A, Row8<T> (&w)[kRows], int lane,
+                                          int r0, int r1, int n_turned, Src src, Dst dst) {
+  for (int r = r0 + (lane >> 4);; r += 4 * kRows) {
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int ru = r + 4 * u;
+      float x[8];
+      rotated(rope, A, w[u], lane, x);
+      if (ru < r1) {
+        if (ru < n_turned && rope.half) w[u].from(x);
+        w[u].store(dst(ru));
+      }
+    }
+    if (r - (lane >> 4) + 4 * kRows >= r1) return;
+    load_rows(w, r + 4 * kRows, r1, src);
+  }
+}
+
+// Waves per token: q_parts of q_rows query rows, then parts of kv_rows key and value rows
+// (keys first).
+template <typename QT, typename KT>
+__global__ __launch_bounds__(256) void rope_append_kernel(
+    RowArgs a, RopeArgs rope, KT* __restrict__ k_cache, KT* __restrict__ v_cache,
+    const int32_t* __restrict__ page_table, const int32_t* __restrict__ seq_lens, int S, int H_q,
+    int H_kv, int max_pages, int num_blocks, int pgsz, int q_parts, int q_rows, int kv_parts,
+    int kv_rows) {
+  const long id = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int parts = q_parts + kv_parts;
+  const long row_l = id / parts;
+  if (row_l >= a.n_tokens) return;
+  const int row = (int)row_l, part = (int)(id % parts);
+  const int lane = threadIdx.x & 63, cg = lane & 15;
+  const bool is_q = part < q_parts;
+
+  // the first rows are requested before the token's place is known
+  const int r0 = is_q ? part * q_rows : (part - q_parts) * kv_rows;
+  const int r1 = is_q ? min(r0 + q_rows, H_q) : min(r0 + kv_rows, 2 * H_kv);
+  const QT* q = static_cast<const QT*>(a.q) + row * a.q_stride + 8 * cg;
+  const KT* k = static_cast<const KT*>(a.k) + row * a.k_stride + 8 * cg;
+  const KT* v = static_cast<const KT*>(a.v) + row * a.v_stride + 8 * cg;
+  auto q_src = [&](int r) { return q + r * kDim; };
+  auto kv_src = [&](int r) { return r < H_kv ? k + r * kDim : v + (r - H_kv) * kDim; };
+  Row8<QT> wq[kRows];
+  Row8<KT> wk[kRows];
+  if (is_q) load_rows(wq, r0 + (lane >> 4), r1, q_src);
+  else load_rows(wk, r0 + (lane >> 4), r1, kv_src);
+
+  int s = row;
+  if (a.cu) {
+    s = wave_search(S, row, [&](int i) { return a.cu[i]; });
+    if (s < 0) return;
+  }
+  const NewTokens t = new_tokens(a, seq_lens, s);
+  const int tok = t.tok0 + (row - t.row0);
+  if (row - t.row0 >= t.n || tok < 0 || tok / pgsz >= max_pages) return;
+  const long blk = page_table[(long)s * max_pages + tok / pgsz];
+  Angles A;
+  const bool placed = load_angles(rope, row, tok, cg, A);
+  if (!placed || blk < 0 || blk >= num_blocks) return;
+  if (is_q) {
+    QT* out = static_cast<QT*>(a.q_out) + row * a.q_out_stride + 8 * cg;
+    move_rows(rope, A, wq, lane, r0, r1, H_q, q_src, [&](int r) { return out + r * kDim; });
+  } else {
+    const long at = (blk * H_kv * pgsz + tok % pgsz) * kDim + 8 * cg;
+    const long head = (long)pgsz * kDim;
+    move_rows(rope, A, wk, lane, r0, r1, H_kv, kv_src, [&](int r) {
+      return r < H_kv ? k_cache + at + r * head : v_cache + at + (r - H_kv) * head;
+    });
+  }
+}
+
+template <typename QT, typename KT>
+hipError_t launch_typed(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& r, void* k_cache,
+                        void* v_cache, const int32_t* page_table, const int32_t* seq_lens,
+                        hipStream_t st) {
+  // rows per wave: as many as 4 kRows while 4,096 waves remain
+  const int hq = a.q ? c.num_q_heads : 0, hkv = 2 * c.num_kv_heads;
+  int per = 4 * kRows;
+  while (per > 4 && (long)a.n_tokens * ((hq + per - 1) / per + (hkv + per - 1) / per) < 4096) per /= 2;
+  const int q_parts = (hq + per - 1) / per, kv_parts = (hkv + per - 1) / per;
+  const long waves = (long)a.n_tokens * (q_parts + kv_parts);
+  if ((waves + 3) / 4 > 0x7fffffffL) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((rope_append_kernel<QT, KT>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a, r,
+                     static_cast<KT*>(k_cache), static_cast<KT*>(v_cache), page_table, seq_lens,
+                     c.num_seqs, hq, c.num_kv_heads, c.max_pages_per_seq, c.num_blocks, c.page_size,
+                     q_parts, per, kv_parts, per);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope_append(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& r,
+                              void* k_cache, void* v_cache, const int32_t* page_table,
+                              const int32_t* seq_lens, hipStream_t st) {
+  const bool qb = !a.q || c.q_dtype == LOCKS_BF16, kb = c.kv_dtype == LOCKS_BF16;
+  if (qb && kb)
+    return launch_typed<uint16_t, uint16_t>(c, a, r, k_cache, v_cache, page_table, seq_lens, st);
+  if (qb) return launch_typed<uint16_t, float>(c, a, r, k_cache, v_cache, page_table, seq_lens, st);
+  if (kb) return launch_typed<float, uint16_t>(c, a, r, k_cache, v_cache, page_table, seq_lens, st);
+  return launch_typed<float, float>(c, a, r, k_cache, v_cache, page_table, seq_lens, st);
+}
+
+}  // namespace locks

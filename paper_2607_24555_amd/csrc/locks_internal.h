@@ -134,6 +134,19 @@ inline int scan_blocks(const locks_cfg_t& c) {
   return (c.max_pages_per_seq + ppb - 1) / ppb;
 }
 
+// ---------------------------------------------------------------- host checks (api.hip)
+
+// LOCKS_OK, or the status of a configuration that no call takes.
+int validate(const locks_cfg_t* c);
+// A HIP result as a status; a failure is kept for locks_last_hip_error.
+int hip_status(hipError_t e);
+int check_ws(const locks_cfg_t* c, void* ws, size_t ws_bytes);
+// With table checks on: validates page_table / seq_lens into the workspace's checked
+// copies (clamping what is out of range, setting the error word) on `st` and points the
+// two at the copies, which every later launch of the call reads.
+int checked_tables(const locks_cfg_t& c, void* ws, const int32_t*& page_table,
+                   const int32_t*& seq_lens, hipStream_t st);
+
 // ---------------------------------------------------------------- launchers
 // Each returns hipError_t of the launch (hipSuccess on success).
 
@@ -207,6 +220,10 @@ hipError_t launch_attend(const locks_cfg_t& c, const void* q, const void* k_cach
                          const void* v_cache, const int32_t* page_table, const int32_t* seq_lens,
                          const int32_t* page_ids, int pages_per_split, int n_splits,
                          float* partial, float* out, float* out_lse, hipStream_t st);
+
+// Combines the partials [S][H_q][splits][d + 2] (o unnormalised, max, sum) of every split.
+hipError_t launch_merge(const locks_cfg_t& c, int n_splits, const float* partial, float* out,
+                        float* out_lse, hipStream_t st);
 
 // Fused decode-step tail: the selection merge inside the attention kernel
 // (bf16 Q and KV, fast selection path), then the split merge.

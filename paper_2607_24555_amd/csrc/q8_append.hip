@@ -1,0 +1,259 @@
+// New tokens of a step, rotated, quantised and appended to the 8-bit cache
+// (locks_q8_append_kv), the rotated queries copied beside them in the same launch.
+//
+// One unit of the grid is a page that receives tokens, a KV head and keys or values; 16
+// tokens of it a wave (one, two or four waves), 16 lanes a token, eight elements a lane.
+// The unit holds its new rows in registers as rotated fp32 values, so a page's largest
+// magnitude, its scale and its codes come from one read.  Only where the scale of a page
+// with earlier rows grows are those rows read and rounded again.
+#include "rope.h"
+
+namespace locks {
+namespace {
+
+constexpr float kTiny = 7.888609052210118e-31f;  // 2^-100: smaller pages are stored as zeros
+
+// The scale of a page whose largest magnitude is amax.
+template <int kCode>
+__device__ __forceinline__ float page_scale(float amax) {
+  if (!(amax >= kTiny)) return 0.0f;
+  if constexpr (kCode == LOCKS_Q8_INT8) {
+    return amax / 127.0f;
+  } else {
+    // 2^e with amax <= 448 2^e = 1.75 2^(e + 8): from amax's exponent, one more where its
+    // mantissa passes 1.75
+    const uint32_t u = __float_as_uint(amax);
+    return __uint_as_float(((u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0)) << 23);
+  }
+}
+
+// Codes of eight scaled elements.
+template <int kCode>
+__device__ __forceinline__ uint2 codes_of(const float (&x)[8]) {
+  if constexpr (kCode == LOCKS_Q8_INT8) {
+    uint32_t b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float c = fminf(fmaxf(rintf(x[e]), -127.0f), 127.0f);
+      b[e] = (uint32_t)(int)(x[e] == x[e] ? c : 0.0f) & 0xffu;
+    }
+    return make_uint2(b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24),
+                      b[4] | (b[5] << 8) | (b[6] << 16) | (b[7] << 24));
+  } else {
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = x[e] == x[e] ? fminf(fmaxf(x[e], -448.0f), 448.0f) : x[e];
+    int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+    int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
+    return make_uint2((uint32_t)lo, (uint32_t)hi);
+  }
+}
+
+template <int kCode>
+__device__ __forceinline__ void values_of(uint2 w, float (&x)[8]) {
+  if constexpr (kCode == LOCKS_Q8_INT8) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = (float)(int8_t)(w.x >> (8 * e));
+      x[4 + e] = (float)(int8_t)(w.y >> (8 * e));
+    }
+  } else {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8(w.x, 0); x[1] = __builtin_amdgcn_cvt_f32_fp8(w.x, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8(w.x, 2); x[3] = __builtin_amdgcn_cvt_f32_fp8(w.x, 3);
+    x[4] = __builtin_amdgcn_cvt_f32_fp8(w.y, 0); x[5] = __builtin_amdgcn_cvt_f32_fp8(w.y, 1);
+    x[6] = __builtin_amdgcn_cvt_f32_fp8(w.y, 2); x[7] = __builtin_amdgcn_cvt_f32_fp8(w.y, 3);
+  }
+}
+
+// kWaves: waves per page (B / 16).  Blocks below page_blocks hold 4 / kWaves units each,
+// the others q_rows query rows of one token a wave, q_parts waves a token.
+template <typename QT, typename KT, int kCode, int kWaves>
+__global__ __launch_bounds__(256) void q8_append_kernel(
+    RowArgs a, RopeArgs rope, uint8_t* __restrict__ k_codes, uint8_t* __restrict__ v_codes,
+    float* __restrict__ k_scale, float* __restrict__ v_scale, const int32_t* __restrict__ page_table,
+    const int32_t* __restrict__ seq_lens, int S, int H_q, int H_kv, int max_pages, int num_blocks,
+    long n_units, unsigned page_blocks, int q_parts, int q_rows) {
+  constexpr int P = 16 * kWaves;
+  __shared__ float s_max[4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, cg = lane & 15, tg = lane >> 4;
+
+  if (blockIdx.x >= page_blocks) {  // query rows
+    const long id = (long)(blockIdx.x - page_blocks) * 4 + wave;
+    const long row_l = id / q_parts;
+    if (row_l >= a.n_tokens) return;
+    const int row = (int)row_l, part = (int)(id % q_parts);
+    int s = row;
+    if (a.cu) {
+      s = wave_search(S, row, [&](int i) { return a.cu[i]; });
+      if (s < 0) return;
+    }
+    const NewTokens t = new_tokens(a, seq_lens, s);
+    const int tok = t.tok0 + (row - t.row0);
+    if (row - t.row0 >= t.n || tok < 0 || tok / P >= max_pages) return;
+    const int blk = page_table[(long)s * max_pages + tok / P];
+    Angles A;
+    if (!load_angles(rope, row, tok, cg, A) || blk < 0 || blk >= num_blocks) return;
+    const int r0 = part * q_rows, r1 = min(r0 + q_rows, H_q);
+    const QT* q = static_cast<const QT*>(a.q) + row * a.q_stride + 8 * cg;
+    QT* out = static_cast<QT*>(a.q_out) + row * a.q_out_stride + 8 * cg;
+    for (int r = r0; r < r1; r += 4) {
+      const int ru = r + tg;
+      Row8<QT> w;
+      w.load(q + min(ru, r1 - 1) * kDim);
+      float x[8];
+      rotated(rope, A, w, lane, x);
+      if (ru < r1) {
+        if (rope.half) w.from(x);
+        w.store(out + ru * kDim);
+      }
+    }
+    return;
+  }
+
+  // ---- which (sequence, page, tensor, KV head) this wave belongs to
+  const long unit = (long)blockIdx.x * (4 / kWaves) + wave / kWaves;
+  bool live = unit < n_units;
+  const int h = (int)(unit % H_kv), kv = (int)(unit / H_kv % 2);
+  const long slot = unit / (2 * (long)H_kv);
+  // pages by slots: sequence s's begin at slot cu[s] / P + 2 s (it touches at most
+  // n / P + 2 pages); without cu one slot a sequence
+  int s = (int)slot, ahead = 0;
+  if (live && a.cu) {
+    s = wave_search(S, slot, [&](int i) { return (long)(a.cu[i] / P) + 2 * i; });
+    live = s >= 0;
+    if (live) ahead = (int)(slot - (a.cu[s] / P + 2 * (long)s));
+  }
+  NewTokens t{0, 0, 0};
+  if (live) t = new_tokens(a, seq_lens, s);
+  const int first = max(t.tok0, 0), L = t.tok0 + t.n;  // tokens [first, L) are new
+  const int j = first / P + ahead;
+  live = live && t.n > 0 && j < max_pages && (long)j * P < L;
+  int blk = -1;
+  if (live) {
+    blk = page_table[(long)s * max_pages + j];
+    live = blk >= 0 && blk < num_blocks;
+  }
+
+  // ---- the new rows of this wave's 16 tokens, rotated
+  const KT* src = static_cast<const KT*>(kv ? a.v : a.k) + h * kDim + 8 * cg;
+  const long stride = kv ? a.v_stride : a.k_stride;
+  const int i0 = 16 * (wave % kWaves) + tg;  // token row of the page, + 4 u
+  float x[4][8];
+  bool on[4];
+  Row8<KT> w[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int T = j * P + i0 + 4 * u;
+    on[u] = live && T >= first && T < L;
+    const long row = on[u] ? t.row0 + (T - t.tok0) : 0;
+    w[u].load(src + row * stride);
+  }
+  float big = -1.0f;  // stays so where no row is placed
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int T = j * P + i0 + 4 * u;
+    if (kv == 0) {
+      Angles A;
+      // (every lane takes part in the exchange; rows that are not new rotate something)
+      if (on[u]) on[u] = load_angles(rope, t.row0 + (T - t.tok0), T, cg, A);
+      rotated(rope, A, w[u], lane, x[u]);
+    } else {
+      if (on[u] && rope.half) {  // a token whose position is outside the table is left out
+        Angles A;
+        on[u] = load_angles(rope, t.row0 + (T - t.tok0), T, cg, A);
+      }
+      w[u].to(x[u]);
+    }
+    if (on[u]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float m = fabsf(x[u][e]);
+        big = fmaxf(big, m <= 3.402823466e38f ? m : 0.0f);
+      }
+    }
+  }
+  big = warp_max(big);
+  const long at = (long)(live ? blk : 0) * H_kv + h;
+  float* scale_at = (kv ? v_scale : k_scale) + at;
+  const float before = live ? *scale_at : 0.0f;
+  if constexpr (kWaves > 1) {  // every wave has read the old scale before it is replaced
+    if (lane == 0) s_max[wave] = big;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kWaves; ++u) big = fmaxf(big, s_max[wave / kWaves * kWaves + u]);
+  }
+  if (!live || big < 0.0f) return;
+  const int earlier = max(first - j * P, 0);  // rows of the page that were there before
+  float scale = page_scale<kCode>(big);
+  if (earlier > 0 && !(scale > before)) scale = before;
+  const float inv = scale > 0.0f ? 1.0f / scale : 0.0f;
+  uint8_t* codes = (kv ? v_codes : k_codes) + at * (P * kDim) + 8 * cg;
+  const bool grew = earlier > 0 && scale > before;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int i = i0 + 4 * u;
+    uint2* to = reinterpret_cast<uint2*>(codes + i * kDim);
+    if (on[u]) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = x[u][e] * inv;
+      *to = codes_of<kCode>(y);
+    } else if (grew && i < earlier) {
+      float y[8];
+      values_of<kCode>(*to, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = y[e] * before * inv;
+      *to = codes_of<kCode>(y);
+    }
+  }
+  if (wave % kWaves == 0 && lane == 0) *scale_at = scale;
+}
+
+template <typename QT, typename KT, int kCode>
+hipError_t launch_typed(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& r,
+                        const locks_q8_t& cache, const int32_t* page_table,
+                        const int32_t* seq_lens, hipStream_t st) {
+  const int hq = a.q ? c.num_q_heads : 0, P = c.page_size, waves = P / 16;
+  const long slots = a.cu ? a.n_tokens / P + 2L * c.num_seqs : c.num_seqs;
+  const long units = slots * 2 * c.num_kv_heads;
+  const long page_blocks = (units + 4 / waves - 1) / (4 / waves);
+  int per = 16;
+  while (per > 4 && (long)a.n_tokens * ((hq + per - 1) / per) < 4096) per /= 2;
+  const int q_parts = (hq + per - 1) / per;
+  const long q_blocks = ((long)a.n_tokens * q_parts + 3) / 4;
+  if (page_blocks + q_blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
+#define LOCKS_Q8_APPEND(W)                                                                        \
+  hipLaunchKernelGGL((q8_append_kernel<QT, KT, kCode, W>), dim3((unsigned)(page_blocks + q_blocks)), \
+                     dim3(256), 0, st, a, r, static_cast<uint8_t*>(cache.k),                       \
+                     static_cast<uint8_t*>(cache.v), cache.k_scale, cache.v_scale, page_table,    \
+                     seq_lens, c.num_seqs, hq, c.num_kv_heads, c.max_pages_per_seq, c.num_blocks, \
+                     units, (unsigned)page_blocks, q_parts, per)
+  if (waves == 1) LOCKS_Q8_APPEND(1);
+  else if (waves == 2) LOCKS_Q8_APPEND(2);
+  else LOCKS_Q8_APPEND(4);
+#undef LOCKS_Q8_APPEND
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_q8_append(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& r,
+                            const locks_q8_t& cache, const int32_t* page_table,
+                            const int32_t* seq_lens, hipStream_t st) {
+  const bool qb = !a.q || c.q_dtype == LOCKS_BF16, kb = c.kv_dtype == LOCKS_BF16;
+#define LOCKS_Q8_TYPES(C)                                                                          \
+  if (qb && kb) return launch_typed<uint16_t, uint16_t, C>(c, a, r, cache, page_table, seq_lens, st); \
+  if (qb) return launch_typed<uint16_t, float, C>(c, a, r, cache, page_table, seq_lens, st);       \
+  if (kb) return launch_typed<float, uint16_t, C>(c, a, r, cache, page_table, seq_lens, st);       \
+  return launch_typed<float, float, C>(c, a, r, cache, page_table, seq_lens, st)
+  if (cache.code == LOCKS_Q8_INT8) {
+    LOCKS_Q8_TYPES(LOCKS_Q8_INT8);
+  }
+  LOCKS_Q8_TYPES(LOCKS_Q8_E4M3);
+#undef LOCKS_Q8_TYPES
+}
+
+}  // namespace locks
