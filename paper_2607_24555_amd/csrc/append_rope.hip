@@ -1,42 +1,16 @@
 // New tokens of a step, rotated and appended to the paged caches (locks_rope_append_kv):
 // query rows from q to q_out, key and value rows into their slots, in one launch.
 //
-// A wave moves rows of one token, four at a time: 16 lanes a row, eight elements a lane
-// (16-byte accesses for bf16).  The angles of a lane's elements are loaded once and serve
-// every row of the wave; a pair half a row apart is exchanged between lanes.  Bound: HBM
-// for prompts, the chain length -> table entry -> store for a few tokens.
+// A wave moves rows of one token, four at a time with 16 lanes each.  A lane holds both
+// elements of its pairs, its four angles are loaded once and serve every row of the wave, and
+// the first rows are requested before the token's place is known.  Bound: HBM for prompts,
+// the chain length -> table entry -> store for a few tokens.
 #include "rope.h"
 
 namespace locks {
 namespace {
 
 constexpr int kRows = 4;  // rows in flight per 16 lanes
-
-// Rows [r0, r1) of a token, 4 at a time, from `src(r)` to `dst(r)` (null: not stored).
-template <typename T, typename Src>
-__device__ __forceinline__ void load_rows(Row8<T> (&w)[kRows], int r, int r1, Src src) {
-#pragma unroll
-  for (int u = 0; u < kRows; ++u) w[u].load(src(min(r + 4 * u, r1 - 1)));
-}
-
-template <typename T, typename Src, typename Dst>
-__device__ __forceinline__ void move_rows(const RopeArgs& rope, const Angles& A, Row8<T> (&w)[kRows], int lane,
-                                          int r0, int r1, int n_turned, Src src, Dst dst) {
-  for (int r = r0 + (lane >> 4);; r += 4 * kRows) {
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-      const int ru = r + 4 * u;
-      float x[8];
-      rotated(rope, A, w[u], lane, x);
-      if (ru < r1) {
-        if (ru < n_turned && rope.half) w[u].from(x);
-        w[u].store(dst(ru));
-      }
-    }
-    if (r - (lane >> 4) + 4 * kRows >= r1) return;
-    load_rows(w, r + 4 * kRows, r1, src);
-  }
-}
 
 // Waves per token: q_parts of q_rows query rows, then parts of kv_rows key and value rows
 // (keys first).
@@ -51,25 +25,27 @@ __global__ __launch_bounds__(256) void rope_append_kernel(
   const long row_l = id / parts;
   if (row_l >= a.n_tokens) return;
   const int row = (int)row_l, part = (int)(id % parts);
-  const int lane = threadIdx.x & 63, cg = lane & 15;
+  const int lane = threadIdx.x & 63;
   const bool is_q = part < q_parts;
 
-  // the first rows are requested before the token's place is known
   const int r0 = is_q ? part * q_rows : (part - q_parts) * kv_rows;
   const int r1 = is_q ? min(r0 + q_rows, H_q) : min(r0 + kv_rows, 2 * H_kv);
-  const QT* q = static_cast<const QT*>(a.q) + row * a.q_stride + 8 * cg;
-  const KT* k = static_cast<const KT*>(a.k) + row * a.k_stride + 8 * cg;
-  const KT* v = static_cast<const KT*>(a.v) + row * a.v_stride + 8 * cg;
+  const Lane ln = lane_of(rope, lane & 15);
+  const int32_t* cu = a.cu;
+  const int tg = lane >> 4;
+  const QT* q = static_cast<const QT*>(a.q) + row * a.q_stride;
+  const KT* k = static_cast<const KT*>(a.k) + row * a.k_stride;
+  const KT* v = static_cast<const KT*>(a.v) + row * a.v_stride;
   auto q_src = [&](int r) { return q + r * kDim; };
   auto kv_src = [&](int r) { return r < H_kv ? k + r * kDim : v + (r - H_kv) * kDim; };
-  Row8<QT> wq[kRows];
-  Row8<KT> wk[kRows];
-  if (is_q) load_rows(wq, r0 + (lane >> 4), r1, q_src);
-  else load_rows(wk, r0 + (lane >> 4), r1, kv_src);
+  Mover<QT, kRows> mq;
+  Mover<KT, kRows> mk;
+  if (is_q) mq.begin(ln, r0 + tg, r1, q_src);
+  else mk.begin(ln, r0 + tg, r1, kv_src);
 
   int s = row;
   if (a.cu) {
-    s = wave_search(S, row, [&](int i) { return a.cu[i]; });
+    s = wave_search(S, row, [cu](int i) { return cu[i]; });
     if (s < 0) return;
   }
   const NewTokens t = new_tokens(a, seq_lens, s);
@@ -77,15 +53,14 @@ __global__ __launch_bounds__(256) void rope_append_kernel(
   if (row - t.row0 >= t.n || tok < 0 || tok / pgsz >= max_pages) return;
   const long blk = page_table[(long)s * max_pages + tok / pgsz];
   Angles A;
-  const bool placed = load_angles(rope, row, tok, cg, A);
+  const bool placed = load_angles(rope, ln, row, tok, A);
   if (!placed || blk < 0 || blk >= num_blocks) return;
   if (is_q) {
-    QT* out = static_cast<QT*>(a.q_out) + row * a.q_out_stride + 8 * cg;
-    move_rows(rope, A, wq, lane, r0, r1, H_q, q_src, [&](int r) { return out + r * kDim; });
+    QT* out = static_cast<QT*>(a.q_out) + row * a.q_out_stride;
+    mq.move(rope, ln, A, tg, r0, r1, H_q, q_src, [&](int r) { return out + r * kDim; });
   } else {
-    const long at = (blk * H_kv * pgsz + tok % pgsz) * kDim + 8 * cg;
-    const long head = (long)pgsz * kDim;
-    move_rows(rope, A, wk, lane, r0, r1, H_kv, kv_src, [&](int r) {
+    const long at = (blk * H_kv * pgsz + tok % pgsz) * kDim, head = (long)pgsz * kDim;
+    mk.move(rope, ln, A, tg, r0, r1, H_kv, kv_src, [&](int r) {
       return r < H_kv ? k_cache + at + r * head : v_cache + at + (r - H_kv) * head;
     });
   }

@@ -598,13 +598,6 @@ hipError_t launch_mfma(const locks_cfg_t& c, dim3 grid, hipStream_t st, const ui
 
 }  // namespace
 
-hipError_t launch_merge(const locks_cfg_t& c, int n_splits, const float* partial, float* out,
-                        float* out_lse, hipStream_t st) {
-  hipLaunchKernelGGL(merge_kernel, dim3(c.num_q_heads, c.num_seqs), dim3(kDim), 0, st,
-                     c.num_q_heads, n_splits, partial, out, out_lse);
-  return hipGetLastError();
-}
-
 hipError_t launch_attend(const locks_cfg_t& c, const void* q, const void* k_cache,
                          const void* v_cache, const int32_t* page_table, const int32_t* seq_lens,
                          const int32_t* page_ids, int pages_per_split, int n_splits,
@@ -626,7 +619,9 @@ hipError_t launch_attend(const locks_cfg_t& c, const void* q, const void* k_cach
     launch_typed<float, float>(c, q, k_cache, v_cache, page_table, seq_lens, page_ids,
                                pages_per_split, n_splits, partial, out, out_lse, st);
   if (e != hipSuccess) return e;
-  if (n_splits > 1) return launch_merge(c, n_splits, partial, out, out_lse, st);
+  if (n_splits > 1)
+    hipLaunchKernelGGL(merge_kernel, dim3(c.num_q_heads, c.num_seqs), dim3(kDim), 0, st,
+                       c.num_q_heads, n_splits, partial, out, out_lse);
   return hipGetLastError();
 }
 
@@ -647,7 +642,9 @@ hipError_t launch_attend_select(const locks_cfg_t& c, const void* q, const void*
       static_cast<const uint16_t*>(k_cache), static_cast<const uint16_t*>(v_cache), page_table,
       seq_lens, nullptr, pages_per_split, n_splits, partial, out, out_lse, tb);
   if (e != hipSuccess) return e;
-  if (n_splits > 1) return launch_merge(c, n_splits, partial, out, out_lse, st);
+  if (n_splits > 1)
+    hipLaunchKernelGGL(merge_kernel, dim3(c.num_q_heads, c.num_seqs), dim3(kDim), 0, st,
+                       c.num_q_heads, n_splits, partial, out, out_lse);
   return hipGetLastError();
 }
 

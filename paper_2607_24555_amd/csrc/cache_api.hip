@@ -63,18 +63,25 @@ int append_args(const locks_cfg_t* c, const locks_rows_t* rows, const locks_rope
   return LOCKS_OK;
 }
 
-// Units (16 tokens) per block: 8, a pair per wave, doubled up to 256 while the grid exceeds
-// 1,024 blocks or the partials of the splits would not fit the workspace (which they may
-// take up to the checked tables; the plan's own split of the dense call always fits).
-int q8_units_per_split(const locks_cfg_t& c, long units) {
+// Equal shares for 512 blocks (two of the three that a compute unit holds: 8 ragged sequences,
+// 272K tokens, 111 us; 256 blocks 120, 768 114, 1,024 122), of at least 8 units (a pair per
+// wave), fewer where the workspace holds fewer partials (they may take it up to the checked
+// tables).  A block per list, without partials, where there are 512 lists of at most 64 units
+// (64 sequences x 8 KV heads, 16 units: 12 us against 20 with a merge), or the workspace holds
+// none.
+Q8Plan q8_plan(const locks_cfg_t& c, long list_units, bool listed) {
   const WsPlan p = plan_workspace(c);
   const long lists = (long)c.num_seqs * c.num_kv_heads;
-  const size_t row = (size_t)c.num_seqs * c.num_q_heads * (kDim + 2) * sizeof(float);
-  int per = 8;
-  while (per < 256 && (lists * ((units + per - 1) / per) > 1024 ||
-                       row * (size_t)((units + per - 1) / per) > p.chk_pt_off))
-    per *= 2;
-  return per;
+  const size_t slot = (size_t)(c.num_q_heads / c.num_kv_heads) * (kDim + 2) * sizeof(float);
+  const long room = (long)(p.chk_pt_off / slot) - lists;
+  list_units = (list_units + 7) / 8 * 8;  // (as the kernel counts a list)
+  long blocks = lists * list_units / 8;
+  blocks = blocks < 512 ? blocks : 512;
+  blocks = blocks < room ? blocks : room;
+  if ((lists >= 512 && list_units <= 64) || blocks < 1) return Q8Plan{0, 0};
+  if (!listed) return Q8Plan{(int)blocks, 0};
+  const long share = ((lists * list_units + blocks - 1) / blocks + 7) / 8 * 8;
+  return Q8Plan{(int)((lists * list_units + share - 1) / share), (int)share};
 }
 
 int q8_attend(const locks_cfg_t* cfg, const void* q, const locks_q8_t* cache,
@@ -88,12 +95,11 @@ int q8_attend(const locks_cfg_t* cfg, const void* q, const locks_q8_t* cache,
   if ((rc = check_ws(cfg, ws, ws_bytes))) return rc;
   if (cfg->num_seqs == 0) return LOCKS_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if ((rc = checked_tables(*cfg, ws, page_table, seq_lens, st))) return rc;
   const long units = (long)(listed ? page_budget(*cfg) : cfg->max_pages_per_seq) << sub_page_log2(*cfg);
-  const int per = q8_units_per_split(*cfg, units);
-  return hip_status(launch_q8_attend(*cfg, q, *cache, page_table, seq_lens, page_ids, per,
-                                     (int)((units + per - 1) / per), static_cast<float*>(ws), out,
-                                     out_lse, st));
+  if ((units + 7) * cfg->num_seqs * cfg->num_kv_heads > 0x7fffffffL) return LOCKS_E_UNSUPPORTED;
+  if ((rc = checked_tables(*cfg, ws, page_table, seq_lens, st))) return rc;
+  return hip_status(launch_q8_attend(*cfg, q, *cache, page_table, seq_lens, page_ids,
+                                     q8_plan(*cfg, units, listed), static_cast<float*>(ws), out, out_lse, st));
 }
 
 }  // namespace

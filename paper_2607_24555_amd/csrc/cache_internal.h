@@ -27,10 +27,16 @@ hipError_t launch_rope_append(const locks_cfg_t& c, const RowArgs& a, const Rope
 hipError_t launch_q8_append(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& r,
                             const locks_q8_t& cache, const int32_t* page_table,
                             const int32_t* seq_lens, hipStream_t st);
-// page_ids == nullptr: every page.  Units (16 tokens) per block and blocks per list.
+// How an attention over an 8-bit cache is split over blocks: `blocks` equal shares of all
+// lists' units, each of `share` units or (0) as many as the lengths come to; blocks = 0: one
+// block a list.
+struct Q8Plan {
+  int blocks, share;
+};
+// page_ids == nullptr: every page.  partial: blocks + lists slots of [G][130] floats.
 hipError_t launch_q8_attend(const locks_cfg_t& c, const void* q, const locks_q8_t& cache,
                             const int32_t* page_table, const int32_t* seq_lens,
-                            const int32_t* page_ids, int units_per_split, int n_splits,
-                            float* partial, float* out, float* out_lse, hipStream_t st);
+                            const int32_t* page_ids, const Q8Plan& plan, float* partial, float* out,
+                            float* out_lse, hipStream_t st);
 
 }  // namespace locks

@@ -221,10 +221,6 @@ hipError_t launch_attend(const locks_cfg_t& c, const void* q, const void* k_cach
                          const int32_t* page_ids, int pages_per_split, int n_splits,
                          float* partial, float* out, float* out_lse, hipStream_t st);
 
-// Combines the partials [S][H_q][splits][d + 2] (o unnormalised, max, sum) of every split.
-hipError_t launch_merge(const locks_cfg_t& c, int n_splits, const float* partial, float* out,
-                        float* out_lse, hipStream_t st);
-
 // Fused decode-step tail: the selection merge inside the attention kernel
 // (bf16 Q and KV, fast selection path), then the split merge.
 bool attend_select_fused(const locks_cfg_t& c);

@@ -1,10 +1,11 @@
 // New tokens of a step, rotated, quantised and appended to the 8-bit cache
 // (locks_q8_append_kv), the rotated queries copied beside them in the same launch.
 //
-// One unit of the grid is a page that receives tokens, a KV head and keys or values; 16
-// tokens of it a wave (one, two or four waves), 16 lanes a token, eight elements a lane.
-// The unit holds its new rows in registers as rotated fp32 values, so a page's largest
-// magnitude, its scale and its codes come from one read.  Only where the scale of a page
+// A unit of the grid is a page that receives tokens, keys or values, and a few KV heads;
+// 16 tokens of it a wave (one, two or four waves), 16 lanes a token, eight elements a lane.
+// The wave keeps its tokens' angles in registers for all its heads and holds a head's new rows
+// as rotated fp32 values, so that a page's largest magnitude, its scale and its codes come
+// from one read; the next head's rows are in flight meanwhile.  Only where the scale of a page
 // with earlier rows grows are those rows read and rounded again.
 #include "rope.h"
 
@@ -67,27 +68,37 @@ __device__ __forceinline__ void values_of(uint2 w, float (&x)[8]) {
   }
 }
 
-// kWaves: waves per page (B / 16).  Blocks below page_blocks hold 4 / kWaves units each,
-// the others q_rows query rows of one token a wave, q_parts waves a token.
+constexpr int kRows = 4;  // query rows in flight per 16 lanes
+
+// kWaves: waves per page (B / 16).  Blocks below page_blocks hold 4 / kWaves units of `heads`
+// KV heads each, head_parts units a page and tensor; the others q_rows query rows of one token
+// a wave, q_parts waves a token.
 template <typename QT, typename KT, int kCode, int kWaves>
 __global__ __launch_bounds__(256) void q8_append_kernel(
     RowArgs a, RopeArgs rope, uint8_t* __restrict__ k_codes, uint8_t* __restrict__ v_codes,
     float* __restrict__ k_scale, float* __restrict__ v_scale, const int32_t* __restrict__ page_table,
     const int32_t* __restrict__ seq_lens, int S, int H_q, int H_kv, int max_pages, int num_blocks,
-    long n_units, unsigned page_blocks, int q_parts, int q_rows) {
+    long n_units, unsigned page_blocks, int heads, int head_parts, int q_parts, int q_rows) {
   constexpr int P = 16 * kWaves;
-  __shared__ float s_max[4];
+  __shared__ float s_max[2][4];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63, cg = lane & 15, tg = lane >> 4;
+  const int lane = threadIdx.x & 63, tg = lane >> 4;
+  const Lane ln = lane_of(rope, lane & 15);
+  const int32_t* cu = a.cu;
 
   if (blockIdx.x >= page_blocks) {  // query rows
     const long id = (long)(blockIdx.x - page_blocks) * 4 + wave;
     const long row_l = id / q_parts;
     if (row_l >= a.n_tokens) return;
     const int row = (int)row_l, part = (int)(id % q_parts);
+    const int r0 = part * q_rows, r1 = min(r0 + q_rows, H_q);
+    const QT* q = static_cast<const QT*>(a.q) + row * a.q_stride;
+    auto src = [&](int r) { return q + r * kDim; };
+    Mover<QT, kRows> mq;
+    mq.begin(ln, r0 + tg, r1, src);
     int s = row;
     if (a.cu) {
-      s = wave_search(S, row, [&](int i) { return a.cu[i]; });
+      s = wave_search(S, row, [cu](int i) { return cu[i]; });
       if (s < 0) return;
     }
     const NewTokens t = new_tokens(a, seq_lens, s);
@@ -95,34 +106,23 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
     if (row - t.row0 >= t.n || tok < 0 || tok / P >= max_pages) return;
     const int blk = page_table[(long)s * max_pages + tok / P];
     Angles A;
-    if (!load_angles(rope, row, tok, cg, A) || blk < 0 || blk >= num_blocks) return;
-    const int r0 = part * q_rows, r1 = min(r0 + q_rows, H_q);
-    const QT* q = static_cast<const QT*>(a.q) + row * a.q_stride + 8 * cg;
-    QT* out = static_cast<QT*>(a.q_out) + row * a.q_out_stride + 8 * cg;
-    for (int r = r0; r < r1; r += 4) {
-      const int ru = r + tg;
-      Row8<QT> w;
-      w.load(q + min(ru, r1 - 1) * kDim);
-      float x[8];
-      rotated(rope, A, w, lane, x);
-      if (ru < r1) {
-        if (rope.half) w.from(x);
-        w.store(out + ru * kDim);
-      }
-    }
+    if (!load_angles(rope, ln, row, tok, A) || blk < 0 || blk >= num_blocks) return;
+    QT* out = static_cast<QT*>(a.q_out) + row * a.q_out_stride;
+    mq.move(rope, ln, A, tg, r0, r1, H_q, src, [&](int r) { return out + r * kDim; });
     return;
   }
 
-  // ---- which (sequence, page, tensor, KV head) this wave belongs to
+  // ---- which (sequence, page, tensor, KV heads) this wave belongs to
   const long unit = (long)blockIdx.x * (4 / kWaves) + wave / kWaves;
   bool live = unit < n_units;
-  const int h = (int)(unit % H_kv), kv = (int)(unit / H_kv % 2);
-  const long slot = unit / (2 * (long)H_kv);
+  const int h0 = (int)(unit % head_parts) * heads, h1 = min(h0 + heads, H_kv);
+  const int kv = (int)(unit / head_parts % 2);
+  const long slot = unit / (2 * (long)head_parts);
   // pages by slots: sequence s's begin at slot cu[s] / P + 2 s (it touches at most
   // n / P + 2 pages); without cu one slot a sequence
   int s = (int)slot, ahead = 0;
   if (live && a.cu) {
-    s = wave_search(S, slot, [&](int i) { return (long)(a.cu[i] / P) + 2 * i; });
+    s = wave_search(S, slot, [cu](int i) { return (long)(cu[i] / P) + 2 * i; });
     live = s >= 0;
     if (live) ahead = (int)(slot - (a.cu[s] / P + 2 * (long)s));
   }
@@ -136,80 +136,88 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
     blk = page_table[(long)s * max_pages + j];
     live = blk >= 0 && blk < num_blocks;
   }
+  // (the same for the block's waves of a page, so a page's waves leave together; pages of
+  // several waves meet at the barriers below)
+  if (kWaves == 1 && !live) return;
 
-  // ---- the new rows of this wave's 16 tokens, rotated
-  const KT* src = static_cast<const KT*>(kv ? a.v : a.k) + h * kDim + 8 * cg;
-  const long stride = kv ? a.v_stride : a.k_stride;
+  // ---- this wave's 16 tokens: where they are in the input, and their angles
   const int i0 = 16 * (wave % kWaves) + tg;  // token row of the page, + 4 u
-  float x[4][8];
+  const int earlier = max(first - j * P, 0);  // rows of the page that were there before
+  const KT* src = static_cast<const KT*>(kv ? a.v : a.k);
+  const long stride = kv ? a.v_stride : a.k_stride;
+  long from[4];
   bool on[4];
   Row8<KT> w[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int T = j * P + i0 + 4 * u;
     on[u] = live && T >= first && T < L;
-    const long row = on[u] ? t.row0 + (T - t.tok0) : 0;
-    w[u].load(src + row * stride);
+    from[u] = on[u] ? (t.row0 + (T - t.tok0)) * stride : 0;
+    w[u].load(src + from[u] + h0 * kDim, ln.a, ln.b);
   }
-  float big = -1.0f;  // stays so where no row is placed
+  Angles A[4];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int T = j * P + i0 + 4 * u;
-    if (kv == 0) {
-      Angles A;
-      // (every lane takes part in the exchange; rows that are not new rotate something)
-      if (on[u]) on[u] = load_angles(rope, t.row0 + (T - t.tok0), T, cg, A);
-      rotated(rope, A, w[u], lane, x[u]);
-    } else {
-      if (on[u] && rope.half) {  // a token whose position is outside the table is left out
-        Angles A;
-        on[u] = load_angles(rope, t.row0 + (T - t.tok0), T, cg, A);
-      }
+    if (on[u]) on[u] = load_angles(rope, ln, t.row0 + (T - t.tok0), T, A[u]);  // a position outside: left out
+  }
+  for (int h = h0; h < h0 + heads; ++h) {  // (as many rounds for every wave)
+    float x[4][8];
+    float big = -1.0f;  // stays so where no row is placed
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
       w[u].to(x[u]);
-    }
-    if (on[u]) {
+      if (kv == 0) rotate(rope, ln, A[u], x[u]);
+      if (on[u]) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float m = fabsf(x[u][e]);
-        big = fmaxf(big, m <= 3.402823466e38f ? m : 0.0f);
+        for (int e = 0; e < 8; ++e) {
+          const float m = fabsf(x[u][e]);
+          big = fmaxf(big, m <= 3.402823466e38f ? m : 0.0f);
+        }
       }
     }
-  }
-  big = warp_max(big);
-  const long at = (long)(live ? blk : 0) * H_kv + h;
-  float* scale_at = (kv ? v_scale : k_scale) + at;
-  const float before = live ? *scale_at : 0.0f;
-  if constexpr (kWaves > 1) {  // every wave has read the old scale before it is replaced
-    if (lane == 0) s_max[wave] = big;
-    __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kWaves; ++u) big = fmaxf(big, s_max[wave / kWaves * kWaves + u]);
-  }
-  if (!live || big < 0.0f) return;
-  const int earlier = max(first - j * P, 0);  // rows of the page that were there before
-  float scale = page_scale<kCode>(big);
-  if (earlier > 0 && !(scale > before)) scale = before;
-  const float inv = scale > 0.0f ? 1.0f / scale : 0.0f;
-  uint8_t* codes = (kv ? v_codes : k_codes) + at * (P * kDim) + 8 * cg;
-  const bool grew = earlier > 0 && scale > before;
+    for (int u = 0; u < 4; ++u) w[u].load(src + from[u] + min(h + 1, h1 - 1) * kDim, ln.a, ln.b);
+    big = warp_max(big);
+    const long at = (long)(live ? blk : 0) * H_kv + min(h, h1 - 1);
+    float* scale_at = (kv ? v_scale : k_scale) + at;
+    const float before = live && earlier > 0 ? *scale_at : 0.0f;
+    if constexpr (kWaves > 1) {  // every wave has read the old scale before it is replaced
+      if (lane == 0) s_max[h & 1][wave] = big;
+      __syncthreads();
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int i = i0 + 4 * u;
-    uint2* to = reinterpret_cast<uint2*>(codes + i * kDim);
-    if (on[u]) {
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = x[u][e] * inv;
-      *to = codes_of<kCode>(y);
-    } else if (grew && i < earlier) {
-      float y[8];
-      values_of<kCode>(*to, y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = y[e] * before * inv;
-      *to = codes_of<kCode>(y);
+      for (int u = 0; u < kWaves; ++u) big = fmaxf(big, s_max[h & 1][wave / kWaves * kWaves + u]);
     }
+    if (!live || big < 0.0f || h >= h1) continue;
+    float scale = page_scale<kCode>(big);
+    if (earlier > 0 && !(scale > before)) scale = before;
+    const float inv = scale > 0.0f ? 1.0f / scale : 0.0f;
+    uint8_t* codes = (kv ? v_codes : k_codes) + at * (P * kDim);
+    const bool grew = earlier > 0 && scale > before;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + 4 * u;
+      uint32_t* to_a = reinterpret_cast<uint32_t*>(codes + i * kDim + ln.a);
+      uint32_t* to_b = reinterpret_cast<uint32_t*>(codes + i * kDim + ln.b);
+      float y[8];
+      bool put = on[u];
+      if (on[u]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = x[u][e] * inv;
+      } else if (grew && i < earlier) {
+        values_of<kCode>(make_uint2(*to_a, *to_b), y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = y[e] * before * inv;
+        put = true;
+      }
+      if (put) {
+        const uint2 c = codes_of<kCode>(y);
+        *to_a = c.x;
+        *to_b = c.y;
+      }
+    }
+    if (wave % kWaves == 0 && lane == 0) *scale_at = scale;
   }
-  if (wave % kWaves == 0 && lane == 0) *scale_at = scale;
 }
 
 template <typename QT, typename KT, int kCode>
@@ -218,7 +226,11 @@ hipError_t launch_typed(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& 
                         const int32_t* seq_lens, hipStream_t st) {
   const int hq = a.q ? c.num_q_heads : 0, P = c.page_size, waves = P / 16;
   const long slots = a.cu ? a.n_tokens / P + 2L * c.num_seqs : c.num_seqs;
-  const long units = slots * 2 * c.num_kv_heads;
+  // heads per unit: up to 4 while 4,096 waves remain
+  int heads = c.num_kv_heads < 4 ? c.num_kv_heads : 4;
+  while (heads > 1 && slots * 2 * waves * ((c.num_kv_heads + heads - 1) / heads) < 4096) --heads;
+  const int head_parts = (c.num_kv_heads + heads - 1) / heads;
+  const long units = slots * 2 * head_parts;
   const long page_blocks = (units + 4 / waves - 1) / (4 / waves);
   int per = 16;
   while (per > 4 && (long)a.n_tokens * ((hq + per - 1) / per) < 4096) per /= 2;
@@ -230,7 +242,7 @@ hipError_t launch_typed(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& 
                      dim3(256), 0, st, a, r, static_cast<uint8_t*>(cache.k),                       \
                      static_cast<uint8_t*>(cache.v), cache.k_scale, cache.v_scale, page_table,    \
                      seq_lens, c.num_seqs, hq, c.num_kv_heads, c.max_pages_per_seq, c.num_blocks, \
-                     units, (unsigned)page_blocks, q_parts, per)
+                     units, (unsigned)page_blocks, heads, head_parts, q_parts, per)
   if (waves == 1) LOCKS_Q8_APPEND(1);
   else if (waves == 2) LOCKS_Q8_APPEND(2);
   else LOCKS_Q8_APPEND(4);

@@ -3,65 +3,85 @@
 //   o_g = sum_i softmax_i(sk q_g^T ck_i / sqrt d) sv cv_i
 // over the listed pages' tokens (page_ids == nullptr: every page).
 //
-// Split-K as in the bf16 kernel: block (split, KV head, seq), four waves with consecutive
-// units (16 tokens) of the list, one partial (o, max, sum) a block, merged afterwards.  A wave
-// takes two units a step on the matrix cores and holds the next two units' codes in flight.
-// Codes are exact in bf16 (int8: 7 bits and sign; e4m3: 4 bits), so the products with a bf16
-// query are too; the key scale multiplies the logits, the value scale the weights, which enter
-// as bf16 hi + lo.  fp32 queries enter as three bf16 terms (24 bits).
+// A list is one (sequence, KV head); its units are 16 tokens each.  The units of all lists in
+// order are cut into equal shares, one a block, by the lengths themselves (read on the device:
+// a table's width says little about them), so a block's share may end one list and begin
+// others.  Its four waves take consecutive quarters of each list's piece, and the piece leaves
+// one partial (o, max, sum) in slot block + list -- either grows from piece to piece, and a
+// list's slots are consecutive -- merged afterwards.  Many short lists take a block each and no
+// merge.  A wave
+// takes two units a step on the matrix cores.  Codes are exact in f16 (int8: 7 bits and sign;
+// e4m3: 4 bits), the key scale multiplies the logits, the value scale the weights, which enter
+// as f16 hi + lo (21 bits; in bf16 hi + lo, 16 bits, they cost three times the error: 2.7e-6
+// against 8e-7 over tables of 256 tokens).
 #include "cache_internal.h"
 
 namespace locks {
 namespace {
 
-typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
-typedef __bf16 bf2v __attribute__((ext_vector_type(2)));
-typedef float f2v __attribute__((ext_vector_type(2)));
+typedef _Float16 h8v __attribute__((ext_vector_type(8)));
+typedef _Float16 h2v __attribute__((ext_vector_type(2)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2v{a, b}, bf2v));
+__device__ __forceinline__ h8v as_h8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_bit_cast(h8v, make_uint4(a, b, c, d));
 }
-__device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ bf8v as_bf8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  return __builtin_bit_cast(bf8v, make_uint4(a, b, c, d));
+// Two floats as f16 halves of a word, rounded toward zero, and what that leaves of them.
+__device__ __forceinline__ uint32_t split_h2(float& a, float& b) {
+  const h2v h = __builtin_bit_cast(h2v, __builtin_amdgcn_cvt_pkrtz(a, b));
+  a -= (float)h[0];
+  b -= (float)h[1];
+  return __builtin_bit_cast(uint32_t, h);
 }
 
-// Four codes (one word) as two words of bf16 pairs, in order.
+// Codes widen to f16 exactly, times kUnit: int8 c as c 2^-9, e4m3 as itself.
+template <int kCode>
+constexpr float kUnit = kCode == LOCKS_Q8_INT8 ? 512.0f : 1.0f;  // what a widened 1 stands for
+
+// int8: excess-128 bytes u in the low halves' low bytes are the f16 subnormals u 2^-24, and
+// one packed multiply-add makes (u - 128) 2^-9 of them.
+__device__ __forceinline__ uint32_t int8_h2(uint32_t w) {
+  const h2v x = __builtin_bit_cast(h2v, w);
+  const h2v y = __builtin_elementwise_fma(x, h2v{(_Float16)32768.0f, (_Float16)32768.0f},
+                                          h2v{(_Float16)-0.25f, (_Float16)-0.25f});
+  return __builtin_bit_cast(uint32_t, y);
+}
+// e4m3: bytes 0 and 1 (kHigh: 2 and 3) of w.
+template <bool kHigh>
+__device__ __forceinline__ uint32_t e4m3_h2(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, kHigh));
+}
+
+// Four codes (one word) as two words of f16 pairs, in order.
 template <int kCode>
 __device__ __forceinline__ void widen(uint32_t w, uint32_t& a, uint32_t& b) {
   if constexpr (kCode == LOCKS_Q8_INT8) {
-    // small integers: the upper halves of their floats are their bf16 values
-    const uint32_t f0 = __float_as_uint((float)(int8_t)w), f1 = __float_as_uint((float)(int8_t)(w >> 8));
-    const uint32_t f2 = __float_as_uint((float)(int8_t)(w >> 16)), f3 = __float_as_uint((float)((int32_t)w >> 24));
-    a = __builtin_amdgcn_perm(f1, f0, 0x07060302u);
-    b = __builtin_amdgcn_perm(f3, f2, 0x07060302u);
+    w ^= 0x80808080u;
+    a = int8_h2(__builtin_amdgcn_perm(0u, w, 0x0c010c00u));
+    b = int8_h2(__builtin_amdgcn_perm(0u, w, 0x0c030c02u));
   } else {
-    a = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
-    b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+    a = e4m3_h2<false>(w);
+    b = e4m3_h2<true>(w);
   }
 }
 
 // Codes of four tokens (words t0 .. t3 hold four elements each) as, per element e, the
-// bf16 pairs (t0, t1) in p[e] and (t2, t3) in q[e].
+// f16 pairs (t0, t1) in p[e] and (t2, t3) in q[e].
 template <int kCode>
 __device__ __forceinline__ void widen_across(uint32_t t0, uint32_t t1, uint32_t t2, uint32_t t3,
                                              uint32_t (&p)[4], uint32_t (&q)[4]) {
   if constexpr (kCode == LOCKS_Q8_INT8) {
-    const uint32_t t[4] = {t0, t1, t2, t3};
-    uint32_t f[4][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[j][e] = __float_as_uint((float)(int8_t)(t[j] >> (8 * e)));
+    t0 ^= 0x80808080u;
+    t1 ^= 0x80808080u;
+    t2 ^= 0x80808080u;
+    t3 ^= 0x80808080u;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      p[e] = __builtin_amdgcn_perm(f[1][e], f[0][e], 0x07060302u);
-      q[e] = __builtin_amdgcn_perm(f[3][e], f[2][e], 0x07060302u);
+      p[e] = int8_h2(__builtin_amdgcn_perm(t1, t0, 0x0c040c00u + 0x00010001u * e));
+      q[e] = int8_h2(__builtin_amdgcn_perm(t3, t2, 0x0c040c00u + 0x00010001u * e));
     }
   } else {
     // element 0 of two tokens, then element 1 (then 2 and 3): pairs the conversion widens
@@ -86,11 +106,99 @@ __device__ __forceinline__ float rows_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Codes of two units.  Lane (c = l % 16, r = l / 16):
-//   k[u][a]: token c, dims 64 a + 16 r .. + 15      v[u][j]: token 4 r + j, dims 8 c .. + 7
-struct Codes {
-  uint4 k[2][2];
-  uint2 v[2][4];
+// Power of two, exponent clamped to what a float holds.
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+__device__ __forceinline__ int exponent(float v) { return (int)(__float_as_uint(v) >> 23 & 255u) - 127; }
+
+// How the lists' units are cut: shares of `share` units (a multiple of 8; 0: a block per list,
+// no partials), or, where `blocks` is set, total / blocks rounded up to such a multiple.
+struct Cut {
+  int fixed_units;  // units of every list (a table's), or 0: the sequence's own
+  int share, blocks;
+};
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int units_of(int len) { return max((len + kPage - 1) / kPage, 0); }
+// A list counts as a multiple of 8 units, so that at the smallest share no block holds a piece
+// of two lists, one after the other (8 heads over 4,099 tokens: 13.0 -> 11.2 us).
+__device__ __forceinline__ int padded(int units) { return (units + 7) & ~7; }
+
+__device__ __forceinline__ int wave_scan(int v) {  // inclusive sums over the wave
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+__device__ __forceinline__ unsigned share_of(const Cut& cut, unsigned units) {
+  if (!cut.blocks) return cut.share;
+  const unsigned per = (units + cut.blocks - 1) / cut.blocks;
+  return per < 8 ? 8 : (per + 7) / 8 * 8;
+}
+// The sequences' lengths and places in the lists' order (units of all lists fit 31 bits, which
+// the host checks).  Up to 64 sequences are one load and one scan, kept in a register.
+struct Order {
+  const int32_t* seq_lens;
+  int S, H_kv, fixed;
+  int len, end;    // S <= 64, lane i: sequence i's length; units of one KV head up to and with it
+  unsigned units;  // of all sequences and KV heads
+  __device__ __forceinline__ Order(const Cut& cut, const int32_t* sl, int S_, int H)
+      : seq_lens(sl), S(S_), H_kv(H), fixed(cut.fixed_units) {
+    const int lane = threadIdx.x & 63;
+    len = S <= 64 && lane < S ? seq_lens[lane] : 0;
+    end = 0;
+    if (fixed) {
+      units = (unsigned)S * padded(fixed) * H_kv;
+      return;
+    }
+    int sum = 0;
+    for (int s0 = 0; s0 < S; s0 += 64) {
+      end = scan_from(s0, sum);
+      sum = __builtin_amdgcn_readlane(end, 63);
+    }
+    units = (unsigned)sum * H_kv;
+  }
+  __device__ __forceinline__ int scan_from(int s0, int sum) const {
+    const int i = s0 + (threadIdx.x & 63);
+    return sum + wave_scan(padded(units_of(S <= 64 ? len : (i < S ? seq_lens[i] : 0))));
+  }
+  // s is wave-uniform
+  __device__ __forceinline__ int length(int s) const {
+    return S <= 64 ? __builtin_amdgcn_readlane(len, s) : seq_lens[s];
+  }
+  __device__ __forceinline__ int list_units(int s) const { return padded(fixed ? fixed : units_of(length(s))); }
+  // Units of one KV head before sequence s.
+  __device__ __forceinline__ int before(int s) const {
+    if (fixed) return s * padded(fixed);
+    int e = end, sum = 0;
+    for (int s0 = 0; S > 64 && s0 <= s; s0 += 64) {
+      e = scan_from(s0, sum);
+      if (s0 + 64 <= s) sum = __builtin_amdgcn_readlane(e, 63);
+    }
+    return (s & 63) ? __builtin_amdgcn_readlane(e, (s & 63) - 1) : sum;
+  }
+  // The sequence that unit u of the lists belongs to (u < units), and before() of it.
+  __device__ __forceinline__ int find(unsigned u, int& bef) const {
+    if (fixed) {
+      const int s = (int)(u / ((unsigned)padded(fixed) * H_kv));
+      bef = s * padded(fixed);
+      return s;
+    }
+    int e = end, sum = 0;
+    for (int s0 = 0; s0 < S; s0 += 64) {
+      if (S > 64) e = scan_from(s0, sum);
+      const unsigned long long past = __ballot((unsigned)e * H_kv > u);
+      if (past) {
+        const int i = __ffsll(past) - 1;
+        bef = i > 0 ? __builtin_amdgcn_readlane(e, i - 1) : sum;
+        return s0 + i;
+      }
+      sum = __builtin_amdgcn_readlane(e, 63);
+    }
+    bef = sum;
+    return S - 1;
+  }
 };
 
 // Lane layout (l = 16 r + c):
@@ -99,99 +207,162 @@ struct Codes {
 //   O^T += V^T P (mfma 16x16x32, M = dim, N = head, K = (r, 4 u + j) = token 4 r + j of
 //                 unit u; tile n covers dims 8 m + n): P is the B operand exactly as S^T
 //                 left it, and lane holds O^T for head c, dims 32 r + 8 j + n.
+// Codes of two units, lane (c, r): k[u][a] token c, dims 64 a + 16 r .. + 15; v[u][j] token
+// 4 r + j, dims 8 c .. + 7.  Each half of the next pair is requested as soon as its registers
+// are free: the keys after the logits' products, the values after the outputs'.
 template <typename QT, int kCode>
-__global__ __launch_bounds__(256) void q8_attend_kernel(
-    int H_q, int H_kv, int max_pages, int k_list, int pgsz, int lg_sub, const QT* __restrict__ q,
+__global__ __launch_bounds__(256, 3) void q8_attend_kernel(
+    int S, int H_q, int H_kv, int max_pages, int k_list, int pgsz, int lg_sub, const QT* __restrict__ q,
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ v_codes,
     const float* __restrict__ k_scale, const float* __restrict__ v_scale,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ seq_lens,
-    const int32_t* __restrict__ page_ids, int units_per_split, int n_splits,
-    float* __restrict__ partial, float* __restrict__ out, float* __restrict__ out_lse) {
-  constexpr int kTerms = sizeof(QT) == 2 ? 1 : 3;
+    const int32_t* __restrict__ page_ids, Cut cut, float* __restrict__ partial, float* __restrict__ out,
+    float* __restrict__ out_lse) {
+  constexpr int kTerms = sizeof(QT) == 2 ? 1 : 2;
   __shared__ float sO[4][kDim][kMaxGroup + 1];
   __shared__ float sM[4][kMaxGroup], sL[4][kMaxGroup];
-  const int split = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int c16 = lane & 15, r4 = lane >> 4;
   const int G = H_q / H_kv;
-  const int L = seq_lens[s];
-  const int n = (L + pgsz - 1) / pgsz;
-  const int upw = units_per_split / 4;  // units per wave, at most 64
-  const int t_begin = split * units_per_split + wave * upw;
+  const long page_bytes = (long)pgsz * kDim;
+  const int k_off = c16 * kDim + 16 * r4, v_off = 4 * r4 * kDim + 8 * c16;
 
-  // ---- lane j: the wave's unit j (first token, or -1: nothing to attend), its codes and scales
-  int my_tok = -1, my_blk = 0;
-  float my_ks = 0.0f, my_vs = 0.0f;
-  if (lane < upw) {
-    const int t = t_begin + lane, entry = t >> lg_sub;
-    int id = entry;
-    if (page_ids) id = entry < k_list ? page_ids[((long)s * H_kv + h) * k_list + entry] : -1;
-    if (id >= 0 && id < n) {
-      const int tok0 = id * pgsz + (t & ((1 << lg_sub) - 1)) * kPage;
-      if (tok0 < L) {
-        my_tok = tok0;
-        my_blk = page_table[(long)s * max_pages + id];
-        my_ks = k_scale[(long)my_blk * H_kv + h] * (kLog2e / 11.313708498984761f);  // / sqrt(128)
-        my_vs = v_scale[(long)my_blk * H_kv + h];
-      }
-    }
+  // ---- the block's share of the units (wave-uniform, on the scalar unit)
+  const Order order(cut, seq_lens, S, H_kv);
+  int s, h, at = 0, left;  // list (s, h), first unit within it, units of the share still to do
+  const bool whole = cut.share == 0 && cut.blocks == 0;
+  if (whole) {
+    s = blockIdx.x / H_kv;
+    h = blockIdx.x % H_kv;
+    left = order.list_units(s);
+  } else {
+    const unsigned share = share_of(cut, order.units), u0 = blockIdx.x * share;
+    if (u0 >= order.units) return;
+    left = uniform((int)min(share, order.units - u0));
+    int before;
+    s = uniform(order.find(u0, before));
+    const unsigned n = order.list_units(s), in = u0 - (unsigned)before * H_kv;
+    h = uniform((int)(in / n));
+    at = uniform((int)(in - h * n));
   }
-  const unsigned long long live = __ballot(my_tok >= 0);
-  const int cnt = live ? 64 - __clzll(live) : 0;  // units up to the last one with tokens
-  // an empty unit's loads read another unit of the wave
-  const int spare = live ? __ffsll((unsigned long long)live) - 1 : 0;
 
-  // ---- queries: B operand of step 2 a + b, in kTerms bf16 terms
+  while (true) {  // one piece: units [at, at + n) of list (s, h)
+  const int L = uniform(order.length(s));
+  const int real = order.fixed ? order.fixed : units_of(L);
+  const int taken = min(left, padded(real) - at), n = min(taken, real - at);
+  const int per_wave = ((n + 3) / 4 + 1) & ~1;
+  const int w_begin = min(wave * per_wave, n), w_end = min(w_begin + per_wave, n);
+
+  // ---- queries: B operand of step 2 a + b, scaled by a power of two per head so that the
+  // largest element is in [2^14, 2^15): f16 holds a bf16 element then to 2^-40 of the largest,
+  // and a float in two terms to 2^-21 of itself
   uint4 qb[kTerms][4];
+  float head_scale;  // logits in log2 units = products * head_scale * key scale
   {
     const QT* row = q + ((long)s * H_q + h * G + min(c16, G - 1)) * kDim + 16 * r4;
+    float x[4][8], big = 0.0f;
 #pragma unroll
     for (int st = 0; st < 4; ++st) {
       const QT* p = row + 64 * (st >> 1) + 8 * (st & 1);
-      if constexpr (kTerms == 1) {
-        qb[0][st] = *reinterpret_cast<const uint4*>(p);
+      if constexpr (sizeof(QT) == 2) {
+        const uint4 w = *reinterpret_cast<const uint4*>(p);
+        const uint32_t y[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[st][2 * e] = __uint_as_float(y[e] << 16);
+          x[st][2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u);
+        }
       } else {
         const float4 x0 = reinterpret_cast<const float4*>(p)[0], x1 = reinterpret_cast<const float4*>(p)[1];
-        float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+        x[st][0] = x0.x; x[st][1] = x0.y; x[st][2] = x0.z; x[st][3] = x0.w;
+        x[st][4] = x1.x; x[st][5] = x1.y; x[st][6] = x1.z; x[st][7] = x1.w;
+      }
 #pragma unroll
-        for (int m = 0; m < kTerms; ++m) {
-          uint32_t w[4];
+      for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[st][e]));
+    }
+    const int e2 = min(14 - exponent(rows_max(big)), 126);
+    const float up = pow2(e2);
+    head_scale = pow2(-e2) * (kUnit<kCode> * kLog2e / 11.313708498984761f);  // / sqrt(128)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            w[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
-            x[2 * e] -= lo_f(w[e]);
-            x[2 * e + 1] -= hi_f(w[e]);
-          }
-          qb[m][st] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+    for (int st = 0; st < 4; ++st) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[st][e] *= up;
+#pragma unroll
+      for (int m = 0; m < kTerms; ++m) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = split_h2(x[st][2 * e], x[st][2 * e + 1]);
+        qb[m][st] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
   }
-
-  const long page_bytes = (long)pgsz * kDim;
-  const int k_off = c16 * kDim + 16 * r4, v_off = 4 * r4 * kDim + 8 * c16;
-  auto load_pair = [&](Codes& C, int j) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int i = j + u < cnt && ((live >> (j + u)) & 1) ? j + u : spare;
-      const long blk = __builtin_amdgcn_readlane(my_blk, i);
-      const int tok0 = __builtin_amdgcn_readlane(my_tok, i);
-      const long base = (blk * H_kv + h) * page_bytes + (long)(tok0 & (pgsz - 1)) * kDim;
-      const uint8_t* kp = k_codes + base + k_off;
-      const uint8_t* vp = v_codes + base + v_off;
-#pragma unroll
-      for (int a = 0; a < 2; ++a) C.k[u][a] = *reinterpret_cast<const uint4*>(kp + 64 * a);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) C.v[u][t] = *reinterpret_cast<const uint2*>(vp + t * kDim);
-    }
-  };
-
   float m = -INFINITY, l = 0.0f;  // l: this lane's tokens only
+  int ve = -126;                  // o is in units of 2^ve (times 2^-15 and the codes' unit)
   f4v o[8];
 #pragma unroll
-  for (int t = 0; t < 8; ++t) o[t] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int n = 0; n < 8; ++n) o[n] = f4v{0.0f, 0.0f, 0.0f, 0.0f};
 
-  auto use_pair = [&](Codes& C, int j) {
+  // 64 units a round.  Lane j: the round's unit j (first token, or -1: nothing to attend), its
+  // codes and scales
+  for (int i0 = w_begin; i0 < w_end; i0 += 64) {
+  const int t = at + i0 + lane, entry = t >> lg_sub;
+  const bool mine = i0 + lane < w_end;
+  int id = entry;
+  if (page_ids) id = mine && entry < k_list ? page_ids[((long)s * H_kv + h) * k_list + entry] : -1;
+  int my_tok = -1, my_blk = 0;
+  float my_ks = 0.0f, my_vs = 0.0f;
+  if (mine && id >= 0 && id < (L + pgsz - 1) / pgsz) {
+    const int tok0 = id * pgsz + (t & ((1 << lg_sub) - 1)) * kPage;
+    if (tok0 < L) {
+      my_tok = tok0;
+      my_blk = page_table[(long)s * max_pages + id];
+      my_ks = k_scale[(long)my_blk * H_kv + h];
+      my_vs = v_scale[(long)my_blk * H_kv + h];
+    }
+  }
+  const unsigned long long live = __ballot(my_tok >= 0);
+  if (!live) continue;
+  const int cnt = 64 - __clzll(live);     // units up to the last one with tokens
+  const int spare = __ffsll(live) - 1;    // an empty unit's loads read another unit
+
+  auto unit_at = [&](int j) -> long {
+    const int i = j < cnt && ((live >> j) & 1) ? j : spare;
+    const long blk = __builtin_amdgcn_readlane(my_blk, i);
+    const int tok0 = __builtin_amdgcn_readlane(my_tok, i);
+    return (blk * H_kv + h) * page_bytes + (long)(tok0 & (pgsz - 1)) * kDim;
+  };
+  uint4 kc[2][2];
+  uint2 vc[2][4];
+  auto load_k = [&](int u, long base) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) kc[u][a] = *reinterpret_cast<const uint4*>(k_codes + base + k_off + 64 * a);
+  };
+  auto load_v = [&](int u, long base) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vc[u][j] = *reinterpret_cast<const uint2*>(v_codes + base + v_off + j * kDim);
+  };
+  {
+    const long b0 = unit_at(0), b1 = unit_at(1);
+    load_k(0, b0);
+    load_k(1, b1);
+    load_v(0, b0);
+    load_v(1, b1);
+  }
+  // weights enter as f16 hi + lo of p * value scale, scaled so that the largest product so far
+  // lies below 2^15 (a weight then keeps 21 bits, down to 2^-40 of the largest)
+  {
+    const int e = exponent(warp_max(my_vs)) + 1;
+    if (e > ve) {
+      const float down = pow2(ve - e);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) o[x] *= down;
+      ve = e;
+    }
+    my_vs *= pow2(-ve);
+    my_vs *= 32768.0f;
+  }
+
+  for (int j = 0; j < cnt; j += 2) {
     float z[2][4], vs[2];
     int valid[2];
 #pragma unroll
@@ -199,34 +370,42 @@ __global__ __launch_bounds__(256) void q8_attend_kernel(
       const int i = min(j + u, 63);
       const int tok0 = __builtin_amdgcn_readlane(my_tok, i);
       valid[u] = j + u < cnt && tok0 >= 0 ? min(kPage, L - tok0) : 0;
-      const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks), i));
+      const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks), i)) * head_scale;
       vs[u] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_vs), i));
       f4v st = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
-        const uint32_t w[4] = {C.k[u][a].x, C.k[u][a].y, C.k[u][a].z, C.k[u][a].w};
+        const uint32_t w[4] = {kc[u][a].x, kc[u][a].y, kc[u][a].z, kc[u][a].w};
         uint32_t b[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) widen<kCode>(w[e], b[2 * e], b[2 * e + 1]);
 #pragma unroll
         for (int mt = kTerms - 1; mt >= 0; --mt) {
-          st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf8(b[0], b[1], b[2], b[3]),
-                                                       __builtin_bit_cast(bf8v, qb[mt][2 * a]), st, 0, 0, 0);
-          st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf8(b[4], b[5], b[6], b[7]),
-                                                       __builtin_bit_cast(bf8v, qb[mt][2 * a + 1]), st, 0, 0, 0);
+          st = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(b[0], b[1], b[2], b[3]),
+                                                      __builtin_bit_cast(h8v, qb[mt][2 * a]), st, 0, 0, 0);
+          st = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_h8(b[4], b[5], b[6], b[7]),
+                                                      __builtin_bit_cast(h8v, qb[mt][2 * a + 1]), st, 0, 0, 0);
         }
       }
 #pragma unroll
-      for (int t = 0; t < 4; ++t) z[u][t] = st[t] * ks;
+      for (int n = 0; n < 4; ++n) z[u][n] = st[n] * ks;
       if (valid[u] < kPage) {  // uniform: an empty or partial unit; its codes may be anything
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-          if (4 * r4 + t >= valid[u]) {
-            z[u][t] = -INFINITY;
-            C.v[u][t] = make_uint2(0u, 0u);
+        for (int n = 0; n < 4; ++n)
+          if (4 * r4 + n >= valid[u]) {
+            z[u][n] = -INFINITY;
+            vc[u][n] = make_uint2(0u, 0u);
           }
         if (valid[u] == 0) vs[u] = 0.0f;
       }
+    }
+    const bool more = j + 2 < cnt;
+    long b0 = 0, b1 = 0;
+    if (more) {
+      b0 = unit_at(j + 2);
+      b1 = unit_at(j + 3);
+      load_k(0, b0);
+      load_k(1, b1);
     }
     const float pm = rows_max(fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])),
                                     fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3]))));
@@ -239,55 +418,52 @@ __global__ __launch_bounds__(256) void q8_attend_kernel(
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const float p0 = __builtin_amdgcn_exp2f(z[u][2 * t] - at), p1 = __builtin_amdgcn_exp2f(z[u][2 * t + 1] - at);
+      for (int n = 0; n < 2; ++n) {
+        const float p0 = __builtin_amdgcn_exp2f(z[u][2 * n] - at), p1 = __builtin_amdgcn_exp2f(z[u][2 * n + 1] - at);
         ps += p0 + p1;
-        const float w0 = p0 * vs[u], w1 = p1 * vs[u];
-        ph[2 * u + t] = pack_bf16(w0, w1);
-        pl[2 * u + t] = pack_bf16(w0 - lo_f(ph[2 * u + t]), w1 - hi_f(ph[2 * u + t]));
+        float w0 = p0 * vs[u], w1 = p1 * vs[u];
+        ph[2 * u + n] = split_h2(w0, w1);
+        pl[2 * u + n] = split_h2(w0, w1);
       }
     l = fmaf(l, sc, ps);
     if (__any(sc != 1.0f)) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] *= sc;
+      for (int n = 0; n < 8; ++n) o[n] *= sc;
     }
-    const bf8v bh = as_bf8(ph[0], ph[1], ph[2], ph[3]), bl = as_bf8(pl[0], pl[1], pl[2], pl[3]);
+    const h8v bh = as_h8(ph[0], ph[1], ph[2], ph[3]), bl = as_h8(pl[0], pl[1], pl[2], pl[3]);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {  // dims 8 m + 4 half + e
       uint32_t p[2][4], r[2][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-        widen_across<kCode>(half ? C.v[u][0].y : C.v[u][0].x, half ? C.v[u][1].y : C.v[u][1].x,
-                            half ? C.v[u][2].y : C.v[u][2].x, half ? C.v[u][3].y : C.v[u][3].x, p[u], r[u]);
+        widen_across<kCode>(half ? vc[u][0].y : vc[u][0].x, half ? vc[u][1].y : vc[u][1].x,
+                            half ? vc[u][2].y : vc[u][2].x, half ? vc[u][3].y : vc[u][3].x, p[u], r[u]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bf8v a = as_bf8(p[0][e], r[0][e], p[1][e], r[1][e]);
-        const int t = 4 * half + e;
-        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bh, o[t], 0, 0, 0);
-        o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, bl, o[t], 0, 0, 0);
+        const h8v a = as_h8(p[0][e], r[0][e], p[1][e], r[1][e]);
+        const int n = 4 * half + e;
+        o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, bh, o[n], 0, 0, 0);
+        o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, bl, o[n], 0, 0, 0);
       }
     }
-  };
-
-  if (cnt > 0) {
-    Codes A, B;
-    load_pair(A, 0);
-    for (int j = 0; j < cnt; j += 4) {
-      load_pair(B, j + 2);
-      use_pair(A, j);
-      load_pair(A, j + 4);
-      if (j + 2 < cnt) use_pair(B, j + 2);
+    if (more) {
+      load_v(0, b0);
+      load_v(1, b1);
     }
+  }
   }
 
   // ---- the block's four waves combined (m in log2 units until here); the odd row pitch of
   // sO keeps the layout's writes and the reads along d free of bank conflicts
   l = rows_sum(l);
   if (r4 == 0) { sM[wave][c16] = m; sL[wave][c16] = l; }
+  {
+    const float down = pow2(ve) * (kUnit<kCode> / 32768.0f);
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
+    for (int n = 0; n < 8; ++n)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sO[wave][32 * r4 + 8 * j + t][c16] = o[t][j];
+      for (int j = 0; j < 4; ++j) sO[wave][32 * r4 + 8 * j + n][c16] = o[n][j] * down;
+  }
   __syncthreads();
   for (int e = tid; e < G * (kDim + 2); e += 256) {
     const int g = e / (kDim + 2), c = e % (kDim + 2);
@@ -303,31 +479,108 @@ __global__ __launch_bounds__(256) void q8_attend_kernel(
         if (c < kDim) acc += sO[w][c][g] * wt;
       }
     }
-    const float mn = mx == -INFINITY ? mx : mx * kLn2;
     const long row = (long)s * H_q + h * G + g;
-    if (n_splits == 1) {
+    if (whole) {
       if (c < kDim) out[row * kDim + c] = ls > 0.0f ? acc / ls : 0.0f;
-      else if (c == kDim && out_lse) out_lse[row] = ls > 0.0f ? mn + logf(ls) : -INFINITY;
+      else if (c == kDim && out_lse) out_lse[row] = ls > 0.0f ? mx * kLn2 + logf(ls) : -INFINITY;
     } else {
-      partial[(row * n_splits + split) * (kDim + 2) + c] = c < kDim ? acc : (c == kDim ? mn : ls);
+      partial[((blockIdx.x + (long)s * H_kv + h) * G + g) * (kDim + 2) + c] = c < kDim ? acc : (c == kDim ? mx : ls);
     }
   }
+  // ---- the next list with units
+  left -= taken;
+  if (left <= 0) return;
+  at = 0;
+  if (++h == H_kv) {
+    h = 0;
+    do ++s;
+    while (order.list_units(s) == 0);
+  }
+  __syncthreads();
+  }
+}
+
+// Combines a row's partials (max in log2 units), of the blocks that hold a piece of its list:
+// one block a row, 16 partials in flight per wave, 4 or 16 waves; lane c holds dims 2 c and
+// 2 c + 1.
+constexpr int kMergeRows = 16;
+__global__ __launch_bounds__(1024) void q8_merge_kernel(int S, int H_q, int H_kv, Cut cut,
+                                                        const int32_t* __restrict__ seq_lens,
+                                                        const float* __restrict__ partial,
+                                                        float* __restrict__ out, float* __restrict__ out_lse) {
+  __shared__ float sO[16][kDim], sM[16], sL[16];
+  const long row = blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int G = H_q / H_kv, s = (int)(row / H_q), h = (int)(row % H_q) / G, g = (int)(row % G);
+  const Order order(cut, seq_lens, S, H_kv);
+  const int mine = order.list_units(s);
+  const unsigned share = share_of(cut, order.units), u0 = (unsigned)order.before(s) * H_kv + h * mine;
+  const unsigned b0 = u0 / share;
+  const int n_parts = mine > 0 ? (int)((u0 + mine - 1) / share - b0 + 1) : 0;
+  const float* p = partial + ((b0 + (long)s * H_kv + h) * G + g) * (kDim + 2);
+  const long pitch = (long)G * (kDim + 2);
+  float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+  for (int t0 = wave * kMergeRows; t0 < n_parts; t0 += waves * kMergeRows) {
+    float mt[kMergeRows], lt[kMergeRows];
+    float2 ot[kMergeRows];
+#pragma unroll
+    for (int u = 0; u < kMergeRows; ++u) {
+      const float* pt = p + min(t0 + u, n_parts - 1) * pitch;
+      ot[u] = reinterpret_cast<const float2*>(pt)[lane];
+      const float2 ml = reinterpret_cast<const float2*>(pt)[kDim / 2];
+      mt[u] = t0 + u < n_parts ? ml.x : -INFINITY;
+      lt[u] = ml.y;
+    }
+    float mm = m;
+#pragma unroll
+    for (int u = 0; u < kMergeRows; ++u) mm = fmaxf(mm, mt[u]);
+    const float at = fmaxf(mm, -3.0e38f);
+    const float sc = __builtin_amdgcn_exp2f(m - at);
+    m = mm;
+    l *= sc;
+    o0 *= sc;
+    o1 *= sc;
+#pragma unroll
+    for (int u = 0; u < kMergeRows; ++u) {
+      const float w = __builtin_amdgcn_exp2f(mt[u] - at);
+      l = fmaf(lt[u], w, l);
+      o0 = fmaf(ot[u].x, w, o0);
+      o1 = fmaf(ot[u].y, w, o1);
+    }
+  }
+  *reinterpret_cast<float2*>(&sO[wave][2 * lane]) = make_float2(o0, o1);
+  if (lane == 0) { sM[wave] = m; sL[wave] = l; }
+  __syncthreads();
+  if (threadIdx.x >= kDim) return;
+  float mx = -INFINITY;
+  for (int w = 0; w < waves; ++w) mx = fmaxf(mx, sM[w]);
+  const float at = fmaxf(mx, -3.0e38f);
+  float ls = 0.0f, acc = 0.0f;
+  for (int w = 0; w < waves; ++w) {
+    const float wt = __builtin_amdgcn_exp2f(sM[w] - at);
+    ls = fmaf(sL[w], wt, ls);
+    acc = fmaf(sO[w][threadIdx.x], wt, acc);
+  }
+  out[row * kDim + threadIdx.x] = ls > 0.0f ? acc / ls : 0.0f;
+  if (out_lse && threadIdx.x == 0) out_lse[row] = ls > 0.0f ? mx * kLn2 + logf(ls) : -INFINITY;
 }
 
 }  // namespace
 
 hipError_t launch_q8_attend(const locks_cfg_t& c, const void* q, const locks_q8_t& cache,
                             const int32_t* page_table, const int32_t* seq_lens,
-                            const int32_t* page_ids, int units_per_split, int n_splits,
-                            float* partial, float* out, float* out_lse, hipStream_t st) {
-  const dim3 grid(n_splits, c.num_kv_heads, c.num_seqs);
+                            const int32_t* page_ids, const Q8Plan& plan, float* partial, float* out,
+                            float* out_lse, hipStream_t st) {
+  const Cut cut{page_ids ? page_budget(c) << sub_page_log2(c) : 0, plan.share, plan.share ? 0 : plan.blocks};
+  const int lists = c.num_seqs * c.num_kv_heads;
+  const dim3 grid(plan.blocks ? plan.blocks : lists);
 #define LOCKS_Q8_ATTEND(QT, C)                                                                  \
-  hipLaunchKernelGGL((q8_attend_kernel<QT, C>), grid, dim3(256), 0, st, c.num_q_heads,           \
-                     c.num_kv_heads, c.max_pages_per_seq, page_budget(c), c.page_size,          \
-                     sub_page_log2(c), static_cast<const QT*>(q),                               \
+  hipLaunchKernelGGL((q8_attend_kernel<QT, C>), grid, dim3(256), 0, st, c.num_seqs,              \
+                     c.num_q_heads, c.num_kv_heads, c.max_pages_per_seq, page_budget(c),        \
+                     c.page_size, sub_page_log2(c), static_cast<const QT*>(q),                  \
                      static_cast<const uint8_t*>(cache.k), static_cast<const uint8_t*>(cache.v), \
-                     cache.k_scale, cache.v_scale, page_table, seq_lens, page_ids,              \
-                     units_per_split, n_splits, partial, out, out_lse)
+                     cache.k_scale, cache.v_scale, page_table, seq_lens, page_ids, cut, partial, \
+                     out, out_lse)
   if (c.q_dtype == LOCKS_BF16) {
     if (cache.code == LOCKS_Q8_INT8) LOCKS_Q8_ATTEND(uint16_t, LOCKS_Q8_INT8);
     else LOCKS_Q8_ATTEND(uint16_t, LOCKS_Q8_E4M3);
@@ -337,8 +590,12 @@ hipError_t launch_q8_attend(const locks_cfg_t& c, const void* q, const locks_q8_
   }
 #undef LOCKS_Q8_ATTEND
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || n_splits == 1) return e;
-  return launch_merge(c, n_splits, partial, out, out_lse, st);
+  if (e != hipSuccess || !plan.blocks) return e;
+  const int parts = plan.blocks / lists + 2;
+  hipLaunchKernelGGL(q8_merge_kernel, dim3(c.num_seqs * c.num_q_heads),
+                     dim3(parts <= 4 * kMergeRows ? 256 : 1024), 0, st, c.num_seqs, c.num_q_heads,
+                     c.num_kv_heads, cut, seq_lens, partial, out, out_lse);
+  return hipGetLastError();
 }
 
 }  // namespace locks

@@ -346,7 +346,10 @@ def _check_attend(st, code, q, out, lse, kc, vc, ks, vs, ids_of):
             assert np.all(np.abs(e[~empty] - l[~empty]) <= dz + 2.0 ** -18 * (np.abs(l[~empty]) + 1))
 
 
-LENS = [[1], [0, 1, 15, 16, 17, 31, 32, 33], [130, 0, 257, 64], [1000, 3], [5000]]
+# a block's share within one list, over many short ones, over empty ones; more than 64
+# sequences; enough lists for a block each
+LENS = [[1], [0, 1, 15, 16, 17, 31, 32, 33], [130, 0, 257, 64], [1000, 3], [5000],
+        [0, 0, 40, 0] * 17 + [0, 700, 0, 0, 9], [0, 1, 20, 5] * 70, [0], [0, 0, 0]]
 
 
 @pytest.mark.parametrize("code", CODES)
@@ -492,6 +495,20 @@ def test_q8_attend_with_table_checks():
         assert word == 3 and rows == [B.LOCKS_TABLE_E_LENGTH, B.LOCKS_TABLE_E_BLOCK]
     finally:
         B.set_table_checks(False)
+
+
+def test_q8_dense_attend_in_a_wide_table():
+    """The same sequences in a table far wider than they are: the work is cut by their lengths."""
+    st = Step([0, 0, 0], [900, 0, 333], G=4, P=16, seed=5)
+    kc, vc, ks, vs = _cache_of(st, torch.int8)
+    cache = C.Q8Cache(kc.cuda(), vc.cuda(), ks.cuda(), vs.cuda())
+    q = torch.randn(3, 8, D, generator=st.gen).bfloat16()
+    wide = torch.full((3, 40000), -1, dtype=torch.int32)
+    wide[:, :st.table.shape[1]] = st.table
+    st.cfg.max_pages_per_seq = 40000
+    out, lse = C.q8_dense_attend(st.cfg, q.cuda(), cache, wide.cuda(), st.sl, B.alloc_workspace(st.cfg))
+    torch.cuda.synchronize()
+    _check_attend(st, torch.int8, q, out, lse, kc, vc, ks, vs, lambda s, h: range(-(-st.lens[s] // 16)))
 
 
 def test_long_cache_offsets_pass_32_bits():
