@@ -76,9 +76,10 @@ Q8Plan q8_plan(const locks_cfg_t& c, long list_units, bool listed) {
   const long room = (long)(p.chk_pt_off / slot) - lists;
   list_units = (list_units + 7) / 8 * 8;  // (as the kernel counts a list)
   long blocks = lists * list_units / 8;
-  blocks = blocks < 512 ? blocks : 512;
+  const long most = lists < 512 ? 512 : lists < 1024 ? lists : 1024;
+  blocks = blocks < most ? blocks : most;
   blocks = blocks < room ? blocks : room;
-  if ((lists >= 512 && list_units <= 64) || blocks < 1) return Q8Plan{0, 0};
+  if (list_units <= (lists >= 512 ? 256 : lists >= 128 ? 64 : 32) || blocks < 1) return Q8Plan{0, 0};
   if (!listed) return Q8Plan{(int)blocks, 0};
   const long share = ((lists * list_units + blocks - 1) / blocks + 7) / 8 * 8;
   return Q8Plan{(int)((lists * list_units + share - 1) / share), (int)share};

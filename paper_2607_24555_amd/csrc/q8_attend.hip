@@ -250,6 +250,7 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   const int L = uniform(order.length(s));
   const int real = order.fixed ? order.fixed : units_of(L);
   const int taken = min(left, padded(real) - at), n = min(taken, real - at);
+  const bool complete = taken == padded(real);  // the whole list: its output is formed here
   const int per_wave = ((n + 3) / 4 + 1) & ~1;
   const int w_begin = min(wave * per_wave, n), w_end = min(w_begin + per_wave, n);
 
@@ -480,7 +481,7 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
       }
     }
     const long row = (long)s * H_q + h * G + g;
-    if (whole) {
+    if (complete) {
       if (c < kDim) out[row * kDim + c] = ls > 0.0f ? acc / ls : 0.0f;
       else if (c == kDim && out_lse) out_lse[row] = ls > 0.0f ? mx * kLn2 + logf(ls) : -INFINITY;
     } else {
@@ -500,40 +501,54 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   }
 }
 
-// Combines a row's partials (max in log2 units), of the blocks that hold a piece of its list:
-// one block a row, 16 partials in flight per wave, 4 or 16 waves; lane c holds dims 2 c and
-// 2 c + 1.
-constexpr int kMergeRows = 16;
-__global__ __launch_bounds__(1024) void q8_merge_kernel(int S, int H_q, int H_kv, Cut cut,
-                                                        const int32_t* __restrict__ seq_lens,
-                                                        const float* __restrict__ partial,
-                                                        float* __restrict__ out, float* __restrict__ out_lse) {
-  __shared__ float sO[16][kDim], sM[16], sL[16];
-  const long row = blockIdx.x;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+// Combines a row's partials (max in log2 units), of the blocks that hold a piece of its list; a
+// list within one block has its output already.  kWaves waves a row, 16 partials in flight each;
+// lane c holds dims 2 c and 2 c + 1.
+template <int kWaves>
+__global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void q8_merge_kernel(
+    int S, int H_q, int H_kv, Cut cut, const int32_t* __restrict__ seq_lens,
+    const float* __restrict__ partial, float* __restrict__ out, float* __restrict__ out_lse) {
+  __shared__ float sO[kWaves][kDim], sM[kWaves], sL[kWaves];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const long row = kWaves == 1 ? (long)blockIdx.x * 4 + wave : blockIdx.x;
+  if (kWaves == 1 && row >= (long)S * H_q) return;
   const int G = H_q / H_kv, s = (int)(row / H_q), h = (int)(row % H_q) / G, g = (int)(row % G);
   const Order order(cut, seq_lens, S, H_kv);
   const int mine = order.list_units(s);
   const unsigned share = share_of(cut, order.units), u0 = (unsigned)order.before(s) * H_kv + h * mine;
   const unsigned b0 = u0 / share;
   const int n_parts = mine > 0 ? (int)((u0 + mine - 1) / share - b0 + 1) : 0;
+  if (n_parts == 1) return;
   const float* p = partial + ((b0 + (long)s * H_kv + h) * G + g) * (kDim + 2);
   const long pitch = (long)G * (kDim + 2);
+  constexpr int kFly = 16, kStep = 4;  // partials in flight, requested four at a time
   float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (int t0 = wave * kMergeRows; t0 < n_parts; t0 += waves * kMergeRows) {
-    float mt[kMergeRows], lt[kMergeRows];
-    float2 ot[kMergeRows];
+  for (int t0 = (kWaves == 1 ? 0 : wave) * kFly; t0 < n_parts; t0 += kWaves * kFly) {
+    float mt[kFly], lt[kFly];
+    float2 ot[kFly];
 #pragma unroll
-    for (int u = 0; u < kMergeRows; ++u) {
-      const float* pt = p + min(t0 + u, n_parts - 1) * pitch;
-      ot[u] = reinterpret_cast<const float2*>(pt)[lane];
-      const float2 ml = reinterpret_cast<const float2*>(pt)[kDim / 2];
-      mt[u] = t0 + u < n_parts ? ml.x : -INFINITY;
-      lt[u] = ml.y;
+    for (int u0 = 0; u0 < kFly; u0 += kStep) {
+      const bool any = t0 + u0 < n_parts;
+#pragma unroll
+      for (int u = u0; u < u0 + kStep; ++u) {
+        ot[u] = make_float2(0.0f, 0.0f);
+        mt[u] = -INFINITY;
+        lt[u] = 0.0f;
+      }
+      if (any) {
+#pragma unroll
+        for (int u = u0; u < u0 + kStep; ++u) {
+          const float* pt = p + min(t0 + u, n_parts - 1) * pitch;
+          ot[u] = reinterpret_cast<const float2*>(pt)[lane];
+          const float2 ml = reinterpret_cast<const float2*>(pt)[kDim / 2];
+          mt[u] = t0 + u < n_parts ? ml.x : -INFINITY;
+          lt[u] = ml.y;
+        }
+      }
     }
     float mm = m;
 #pragma unroll
-    for (int u = 0; u < kMergeRows; ++u) mm = fmaxf(mm, mt[u]);
+    for (int u = 0; u < kFly; ++u) mm = fmaxf(mm, mt[u]);
     const float at = fmaxf(mm, -3.0e38f);
     const float sc = __builtin_amdgcn_exp2f(m - at);
     m = mm;
@@ -541,28 +556,37 @@ __global__ __launch_bounds__(1024) void q8_merge_kernel(int S, int H_q, int H_kv
     o0 *= sc;
     o1 *= sc;
 #pragma unroll
-    for (int u = 0; u < kMergeRows; ++u) {
+    for (int u = 0; u < kFly; ++u) {
       const float w = __builtin_amdgcn_exp2f(mt[u] - at);
       l = fmaf(lt[u], w, l);
       o0 = fmaf(ot[u].x, w, o0);
       o1 = fmaf(ot[u].y, w, o1);
     }
   }
-  *reinterpret_cast<float2*>(&sO[wave][2 * lane]) = make_float2(o0, o1);
-  if (lane == 0) { sM[wave] = m; sL[wave] = l; }
-  __syncthreads();
-  if (threadIdx.x >= kDim) return;
-  float mx = -INFINITY;
-  for (int w = 0; w < waves; ++w) mx = fmaxf(mx, sM[w]);
-  const float at = fmaxf(mx, -3.0e38f);
-  float ls = 0.0f, acc = 0.0f;
-  for (int w = 0; w < waves; ++w) {
-    const float wt = __builtin_amdgcn_exp2f(sM[w] - at);
-    ls = fmaf(sL[w], wt, ls);
-    acc = fmaf(sO[w][threadIdx.x], wt, acc);
+  if constexpr (kWaves == 1) {
+    const float inv = l > 0.0f ? 1.0f : 0.0f;
+    const float den = l > 0.0f ? l : 1.0f;
+    reinterpret_cast<float2*>(out + row * kDim)[lane] = make_float2(inv * (o0 / den), inv * (o1 / den));
+    if (out_lse && lane == 0) out_lse[row] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
+  } else {
+    *reinterpret_cast<float2*>(&sO[wave][2 * lane]) = make_float2(o0, o1);
+    if (lane == 0) { sM[wave] = m; sL[wave] = l; }
+    __syncthreads();
+    if (threadIdx.x >= kDim) return;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mx = fmaxf(mx, sM[w]);
+    const float at = fmaxf(mx, -3.0e38f);
+    float ls = 0.0f, acc = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float wt = __builtin_amdgcn_exp2f(sM[w] - at);
+      ls = fmaf(sL[w], wt, ls);
+      acc = fmaf(sO[w][threadIdx.x], wt, acc);
+    }
+    out[row * kDim + threadIdx.x] = ls > 0.0f ? acc / ls : 0.0f;
+    if (out_lse && threadIdx.x == 0) out_lse[row] = ls > 0.0f ? mx * kLn2 + logf(ls) : -INFINITY;
   }
-  out[row * kDim + threadIdx.x] = ls > 0.0f ? acc / ls : 0.0f;
-  if (out_lse && threadIdx.x == 0) out_lse[row] = ls > 0.0f ? mx * kLn2 + logf(ls) : -INFINITY;
 }
 
 }  // namespace
@@ -591,10 +615,15 @@ hipError_t launch_q8_attend(const locks_cfg_t& c, const void* q, const locks_q8_
 #undef LOCKS_Q8_ATTEND
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !plan.blocks) return e;
-  const int parts = plan.blocks / lists + 2;
-  hipLaunchKernelGGL(q8_merge_kernel, dim3(c.num_seqs * c.num_q_heads),
-                     dim3(parts <= 4 * kMergeRows ? 256 : 1024), 0, st, c.num_seqs, c.num_q_heads,
-                     c.num_kv_heads, cut, seq_lens, partial, out, out_lse);
+  const int rows = c.num_seqs * c.num_q_heads;
+#define LOCKS_Q8_MERGE(W, GRID, BLOCK)                                                          \
+  hipLaunchKernelGGL(q8_merge_kernel<W>, dim3(GRID), dim3(BLOCK), 0, st, c.num_seqs, c.num_q_heads, \
+                     c.num_kv_heads, cut, seq_lens, partial, out, out_lse)
+  // waves a row by the partials of an average list
+  if (plan.blocks <= 2 * lists) LOCKS_Q8_MERGE(1, (rows + 3) / 4, 256);
+  else if (plan.blocks <= 64 * lists) LOCKS_Q8_MERGE(4, rows, 256);
+  else LOCKS_Q8_MERGE(16, rows, 1024);
+#undef LOCKS_Q8_MERGE
   return hipGetLastError();
 }
 
