@@ -95,6 +95,14 @@ int locks_q8_append_kv(const locks_cfg_t* cfg, const locks_rows_t* rows,
                        const locks_rope_t* rope, const locks_q8_t* cache,
                        const int32_t* page_table, const int32_t* seq_lens, void* stream);
 
+/* locks_build_summaries from the keys of an 8-bit cache: the summaries that the fp32 keys
+ * code * scale have, bit for bit, so that locks_select serves a sequence whose cache is
+ * held in 8 bits (cfg->kv_dtype is not used).  Arguments and errors as there. */
+int locks_q8_build_summaries(const locks_cfg_t* cfg, const locks_q8_t* cache,
+                             const int32_t* page_table, const int32_t* seq_lens,
+                             const int32_t* build_list, int32_t n_build, void* summaries,
+                             void* stream);
+
 /* locks_dense_attend and locks_sparse_attend over an 8-bit cache (q [S][H_q][128] of
  * q_dtype, already rotated; cfg->kv_dtype is not used): same arguments, outputs, workspace
  * and table checks.  Rows past a sequence's end may hold any codes, and so may blocks that

@@ -46,6 +46,7 @@ _PC, _PR, _PO, _PQ = (ctypes.POINTER(t) for t in (_Cfg, _Rows, _Rope, _Q8))
 _SIGS = {
     "locks_rope_append_kv": (ctypes.c_int, [_PC, _PR, _PO, _P, _P, _P, _P, _P]),
     "locks_q8_append_kv": (ctypes.c_int, [_PC, _PR, _PO, _PQ, _P, _P, _P]),
+    "locks_q8_build_summaries": (ctypes.c_int, [_PC, _PQ, _P, _P, _P, _I, _P, _P]),
     "locks_q8_dense_attend": (ctypes.c_int, [_PC, _P, _PQ, _P, _P, _P, _P, _P, _SZ, _P]),
     "locks_q8_sparse_attend": (ctypes.c_int, [_PC, _P, _PQ, _P, _P, _P, _P, _P, _P, _SZ, _P]),
 }
@@ -256,6 +257,22 @@ def q8_append_kv(cfg: Config, k_new, v_new, cache: Q8Cache, page_table, seq_lens
                                 cu_tokens, q, q_out)
     call(stream)
     return call.outputs
+
+
+def q8_build_summaries(cfg: Config, cache: Q8Cache, page_table, seq_lens, summaries,
+                       build_list: Optional[torch.Tensor] = None, stream=None):
+    """locks.build_summaries from the keys of an 8-bit cache -- locks_q8_build_summaries."""
+    B._check_tables(cfg, page_table, seq_lens)
+    B._check_summaries(cfg, summaries)
+    B._check_list("build_list", build_list)
+    if build_list is not None and build_list.shape[0] == 0:
+        return                      # an empty list names no page (NULL would mean all)
+    store = _q8(cfg, cache)
+    _current_device(cache.k, cache.k_scale, page_table, seq_lens, summaries, build_list)
+    c = cfg.c()
+    B._check(lib().locks_q8_build_summaries(
+        ctypes.byref(c), ctypes.byref(store), B._ptr(page_table), B._ptr(seq_lens), B._ptr(build_list),
+        0 if build_list is None else int(build_list.shape[0]), B._ptr(summaries), B._stream(stream)))
 
 
 def _prepare_attend(cfg, q, cache, page_table, seq_lens, page_ids, listed, ws, out, out_lse):

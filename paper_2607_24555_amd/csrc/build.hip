@@ -8,7 +8,7 @@
 // exactly symmetric; its eigenpairs come from the register-resident tridiagonal
 // solver of tridiag16.h (one 16-lane DPP row per item).  Everything is fp32.
 #include "build_common.h"
-#include "locks_internal.h"
+#include "cache_internal.h"
 #include "tridiag16.h"
 
 namespace locks {
@@ -57,9 +57,11 @@ __device__ __forceinline__ int group16_min_int(int v) {
 // kBuildLast builds only those pages and scores them for the step's query (Eq. 1
 // on the decoded summary), writing their page scores and one extra (max, sum)
 // partial per query head of their sequence.
-template <typename KT, bool kFactors, int kMode>
+// ST: the cache's elements, KT or codes (with k_scale [num_blocks][H_kv]; KT is then float).
+template <typename KT, typename ST, bool kFactors, int kMode>
 __global__ __launch_bounds__(64) void build_kernel(
-    int S, int H_kv, int max_pages, int r, const KT* __restrict__ k_cache,
+    int S, int H_kv, int max_pages, int r, const ST* __restrict__ k_cache,
+    const float* __restrict__ k_scale,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ build_list, int n_items, int all_pages,
     uint8_t* __restrict__ summaries, float* __restrict__ mu_out, float* __restrict__ basis_out,
@@ -130,15 +132,17 @@ __global__ __launch_bounds__(64) void build_kernel(
   if (kMode == kBuildLast) __builtin_amdgcn_s_setprio(3);
   const long blk = active ? (long)page_table[(long)s * max_pages + j] : 0;
 
+  const float key_scale = sizeof(ST) == 1 && active ? k_scale[blk * H_kv + h] : 1.0f;
+
   // ---- load row li of the page (16-byte loads), track its squared norm
   float energy = 0.0f;
   {
     constexpr int kVec = 16 / sizeof(KT);  // elements per 16-byte load
-    const uint4* src = reinterpret_cast<const uint4*>(k_cache + ((blk * H_kv + h) * kPage + li) * kDim);
+    const ST* src = k_cache + ((blk * H_kv + h) * kPage + li) * kDim;
     uint4* dst = reinterpret_cast<uint4*>(&sK[grp][li][0]);
     uint4 w[kDim / kVec];
 #pragma unroll
-    for (int u = 0; u < kDim / kVec; ++u) w[u] = active ? src[u] : make_uint4(0, 0, 0, 0);
+    for (int u = 0; u < kDim / kVec; ++u) w[u] = active ? load_keys<KT>(src, u * kVec, key_scale) : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int u = 0; u < kDim / kVec; ++u) dst[u] = w[u];
 #pragma unroll
@@ -235,12 +239,12 @@ __global__ __launch_bounds__(64) void build_kernel(
   constexpr int kSliceVec = 8 * (int)sizeof(KT) / 16;  // 16-byte loads per 8-element slice
   uint4 ks[kPage][kSliceVec];
   {
-    const uint4* kpage = reinterpret_cast<const uint4*>(k_cache + (blk * H_kv + h) * kPage * kDim);
+    const ST* kpage = k_cache + (blk * H_kv + h) * kPage * kDim;
 #pragma unroll
     for (int i = 0; i < kPage; ++i)
 #pragma unroll
       for (int u = 0; u < kSliceVec; ++u)
-        ks[i][u] = active ? kpage[(i * kDim + 8 * li) / (16 / (int)sizeof(KT)) + u]
+        ks[i][u] = active ? load_keys<KT>(kpage, i * kDim + 8 * li + u * (16 / (int)sizeof(KT)), key_scale)
                           : make_uint4(0, 0, 0, 0);
   }
   float cabs = 0.0f;  // running max |C[li][:]| for the row scale
@@ -460,7 +464,8 @@ __global__ __launch_bounds__(64) void build_kernel(
 hipError_t launch_build(const locks_cfg_t& c, const void* k_cache, const int32_t* page_table,
                         const int32_t* seq_lens, const int32_t* build_list, int32_t n_items,
                         bool all_pages, void* summaries, float* mu, float* basis, float* coef,
-                        float* sigma2, hipStream_t st, BuildMode mode, const BuildStep* step) {
+                        float* sigma2, hipStream_t st, BuildMode mode, const BuildStep* step,
+                        const float* code_scale, int code) {
   const long items = all_pages ? (long)c.num_seqs * c.max_pages_per_seq * c.num_kv_heads
                                : (long)n_items * c.num_kv_heads;
   if (items == 0) return hipSuccess;
@@ -470,23 +475,29 @@ hipError_t launch_build(const locks_cfg_t& c, const void* k_cache, const int32_t
   if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(64);
   const BuildStep bs = step ? *step : BuildStep{};
-#define LOCKS_BUILD(KT, F, M)                                                                  \
-  hipLaunchKernelGGL((build_kernel<KT, F, M>), grid, block, 0, st, c.num_seqs, c.num_kv_heads,  \
-                     c.max_pages_per_seq, c.rank, static_cast<const KT*>(k_cache), page_table,  \
-                     seq_lens, build_list, n_items, (int)all_pages, (uint8_t*)summaries, mu,    \
-                     basis, coef, sigma2, bs, c.basis)
+#define LOCKS_BUILD_S(KT, ST, F, M)                                                            \
+  hipLaunchKernelGGL((build_kernel<KT, ST, F, M>), grid, block, 0, st, c.num_seqs, c.num_kv_heads, \
+                     c.max_pages_per_seq, c.rank, static_cast<const ST*>(k_cache), code_scale,  \
+                     page_table, seq_lens, build_list, n_items, (int)all_pages,                 \
+                     (uint8_t*)summaries, mu, basis, coef, sigma2, bs, c.basis)
+#define LOCKS_BUILD(KT, F, M) LOCKS_BUILD_S(KT, KT, F, M)
 #define LOCKS_BUILD_T(KT)                                     \
   if (factors) LOCKS_BUILD(KT, true, kBuildAll);              \
   else if (mode == kBuildInner) LOCKS_BUILD(KT, false, kBuildInner); \
   else if (mode == kBuildLast) LOCKS_BUILD(KT, false, kBuildLast);   \
   else LOCKS_BUILD(KT, false, kBuildAll)
-  if (c.kv_dtype == LOCKS_BF16) {
+  if (code_scale) {  // 8-bit keys: summaries only, and not within a step
+    if (mode != kBuildAll || factors) return hipErrorInvalidValue;
+    if (code == LOCKS_Q8_INT8) LOCKS_BUILD_S(float, Int8Codes, false, kBuildAll);
+    else LOCKS_BUILD_S(float, E4m3Codes, false, kBuildAll);
+  } else if (c.kv_dtype == LOCKS_BF16) {
     LOCKS_BUILD_T(uint16_t);
   } else {
     LOCKS_BUILD_T(float);
   }
 #undef LOCKS_BUILD_T
 #undef LOCKS_BUILD
+#undef LOCKS_BUILD_S
   return hipGetLastError();
 }
 

@@ -29,7 +29,7 @@
 // tokens x 8 heads at r = 8: 756 us at 32 tokens and 1,548 at 64, where Gram rows in LDS, eigenvectors solved through LDS by r
 // lanes and one reduction at a time took 1,470 and 3,900.
 #include "build_common.h"
-#include "locks_internal.h"
+#include "cache_internal.h"
 
 namespace locks {
 namespace {
@@ -205,10 +205,11 @@ struct PageItem {
   long row;  // blk * H_kv + h
 };
 
-template <typename KT, int B, bool kFactors, int kMaxR>
+// ST: the cache's elements, KT or codes (with k_scale [num_blocks][H_kv]; KT is then float).
+template <typename KT, typename ST, int B, bool kFactors, int kMaxR>
 __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(B == 32 && kMaxR <= 8 ? 4 : (kMaxR <= 8 ? 3 : 2)))) void build_page_kernel(
-    int S, int H_kv, int max_pages, int r, const KT* __restrict__ k_cache,
-    const int32_t* __restrict__ page_table, const int32_t* __restrict__ seq_lens,
+    int S, int H_kv, int max_pages, int r, const ST* __restrict__ k_cache,
+    const float* __restrict__ k_scale, const int32_t* __restrict__ page_table, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ build_list, int n_items, int all_pages,
     uint8_t* __restrict__ summaries, float* __restrict__ mu_out, float* __restrict__ basis_out,
     float* __restrict__ coef_out, float* __restrict__ sigma2_out) {
@@ -264,9 +265,17 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(B == 32 && k
   auto kpage = [&](int t) { return k_cache + item[t].row * (long)B * kDim; };
   // 16 bytes of item t at token tok0 (uniform) and lane offset `off` bytes (zeros for an
   // inactive item)
+  float key_scale[kI];
+#pragma unroll
+  for (int t = 0; t < kI; ++t) key_scale[t] = sizeof(ST) == 1 && item[t].active ? k_scale[item[t].row] : 1.0f;
   auto key16 = [&](int t, int tok0, uint32_t off) {
-    const char* p = reinterpret_cast<const char*>(kpage(t) + tok0 * kDim);
-    return item[t].active ? *reinterpret_cast<const uint4*>(p + off) : make_uint4(0, 0, 0, 0);
+    if constexpr (sizeof(ST) == 1) {
+      return item[t].active ? load_keys<KT>(kpage(t) + tok0 * kDim, off / sizeof(KT), key_scale[t])
+                            : make_uint4(0, 0, 0, 0);
+    } else {
+      const char* p = reinterpret_cast<const char*>(kpage(t) + tok0 * kDim);
+      return item[t].active ? *reinterpret_cast<const uint4*>(p + off) : make_uint4(0, 0, 0, 0);
+    }
   };
   constexpr uint32_t kEl = sizeof(KT);
   const uint32_t off_row = (uint32_t)(q4 * kDim + 8 * l16) * kEl;      // token q4, dims 8 l16 ..
@@ -808,7 +817,8 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(B == 32 && k
 hipError_t launch_build_page(const locks_cfg_t& c, const void* k_cache, const int32_t* page_table,
                              const int32_t* seq_lens, const int32_t* build_list, int32_t n_items,
                              bool all_pages, void* summaries, float* mu, float* basis,
-                             float* coef, float* sigma2, hipStream_t st) {
+                             float* coef, float* sigma2, hipStream_t st, const float* code_scale,
+                             int code) {
   const long items = all_pages ? (long)c.num_seqs * c.max_pages_per_seq * c.num_kv_heads
                                : (long)n_items * c.num_kv_heads;
   if (items == 0) return hipSuccess;
@@ -820,24 +830,38 @@ hipError_t launch_build_page(const locks_cfg_t& c, const void* k_cache, const in
   const dim3 grid((unsigned)blocks), block(64);
   // ranks up to 8 take the instance whose rank-sized arrays (LDS and registers)
   // hold 8 vectors: its smaller LDS fits more waves per compute unit
-#define LOCKS_BUILD_PAGE_R(KT, BP, F, MR)                                                      \
-  hipLaunchKernelGGL((build_page_kernel<KT, BP, F, MR>), grid, block, 0, st, c.num_seqs,        \
-                     c.num_kv_heads, c.max_pages_per_seq, c.rank, static_cast<const KT*>(k_cache), \
-                     page_table, seq_lens, build_list, n_items, (int)all_pages,                \
+#define LOCKS_BUILD_PAGE_R(KT, ST, BP, F, MR)                                                  \
+  hipLaunchKernelGGL((build_page_kernel<KT, ST, BP, F, MR>), grid, block, 0, st, c.num_seqs,    \
+                     c.num_kv_heads, c.max_pages_per_seq, c.rank, static_cast<const ST*>(k_cache), \
+                     code_scale, page_table, seq_lens, build_list, n_items, (int)all_pages,     \
                      (uint8_t*)summaries, mu, basis, coef, sigma2)
-#define LOCKS_BUILD_PAGE(KT, BP, F)                                                            \
-  if (c.rank <= 8) LOCKS_BUILD_PAGE_R(KT, BP, F, 8); else LOCKS_BUILD_PAGE_R(KT, BP, F, kMaxRank)
+#define LOCKS_BUILD_PAGE(KT, ST, BP, F)                                                        \
+  if (c.rank <= 8) LOCKS_BUILD_PAGE_R(KT, ST, BP, F, 8); else LOCKS_BUILD_PAGE_R(KT, ST, BP, F, kMaxRank)
 #define LOCKS_BUILD_PAGE_B(KT)                                                                 \
   switch (c.page_size) {                                                                       \
-    case 32: if (factors) LOCKS_BUILD_PAGE(KT, 32, true); else LOCKS_BUILD_PAGE(KT, 32, false); break; \
-    case 64: if (factors) LOCKS_BUILD_PAGE(KT, 64, true); else LOCKS_BUILD_PAGE(KT, 64, false); break; \
+    case 32: if (factors) LOCKS_BUILD_PAGE(KT, KT, 32, true); else LOCKS_BUILD_PAGE(KT, KT, 32, false); break; \
+    case 64: if (factors) LOCKS_BUILD_PAGE(KT, KT, 64, true); else LOCKS_BUILD_PAGE(KT, KT, 64, false); break; \
     default: return hipErrorInvalidValue;                                                      \
   }
-  if (c.kv_dtype == LOCKS_BF16) {
+#define LOCKS_BUILD_PAGE_C(ST)                                                                 \
+  switch (c.page_size) {                                                                       \
+    case 32: LOCKS_BUILD_PAGE(float, ST, 32, false); break;                                    \
+    case 64: LOCKS_BUILD_PAGE(float, ST, 64, false); break;                                    \
+    default: return hipErrorInvalidValue;                                                      \
+  }
+  if (code_scale) {  // 8-bit keys: summaries only
+    if (factors) return hipErrorInvalidValue;
+    if (code == LOCKS_Q8_INT8) {
+      LOCKS_BUILD_PAGE_C(Int8Codes);
+    } else {
+      LOCKS_BUILD_PAGE_C(E4m3Codes);
+    }
+  } else if (c.kv_dtype == LOCKS_BF16) {
     LOCKS_BUILD_PAGE_B(uint16_t);
   } else {
     LOCKS_BUILD_PAGE_B(float);
   }
+#undef LOCKS_BUILD_PAGE_C
 #undef LOCKS_BUILD_PAGE_B
 #undef LOCKS_BUILD_PAGE
 #undef LOCKS_BUILD_PAGE_R

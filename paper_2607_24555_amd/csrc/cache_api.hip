@@ -136,6 +136,27 @@ int locks_q8_append_kv(const locks_cfg_t* cfg, const locks_rows_t* rows,
                                      static_cast<hipStream_t>(stream)));
 }
 
+int locks_q8_build_summaries(const locks_cfg_t* cfg, const locks_q8_t* cache,
+                             const int32_t* page_table, const int32_t* seq_lens,
+                             const int32_t* build_list, int32_t n_build, void* summaries,
+                             void* stream) {
+  int rc = validate(cfg);
+  if (rc) return rc;
+  if ((rc = q8_valid(cache))) return rc;
+  if (!page_table || !seq_lens || !summaries || n_build < 0 || (!build_list && n_build > 0))
+    return LOCKS_E_INVAL;
+  if (cfg->num_seqs == 0) return LOCKS_OK;
+  const bool all = build_list == nullptr;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (cfg->page_size != kPage)
+    return hip_status(launch_build_page(*cfg, cache->k, page_table, seq_lens, build_list, n_build, all,
+                                        summaries, nullptr, nullptr, nullptr, nullptr, st,
+                                        cache->k_scale, cache->code));
+  return hip_status(launch_build(*cfg, cache->k, page_table, seq_lens, build_list, n_build, all, summaries,
+                                 nullptr, nullptr, nullptr, nullptr, st, kBuildAll, nullptr,
+                                 cache->k_scale, cache->code));
+}
+
 int locks_q8_dense_attend(const locks_cfg_t* cfg, const void* q, const locks_q8_t* cache,
                           const int32_t* page_table, const int32_t* seq_lens, float* out,
                           float* out_lse, void* ws, size_t ws_bytes, void* stream) {

@@ -157,6 +157,7 @@ int checked_tables(const locks_cfg_t& c, void* ws, const int32_t*& page_table,
 // domain, valid for the sequences with sl_scan < seq_lens), so it may run beside
 // the scan and needs nothing from kBuildInner.
 enum BuildMode { kBuildAll = 0, kBuildInner = 1, kBuildLast = 2 };
+// (code_scale: k_cache holds 8-bit codes of kind `code`, one scale per block and KV head.)
 struct BuildStep {
   int32_t* sl_scan;
   float2* part_x;
@@ -170,14 +171,16 @@ hipError_t launch_build(const locks_cfg_t& c, const void* k_cache, const int32_t
                         const int32_t* seq_lens, const int32_t* build_list, int32_t n_items,
                         bool all_pages, void* summaries, float* mu, float* basis, float* coef,
                         float* sigma2, hipStream_t st, BuildMode mode = kBuildAll,
-                        const BuildStep* step = nullptr);
+                        const BuildStep* step = nullptr, const float* code_scale = nullptr,
+                        int code = 0);
 
 // The same build for pages of B = 16, 32 or 64 tokens (tridiagonal eigensolver);
 // every listed or complete page, or the unquantised factors when mu != nullptr.
 hipError_t launch_build_page(const locks_cfg_t& c, const void* k_cache, const int32_t* page_table,
                              const int32_t* seq_lens, const int32_t* build_list, int32_t n_items,
                              bool all_pages, void* summaries, float* mu, float* basis,
-                             float* coef, float* sigma2, hipStream_t st);
+                             float* coef, float* sigma2, hipStream_t st,
+                             const float* code_scale = nullptr, int code = 0);
 
 hipError_t launch_scan(const locks_cfg_t& c, const void* q, const void* summaries,
                        const int32_t* page_table, const int32_t* seq_lens, float* s_hat,

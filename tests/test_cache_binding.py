@@ -133,6 +133,15 @@ def test_bad_stores_are_rejected(lib, bad, code):
                                       FAKE, need, None) == code
 
 
+def test_build_arguments(lib):
+    c, s = cfg().c(), q8()
+    build = lambda c=c, s=s, pt=FAKE, sl=FAKE, lst=None, n=0, out=FAKE: lib.locks_q8_build_summaries(
+        ctypes.byref(c), _ref(s), pt, sl, lst, n, out, None)
+    assert build(s=None) == build(pt=None) == build(sl=None) == build(out=None) == -1
+    assert build(n=-1) == build(n=3) == -1 and build(s=q8(code=9)) == -2 and build(s=q8(k=0x1001)) == -1
+    assert build(c=cfg(rank=0).c()) == -1 and build(c=cfg(num_seqs=0).c()) == 0
+
+
 def test_attention_arguments(lib):
     c, s = cfg().c(), q8()
     need = lib.locks_workspace_bytes(ctypes.byref(c))

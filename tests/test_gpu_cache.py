@@ -475,6 +475,78 @@ def test_serving_loop(code):
     assert torch.equal(eager.k_scale, c.k_scale) and torch.equal(eager.v_scale, c.v_scale)
 
 
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("P,rank", [(16, 8), (16, 2), (16, 15), (32, 8), (32, 12), (64, 8), (64, 9)])
+def test_q8_build_equals_the_build_of_the_decoded_keys(code, P, rank):
+    """Summaries from codes are those of the fp32 keys code * scale, bit for bit, for every
+    page and for a list; what names no complete page is skipped."""
+    lens = [P * 5 + 3, P - 1, P * 2, 0]
+    st = Step([0] * 4, lens, P=P, kv="fp32", q="fp32", seed=rank)
+    st.cfg.rank = rank
+    print(f"[q8 build] {code} P={P} r={rank}", flush=True)
+    kc, vc, ks, vs = _cache_of(st, code, seed=rank)
+    cache = C.Q8Cache(kc.cuda(), vc.cuda(), ks.cuda(), vs.cuda())
+    decoded = (kc.float() * ks[..., None, None]).cuda()
+    for lst in (None, torch.tensor([[0, 4], [2, 0], [0, 5], [1, 0], [7, 0], [0, -1]], dtype=torch.int32).cuda()):
+        want, got = B.alloc_summaries(st.cfg), B.alloc_summaries(st.cfg)
+        want.fill_(7)
+        got.fill_(7)
+        B.build_summaries(st.cfg, decoded, st.pt, st.sl, want, lst)
+        C.q8_build_summaries(st.cfg, cache, st.pt, st.sl, got, lst)
+        torch.cuda.synchronize()
+        assert torch.equal(want, got)
+        assert int((got != 7).any(-1).any(-1).sum()) == (7 if lst is None else 2)
+    C.q8_build_summaries(st.cfg, cache, st.pt, st.sl, got, torch.zeros(0, 2, dtype=torch.int32).cuda())
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("P", [16, 64])
+def test_locks_step_over_an_8_bit_cache(code, P):
+    """Prompts appended, their summaries built from the codes, then tokens: append, build of
+    the pages that fill, selection, attention over the selected pages -- against the same
+    step over an fp32 cache of the decoded values."""
+    H, G, lens0, T = 2, 4, [40 * P + 3, 25 * P - 2], 5
+    S = 2
+    mp = 48
+    cfg = B.Config(S, G * H, H, 8, 8 * P, mp, S * mp, page_size=P)
+    wide = B.Config(S, G * H, H, 8, 8 * P, mp, S * mp, B.LOCKS_FP32, B.LOCKS_BF16, page_size=P)
+    g = torch.Generator().manual_seed(5 + P)
+    pt = torch.randperm(S * mp, generator=g).int().reshape(S, mp).cuda()
+    rope = C.Rope(C.rope_table(mp * P, 128))
+    mk = lambda n: [torch.randn(n, h, D, generator=g).bfloat16().cuda() for h in (G * H, H, H)]
+    q, k, v = mk(sum(lens0))
+    cache = C.alloc_q8_cache(cfg, code)
+    summ = B.alloc_summaries(cfg)
+    sl = torch.tensor(lens0, dtype=torch.int32).cuda()
+    cu = torch.tensor([0, lens0[0], sum(lens0)], dtype=torch.int32).cuda()
+    C.q8_append_kv(cfg, k, v, cache, pt, sl, rope, cu_tokens=cu)
+    C.q8_build_summaries(cfg, cache, pt, sl, summ)
+    ws, wws = B.alloc_workspace(cfg), B.alloc_workspace(wide)
+    for t in range(T):
+        q, k, v = mk(S)
+        lens = [L + t + 1 for L in lens0]
+        sl = torch.tensor(lens, dtype=torch.int32).cuda()
+        full = [[s, L // P - 1] for s, L in enumerate(lens) if L % P == 0]
+        qr = C.q8_append_kv(cfg, k, v, cache, pt, sl, rope, q=q)
+        if full:
+            C.q8_build_summaries(cfg, cache, pt, sl, summ, torch.tensor(full, dtype=torch.int32).cuda())
+        ids, _ = B.select(cfg, qr, summ, pt, sl, ws)
+        out, lse = C.q8_sparse_attend(cfg, qr, cache, pt, sl, ids, ws)
+        kd, vd = (c.float() * x[..., None, None] for c, x in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)))
+        ws2 = B.alloc_summaries(wide)
+        B.build_summaries(wide, kd, pt, sl, ws2)
+        ids2, _, out2, lse2 = B.decode_step(wide, qr, kd, vd, pt, sl, ws2, wws)
+        torch.cuda.synchronize()
+        assert torch.equal(ids, ids2)
+        st = Step([0] * S, lens, H=H, G=G, P=P, seed=1)
+        st.table, st.cfg = pt.cpu(), cfg
+        _check_attend(st, code, qr.cpu(), out, lse, *[x.cpu() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale)],
+                      lambda s, h: [int(j) for j in ids[s, h] if j >= 0])
+        # both within the bound of the 64-bit result, so within twice of each other
+        assert float((out - out2).abs().max()) < 1e-3 and float((lse - lse2).abs().max()) < 1e-3
+    assert lens[1] // P > lens0[1] // P   # a page filled on the way
+
+
 def test_q8_attend_with_table_checks():
     """A bad entry and a bad length are clamped and reported, as in the other attentions."""
     st = Step([0, 0], [100, 60], seed=9)
