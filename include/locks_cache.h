@@ -42,7 +42,7 @@ typedef struct locks_rope {
 /* The rows of a step's new tokens.  With cu_tokens (device [num_seqs + 1], ascending from
  * 0) sequence s's new tokens are rows [cu_tokens[s], cu_tokens[s + 1]) and are its last
  * ones, seq_lens[s] counting them; a sequence may have none, and rows from
- * cu_tokens[num_seqs] on are padding: they are not read, and q_out's are left as they
+ * cu_tokens[num_seqs] (at most n_tokens) on are padding: they are not read, and q_out's are left as they
  * were.  Without it, row s is the newest token of sequence s and n_tokens must be num_seqs
  * (a sequence of length 0 has none).
  * Row t, head h of a tensor starts stride * t + 128 * h elements from its pointer. */
@@ -106,7 +106,9 @@ int locks_q8_build_summaries(const locks_cfg_t* cfg, const locks_q8_t* cache,
 /* locks_dense_attend and locks_sparse_attend over an 8-bit cache (q [S][H_q][128] of
  * q_dtype, already rotated; cfg->kv_dtype is not used): same arguments, outputs, workspace
  * and table checks.  Rows past a sequence's end may hold any codes, and so may blocks that
- * its table does not reach.  Returns LOCKS_E_INVAL for a null or misaligned pointer. */
+ * its table does not reach.  A NaN in a query or in a scale of a live page gives NaN in its
+ * outputs.  Returns LOCKS_E_INVAL for a null or misaligned pointer, LOCKS_E_UNSUPPORTED for
+ * tables of 2^31 sixteen-token units or more over all sequences and KV heads. */
 int locks_q8_dense_attend(const locks_cfg_t* cfg, const void* q, const locks_q8_t* cache,
                           const int32_t* page_table, const int32_t* seq_lens, float* out,
                           float* out_lse, void* ws, size_t ws_bytes, void* stream);

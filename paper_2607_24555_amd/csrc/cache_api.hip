@@ -29,10 +29,11 @@ int append_args(const locks_cfg_t* c, const locks_rows_t* rows, const locks_rope
   if (!rows || !page_table || !seq_lens || rows->n_tokens < 0) return LOCKS_E_INVAL;
   if (!rows->cu_tokens && rows->n_tokens != c->num_seqs) return LOCKS_E_INVAL;
   const int kb = c->kv_dtype == LOCKS_BF16 ? 2 : 4, qb = c->q_dtype == LOCKS_BF16 ? 2 : 4;
-  if (!rows_valid(rows->k, rows->k_stride, c->num_kv_heads, kb) ||
-      !rows_valid(rows->v, rows->v_stride, c->num_kv_heads, kb))
+  const bool any = rows->n_tokens > 0;  // (no rows: their pointers are not looked at)
+  if (any && (!rows_valid(rows->k, rows->k_stride, c->num_kv_heads, kb) ||
+              !rows_valid(rows->v, rows->v_stride, c->num_kv_heads, kb)))
     return LOCKS_E_INVAL;
-  if (rows->q && (!rows_valid(rows->q, rows->q_stride, c->num_q_heads, qb) ||
+  if (any && rows->q && (!rows_valid(rows->q, rows->q_stride, c->num_q_heads, qb) ||
                   !rows_valid(rows->q_out, rows->q_out_stride, c->num_q_heads, qb)))
     return LOCKS_E_INVAL;
   if (rows->q && rows->q == rows->q_out && rows->q_stride != rows->q_out_stride) return LOCKS_E_INVAL;
@@ -91,7 +92,8 @@ int q8_attend(const locks_cfg_t* cfg, const void* q, const locks_q8_t* cache,
   int rc = validate(cfg);
   if (rc) return rc;
   if ((rc = q8_valid(cache))) return rc;
-  if (!q || !aligned16(q) || !page_table || !seq_lens || !out || (listed && !page_ids))
+  if (!q || !aligned16(q) || !page_table || !seq_lens || !out || !aligned16(out) ||
+      (listed && !page_ids))
     return LOCKS_E_INVAL;
   if ((rc = check_ws(cfg, ws, ws_bytes))) return rc;
   if (cfg->num_seqs == 0) return LOCKS_OK;

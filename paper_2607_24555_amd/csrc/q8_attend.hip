@@ -471,19 +471,18 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
     float mx = -INFINITY;
 #pragma unroll
     for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sM[w][g]);
+    const float origin = fmaxf(mx, -3.0e38f);
     float acc = 0.0f, ls = 0.0f;
-    if (mx > -INFINITY) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float wt = __builtin_amdgcn_exp2f(sM[w][g] - mx);
-        ls += sL[w][g] * wt;
-        if (c < kDim) acc += sO[w][c][g] * wt;
-      }
+    for (int w = 0; w < 4; ++w) {
+      const float wt = __builtin_amdgcn_exp2f(sM[w][g] - origin);
+      ls += sL[w][g] * wt;
+      if (c < kDim) acc += sO[w][c][g] * wt;
     }
     const long row = (long)s * H_q + h * G + g;
     if (complete) {
-      if (c < kDim) out[row * kDim + c] = ls > 0.0f ? acc / ls : 0.0f;
-      else if (c == kDim && out_lse) out_lse[row] = ls > 0.0f ? mx * kLn2 + logf(ls) : -INFINITY;
+      if (c < kDim) out[row * kDim + c] = ls == 0.0f ? 0.0f : acc / ls;
+      else if (c == kDim && out_lse) out_lse[row] = ls == 0.0f ? -INFINITY : mx * kLn2 + logf(ls);
     } else {
       partial[((blockIdx.x + (long)s * H_kv + h) * G + g) * (kDim + 2) + c] = c < kDim ? acc : (c == kDim ? mx : ls);
     }
@@ -564,10 +563,9 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void q8_merge_kern
     }
   }
   if constexpr (kWaves == 1) {
-    const float inv = l > 0.0f ? 1.0f : 0.0f;
-    const float den = l > 0.0f ? l : 1.0f;
-    reinterpret_cast<float2*>(out + row * kDim)[lane] = make_float2(inv * (o0 / den), inv * (o1 / den));
-    if (out_lse && lane == 0) out_lse[row] = l > 0.0f ? m * kLn2 + logf(l) : -INFINITY;
+    reinterpret_cast<float2*>(out + row * kDim)[lane] =
+        l == 0.0f ? make_float2(0.0f, 0.0f) : make_float2(o0 / l, o1 / l);
+    if (out_lse && lane == 0) out_lse[row] = l == 0.0f ? -INFINITY : m * kLn2 + logf(l);
   } else {
     *reinterpret_cast<float2*>(&sO[wave][2 * lane]) = make_float2(o0, o1);
     if (lane == 0) { sM[wave] = m; sL[wave] = l; }
@@ -584,8 +582,8 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void q8_merge_kern
       ls = fmaf(sL[w], wt, ls);
       acc = fmaf(sO[w][threadIdx.x], wt, acc);
     }
-    out[row * kDim + threadIdx.x] = ls > 0.0f ? acc / ls : 0.0f;
-    if (out_lse && threadIdx.x == 0) out_lse[row] = ls > 0.0f ? mx * kLn2 + logf(ls) : -INFINITY;
+    out[row * kDim + threadIdx.x] = ls == 0.0f ? 0.0f : acc / ls;
+    if (out_lse && threadIdx.x == 0) out_lse[row] = ls == 0.0f ? -INFINITY : mx * kLn2 + logf(ls);
   }
 }
 

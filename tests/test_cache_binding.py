@@ -113,6 +113,7 @@ def test_null_arguments_and_empty_batches(lib):
     assert _appends(lib, cfg(kv_dtype=5).c(), rows(), rope()) == (-2, -2)
     # nothing to append: no launch
     assert _appends(lib, c, rows(n_tokens=0), rope()) == (0, 0)
+    assert _appends(lib, c, rows(n_tokens=0, k=None, v=None, q=None, q_out=None), None) == (0, 0)
     assert _appends(lib, cfg(num_seqs=0).c(), rows(n_tokens=0, cu_tokens=None), None) == (0, 0)
     # fp32 rows need strides of 16 bytes too
     f = cfg(kv_dtype=B.LOCKS_FP32, q_dtype=B.LOCKS_FP32).c()
@@ -148,6 +149,10 @@ def test_attention_arguments(lib):
     dense = lambda c=c, q=FAKE, s=s, pt=FAKE, sl=FAKE, out=FAKE, ws=FAKE, n=need: lib.locks_q8_dense_attend(
         ctypes.byref(c), q, None if s is None else ctypes.byref(s), pt, sl, out, None, ws, n, None)
     assert dense(q=None) == dense(q=ODD) == dense(s=None) == dense(pt=None) == dense(sl=None) == dense(out=None) == -1
+    assert dense(out=ODD) == -1
+    # 16 x 8 x 2^24 x 4 units
+    wide = cfg(num_seqs=16, num_q_heads=8, num_kv_heads=8, max_pages_per_seq=1 << 24, page_size=64).c()
+    assert dense(c=wide, n=1 << 62) == -2
     assert dense(ws=None) == dense(n=need - 1) == dense(ws=ctypes.c_void_p(0x1010)) == -3
     assert dense(c=cfg(page_size=48).c()) == -2 and dense(c=cfg(budget_tokens=1).c()) == -1
     assert lib.locks_q8_sparse_attend(ctypes.byref(c), FAKE, ctypes.byref(s), FAKE, FAKE, None, FAKE, None,

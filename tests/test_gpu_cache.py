@@ -583,6 +583,40 @@ def test_q8_dense_attend_in_a_wide_table():
     _check_attend(st, torch.int8, q, out, lse, kc, vc, ks, vs, lambda s, h: range(-(-st.lens[s] // 16)))
 
 
+def test_q8_attend_nan_and_one_output():
+    """A NaN query stays NaN and touches no other head or sequence; the LSE is optional."""
+    st = Step([0, 0], [300, 40], G=4, seed=6)
+    kc, vc, ks, vs = _cache_of(st, torch.int8)
+    cache = C.Q8Cache(kc.cuda(), vc.cuda(), ks.cuda(), vs.cuda())
+    q = torch.randn(2, 8, D, generator=st.gen).bfloat16().cuda()
+    ws = B.alloc_workspace(st.cfg)
+    want, lse = C.q8_dense_attend(st.cfg, q, cache, st.pt, st.sl, ws)
+    q[0, 2, 17] = float("nan")
+    out = torch.zeros(2, 8, D).cuda()
+    got, none = C.q8_dense_attend(st.cfg, q, cache, st.pt, st.sl, ws, out=out, out_lse=None)
+    nan = torch.zeros(2, 8, dtype=torch.bool).cuda()
+    nan[0, 2] = True
+    assert none is None and got is out
+    assert bool(torch.isnan(got[nan]).all()) and torch.equal(got[~nan], want[~nan])
+
+
+def test_empty_appends():
+    """No new rows at all, and a batch in which no sequence has any: nothing changes."""
+    st = Step([5, 20], [0, 0], seed=2)
+    cache = C.alloc_q8_cache(st.cfg)
+    cache.k_scale += 1
+    kc = torch.ones(st.cfg.num_blocks, st.H, 16, D, dtype=torch.bfloat16).cuda()
+    rope = C.Rope(C.rope_table(64, 128))
+    for n in (0, 3):                                  # (three rows of padding)
+        k = torch.ones(n, st.H, D, dtype=torch.bfloat16).cuda()
+        q = torch.ones(n, st.G * st.H, D, dtype=torch.bfloat16).cuda()
+        q_out = torch.full_like(q, 3)
+        C.q8_append_kv(st.cfg, k, k, cache, st.pt, st.sl, rope, cu_tokens=st.cu_dev, q=q, q_out=q_out)
+        C.rope_append_kv(st.cfg, k, k, kc, kc, st.pt, st.sl, rope, cu_tokens=st.cu_dev, q=q, q_out=q_out)
+        assert bool((q_out == 3).all())
+    assert bool((cache.k_scale == 1).all()) and not bool(cache.k.any()) and bool((kc == 1).all())
+
+
 def test_long_cache_offsets_pass_32_bits():
     """Blocks whose codes lie past 4 GiB, and a cache past 2^31 elements: the last blocks are
     appended to and attended."""
