@@ -7,6 +7,8 @@
 // as rotated fp32 values, so that a page's largest magnitude, its scale and its codes come
 // from one read; the next head's rows are in flight meanwhile.  Only where the scale of a page
 // with earlier rows grows are those rows read and rounded again.
+#include <type_traits>
+
 #include "rope.h"
 
 namespace locks {
@@ -28,28 +30,59 @@ __device__ __forceinline__ float page_scale(float amax) {
   }
 }
 
-// Codes of eight scaled elements.
+// Codes of eight scaled elements, none of them NaN.
 template <int kCode>
 __device__ __forceinline__ uint2 codes_of(const float (&x)[8]) {
+  constexpr float kMost = kCode == LOCKS_Q8_INT8 ? 127.0f : 448.0f;
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = __builtin_amdgcn_fmed3f(x[e], -kMost, kMost);
   if constexpr (kCode == LOCKS_Q8_INT8) {
+    // 1.5 2^23 + y rounds y to an integer, ties to even, in the low bits
     uint32_t b[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float c = fminf(fmaxf(rintf(x[e]), -127.0f), 127.0f);
-      b[e] = (uint32_t)(int)(x[e] == x[e] ? c : 0.0f) & 0xffu;
-    }
-    return make_uint2(b[0] | (b[1] << 8) | (b[2] << 16) | (b[3] << 24),
-                      b[4] | (b[5] << 8) | (b[6] << 16) | (b[7] << 24));
-  } else {
-    float y[8];
+    for (int e = 0; e < 8; ++e) b[e] = __float_as_uint(y[e] + 12582912.0f);
+    uint32_t w[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = x[e] == x[e] ? fminf(fmaxf(x[e], -448.0f), 448.0f) : x[e];
+    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(b[2 * e + 1], b[2 * e], 0x0c0c0400u);
+    return make_uint2(__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u));
+  } else {
     int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
     int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
     return make_uint2((uint32_t)lo, (uint32_t)hi);
   }
+}
+
+// The same where there may be NaN among them: 0 (int8) or e4m3's NaN.
+template <int kCode>
+__device__ __forceinline__ uint2 codes_of_any(const float (&x)[8]) {
+  float y[8];
+  uint32_t keep[2] = {0u, 0u};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    y[e] = x[e] == x[e] ? x[e] : 0.0f;
+    keep[e >> 2] |= x[e] == x[e] ? 0xffu << (8 * (e & 3)) : 0u;
+  }
+  const uint2 c = codes_of<kCode>(y);
+  const uint32_t nan = kCode == LOCKS_Q8_INT8 ? 0u : 0x7f7f7f7fu;
+  return make_uint2((c.x & keep[0]) | (nan & ~keep[0]), (c.y & keep[1]) | (nan & ~keep[1]));
+}
+
+// Max over the wave.
+__device__ __forceinline__ float wave_max(float v) {
+  auto dpp = [](float x, auto ctl) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctl)::value, 0xf, 0xf, true));
+  };
+  v = fmaxf(v, dpp(v, std::integral_constant<int, 0xB1>{}));   // quad xor 1, xor 2
+  v = fmaxf(v, dpp(v, std::integral_constant<int, 0x4E>{}));
+  v = fmaxf(v, dpp(v, std::integral_constant<int, 0x141>{}));  // half-row and row mirrors
+  v = fmaxf(v, dpp(v, std::integral_constant<int, 0x140>{}));
+  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
 
 template <int kCode>
@@ -78,67 +111,62 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
     RowArgs a, RopeArgs rope, uint8_t* __restrict__ k_codes, uint8_t* __restrict__ v_codes,
     float* __restrict__ k_scale, float* __restrict__ v_scale, const int32_t* __restrict__ page_table,
     const int32_t* __restrict__ seq_lens, int S, int H_q, int H_kv, int max_pages, int num_blocks,
-    long n_units, unsigned page_blocks, int heads, int head_parts, int q_parts, int q_rows) {
+    unsigned n_units, unsigned page_blocks, int heads, unsigned head_parts, unsigned q_parts, int q_rows) {
   constexpr int P = 16 * kWaves;
   __shared__ float s_max[2][4];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, tg = lane >> 4;
   const Lane ln = lane_of(rope, lane & 15);
-  const int32_t* cu = a.cu;
 
   if (blockIdx.x >= page_blocks) {  // query rows
-    const long id = (long)(blockIdx.x - page_blocks) * 4 + wave;
-    const long row_l = id / q_parts;
-    if (row_l >= a.n_tokens) return;
-    const int row = (int)row_l, part = (int)(id % q_parts);
+    const unsigned id = (blockIdx.x - page_blocks) * 4 + wave;
+    const int row = (int)(id / q_parts), part = (int)(id % q_parts);
+    if (row >= a.n_tokens) return;
     const int r0 = part * q_rows, r1 = min(r0 + q_rows, H_q);
     const QT* q = static_cast<const QT*>(a.q) + row * a.q_stride;
     auto src = [&](int r) { return q + r * kDim; };
     Mover<QT, kRows> mq;
     mq.begin(ln, r0 + tg, r1, src);
-    int s = row;
-    if (a.cu) {
-      s = wave_search(S, row, [cu](int i) { return cu[i]; });
-      if (s < 0) return;
-    }
-    const NewTokens t = new_tokens(a, seq_lens, s);
+    const NewTokens t = tokens_of_row(a, seq_lens, S, row);
+    if (t.s < 0) return;
     const int tok = t.tok0 + (row - t.row0);
     if (row - t.row0 >= t.n || tok < 0 || tok / P >= max_pages) return;
-    const int blk = page_table[(long)s * max_pages + tok / P];
+    const int blk = page_table[(long)t.s * max_pages + tok / P];
+    Positions pos;
+    if (!positions_of(rope, row, tok, pos)) return;
     Angles A;
-    if (!load_angles(rope, ln, row, tok, A) || blk < 0 || blk >= num_blocks) return;
+    load_angles(rope, ln, pos, A);
+    if (blk < 0 || blk >= num_blocks) return;
     QT* out = static_cast<QT*>(a.q_out) + row * a.q_out_stride;
     mq.move(rope, ln, A, tg, r0, r1, H_q, src, [&](int r) { return out + r * kDim; });
     return;
   }
 
   // ---- which (sequence, page, tensor, KV heads) this wave belongs to
-  const long unit = (long)blockIdx.x * (4 / kWaves) + wave / kWaves;
+  const unsigned unit = blockIdx.x * (4 / kWaves) + wave / kWaves;
   bool live = unit < n_units;
   const int h0 = (int)(unit % head_parts) * heads, h1 = min(h0 + heads, H_kv);
   const int kv = (int)(unit / head_parts % 2);
-  const long slot = unit / (2 * (long)head_parts);
+  const int slot = (int)(unit / (2 * head_parts));
   // pages by slots: sequence s's begin at slot cu[s] / P + 2 s (it touches at most
   // n / P + 2 pages); without cu one slot a sequence
-  int s = (int)slot, ahead = 0;
-  if (live && a.cu) {
-    s = wave_search(S, slot, [cu](int i) { return (long)(cu[i] / P) + 2 * i; });
-    live = s >= 0;
-    if (live) ahead = (int)(slot - (a.cu[s] / P + 2 * (long)s));
+  NewTokens t{-1, 0, 0, 0};
+  int ahead = 0;
+  if (live) {
+    if (a.cu) {
+      t = find_tokens(a, seq_lens, S, slot, [](int c, int i) { return (long)(c / P) + 2 * i; });
+      ahead = (int)(slot - (t.row0 / P + 2 * (long)t.s));
+    } else {
+      t = one_token(seq_lens, slot);
+    }
   }
-  NewTokens t{0, 0, 0};
-  if (live) t = new_tokens(a, seq_lens, s);
   const int first = max(t.tok0, 0), L = t.tok0 + t.n;  // tokens [first, L) are new
   const int j = first / P + ahead;
-  live = live && t.n > 0 && j < max_pages && (long)j * P < L;
-  int blk = -1;
-  if (live) {
-    blk = page_table[(long)s * max_pages + j];
-    live = blk >= 0 && blk < num_blocks;
-  }
+  live = live && t.s >= 0 && t.n > 0 && j < max_pages && (long)j * P < L;
   // (the same for the block's waves of a page, so a page's waves leave together; pages of
   // several waves meet at the barriers below)
   if (kWaves == 1 && !live) return;
+  const int blk = live ? page_table[(long)t.s * max_pages + j] : 0;  // looked at where it is used
 
   // ---- this wave's 16 tokens: where they are in the input, and their angles
   const int i0 = 16 * (wave % kWaves) + tg;  // token row of the page, + 4 u
@@ -159,26 +187,43 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int T = j * P + i0 + 4 * u;
-    if (on[u]) on[u] = load_angles(rope, ln, t.row0 + (T - t.tok0), T, A[u]);  // a position outside: left out
+    if (!on[u]) continue;
+    Positions pos;
+    on[u] = positions_of(rope, t.row0 + (T - t.tok0), T, pos);  // a position outside: left out
+    if (kv == 0 && on[u]) load_angles(rope, ln, pos, A[u]);
   }
+  live = live && blk >= 0 && blk < num_blocks;
   for (int h = h0; h < h0 + heads; ++h) {  // (as many rounds for every wave)
     float x[4][8];
     float big = -1.0f;  // stays so where no row is placed
+    bool nan = false;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       w[u].to(x[u]);
       if (kv == 0) rotate(rope, ln, A[u], x[u]);
       if (on[u]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float m = fabsf(x[u][e]);
-          big = fmaxf(big, m <= 3.402823466e38f ? m : 0.0f);
+        for (int e = 0; e < 8; e += 2) {
+          big = fmaxf(fmaxf(big, fabsf(x[u][e])), fabsf(x[u][e + 1]));
+          nan |= __builtin_isunordered(x[u][e], x[u][e + 1]);
         }
       }
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) w[u].load(src + from[u] + min(h + 1, h1 - 1) * kDim, ln.a, ln.b);
-    big = warp_max(big);
+    big = wave_max(big);
+    const bool odd = __any(nan) || big > 3.402823466e38f;  // (rare) elements that are not finite
+    if (odd) {
+      big = -1.0f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float m = fabsf(x[u][e]);
+          if (on[u]) big = fmaxf(big, m <= 3.402823466e38f ? m : 0.0f);
+        }
+      big = wave_max(big);
+    }
     const long at = (long)(live ? blk : 0) * H_kv + min(h, h1 - 1);
     float* scale_at = (kv ? v_scale : k_scale) + at;
     const float before = live && earlier > 0 ? *scale_at : 0.0f;
@@ -196,24 +241,23 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
     const bool grew = earlier > 0 && scale > before;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const int i = i0 + 4 * u;
-      uint32_t* to_a = reinterpret_cast<uint32_t*>(codes + i * kDim + ln.a);
-      uint32_t* to_b = reinterpret_cast<uint32_t*>(codes + i * kDim + ln.b);
+      uint8_t* to = codes + (i0 + 4 * u) * kDim;
       float y[8];
-      bool put = on[u];
-      if (on[u]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = x[u][e] * inv;
-      } else if (grew && i < earlier) {
-        values_of<kCode>(make_uint2(*to_a, *to_b), y);
+      for (int e = 0; e < 8; ++e) y[e] = x[u][e] * inv;
+      uint2 c = codes_of<kCode>(y);
+      if (odd) c = codes_of_any<kCode>(y);
+      bool put = on[u];
+      if (grew && i0 + 4 * u < earlier) {  // an earlier row under the larger scale
+        values_of<kCode>(make_uint2(*reinterpret_cast<uint32_t*>(to + ln.a), *reinterpret_cast<uint32_t*>(to + ln.b)), y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = y[e] * before * inv;
+        c = codes_of_any<kCode>(y);
         put = true;
       }
       if (put) {
-        const uint2 c = codes_of<kCode>(y);
-        *to_a = c.x;
-        *to_b = c.y;
+        *reinterpret_cast<uint32_t*>(to + ln.a) = c.x;
+        *reinterpret_cast<uint32_t*>(to + ln.b) = c.y;
       }
     }
     if (wave % kWaves == 0 && lane == 0) *scale_at = scale;
@@ -236,13 +280,13 @@ hipError_t launch_typed(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& 
   while (per > 4 && (long)a.n_tokens * ((hq + per - 1) / per) < 4096) per /= 2;
   const int q_parts = (hq + per - 1) / per;
   const long q_blocks = ((long)a.n_tokens * q_parts + 3) / 4;
-  if (page_blocks + q_blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
+  if (4 * (page_blocks + q_blocks) > 0x7fffffffL) return hipErrorInvalidConfiguration;
 #define LOCKS_Q8_APPEND(W)                                                                        \
   hipLaunchKernelGGL((q8_append_kernel<QT, KT, kCode, W>), dim3((unsigned)(page_blocks + q_blocks)), \
                      dim3(256), 0, st, a, r, static_cast<uint8_t*>(cache.k),                       \
                      static_cast<uint8_t*>(cache.v), cache.k_scale, cache.v_scale, page_table,    \
                      seq_lens, c.num_seqs, hq, c.num_kv_heads, c.max_pages_per_seq, c.num_blocks, \
-                     units, (unsigned)page_blocks, heads, head_parts, q_parts, per)
+                     (unsigned)units, (unsigned)page_blocks, heads, head_parts, q_parts, per)
   if (waves == 1) LOCKS_Q8_APPEND(1);
   else if (waves == 2) LOCKS_Q8_APPEND(2);
   else LOCKS_Q8_APPEND(4);

@@ -95,14 +95,44 @@ __device__ __forceinline__ int wave_search(int S, long at, Key key) {
 // The new tokens of sequence s: rows [row0, row0 + n) of the input are tokens
 // [tok0, tok0 + n) of the sequence.
 struct NewTokens {
-  int row0, n, tok0;
+  int s, row0, n, tok0;
 };
-__device__ __forceinline__ NewTokens new_tokens(const RowArgs& a, const int32_t* seq_lens, int s) {
-  const int L = seq_lens[s];
-  if (!a.cu) return NewTokens{s, L > 0 ? 1 : 0, L - 1};
-  const int r0 = a.cu[s], r1 = min(a.cu[s + 1], a.n_tokens);
+// ... of the sequence with the largest key(cu[s], s) <= at (s = -1: none).  Up to 64 sequences
+// every lane holds one's entries, so that nothing is loaded once the sequence is known.
+template <typename Key>
+__device__ __forceinline__ NewTokens find_tokens(const RowArgs& a, const int32_t* seq_lens, int S, long at, Key key) {
+  const int32_t* cu = a.cu;
+  int s, r0, r1, L;
+  if (S <= 64) {
+    const int lane = threadIdx.x & 63, i = min(lane, S - 1);
+    const int c = cu[i], len = seq_lens[i];
+    const int end = cu[S];
+    s = __popcll(__ballot(lane < S && key(c, i) <= at)) - 1;
+    if (s < 0) return NewTokens{-1, 0, 0, 0};
+    r0 = __builtin_amdgcn_readlane(c, s);
+    r1 = s + 1 < S ? __builtin_amdgcn_readlane(c, min(s + 1, 63)) : end;
+    L = __builtin_amdgcn_readlane(len, s);
+  } else {
+    s = wave_search(S, at, [cu, key](int i) { return key(cu[i], i); });
+    if (s < 0) return NewTokens{-1, 0, 0, 0};
+    s = __builtin_amdgcn_readfirstlane(s);
+    r0 = cu[s];
+    r1 = cu[s + 1];
+    L = seq_lens[s];
+  }
+  r1 = min(r1, a.n_tokens);
   const int n = r0 >= 0 && r1 > r0 ? r1 - r0 : 0;
-  return NewTokens{r0, n, L - n};
+  return NewTokens{s, r0, n, L - n};
+}
+// One new token a sequence, row s.
+__device__ __forceinline__ NewTokens one_token(const int32_t* seq_lens, int s) {
+  const int L = seq_lens[s];
+  return NewTokens{s, s, L > 0 ? 1 : 0, L - 1};
+}
+// ... of the sequence that input row `row` belongs to.
+__device__ __forceinline__ NewTokens tokens_of_row(const RowArgs& a, const int32_t* seq_lens, int S, int row) {
+  if (!a.cu) return one_token(seq_lens, row);
+  return find_tokens(a, seq_lens, S, row, [](int c, int) { return (long)c; });
 }
 
 // Which elements of a row lane cg of 16 holds: both of each of its four pairs, so that a
@@ -122,19 +152,28 @@ __device__ __forceinline__ Lane lane_of(const RopeArgs& r, int cg) {
 struct Angles {
   float c[4], s[4];
 };
-// The lane's angles for the token of a row.  Returns false where a position lies outside the
-// table (the same for all lanes of the token).
-__device__ __forceinline__ bool load_angles(const RopeArgs& r, const Lane& ln, int row, int tok, Angles& A) {
+// The table rows of a token's axes, or false where one lies outside the table (the same for
+// all lanes of the token).
+struct Positions {
+  int p0, p1, p2;
+};
+__device__ __forceinline__ bool positions_of(const RopeArgs& r, int row, int tok, Positions& p) {
+  p = Positions{tok, tok, tok};
   if (r.half == 0) return true;
-  int p0 = tok, p1 = tok, p2 = tok;
   if (r.positions) {
-    p0 = p1 = p2 = r.positions[row];
-    if (r.n_axes > 1) p1 = p2 = r.positions[(long)r.n_tokens + row];
-    if (r.n_axes > 2) p2 = r.positions[2 * (long)r.n_tokens + row];
+    p.p0 = p.p1 = p.p2 = r.positions[row];
+    if (r.n_axes > 1) p.p1 = p.p2 = r.positions[(long)r.n_tokens + row];
+    if (r.n_axes > 2) p.p2 = r.positions[2 * (long)r.n_tokens + row];
   }
-  if ((unsigned)p0 >= (unsigned)r.n_pos || (unsigned)p1 >= (unsigned)r.n_pos || (unsigned)p2 >= (unsigned)r.n_pos)
-    return false;
-  if (!ln.turn) return true;
+  const unsigned n = r.n_pos;
+  return (unsigned)p.p0 < n && (unsigned)p.p1 < n && (unsigned)p.p2 < n;
+}
+// The lane's angles at a token's positions.  (Values, not members, are selected: a select of
+// members is one of addresses, which puts the struct into LDS and makes the kernel read its
+// dispatch packet from host memory: 64 tokens 3.1 us without, 13 with.)
+__device__ __forceinline__ void load_angles(const RopeArgs& r, const Lane& ln, const Positions& p, Angles& A) {
+  if (!ln.turn) return;
+  const int p0 = p.p0, p1 = p.p1, p2 = p.p2;
   if (r.n_axes == 1) {
     const float* t = r.table + (long)p0 * (2 * r.half) + ln.pair0;  // 16-byte aligned
     const float4 c = *reinterpret_cast<const float4*>(t), s = *reinterpret_cast<const float4*>(t + r.half);
@@ -144,36 +183,33 @@ __device__ __forceinline__ bool load_angles(const RopeArgs& r, const Lane& ln, i
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int i = ln.pair0 + e;
-      const float* t = r.table + (long)(i < r.axis1 ? p0 : (i < r.axis2 ? p1 : p2)) * (2 * r.half) + i;
+      const int at = i < r.axis1 ? p0 : (i < r.axis2 ? p1 : p2);
+      const float* t = r.table + (long)at * (2 * r.half) + i;
       A.c[e] = t[0];
       A.s[e] = t[r.half];
     }
   }
-  return true;
 }
 
-// The lane's eight elements, rotated in place.  (Elements are picked by value: with the two
-// orders as branches the compiler merges them into one that indexes x from memory.)
+// The lane's eight elements, rotated in place.
 __device__ __forceinline__ void rotate(const RopeArgs& r, const Lane& ln, const Angles& A, float (&x)[8]) {
   if (!ln.turn) return;
-  const bool il = r.interleaved;
-  const float x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3], x4 = x[4], x5 = x[5], x6 = x[6], x7 = x[7];
-  const float a[4] = {x0, il ? x2 : x1, il ? x4 : x2, il ? x6 : x3};
-  const float b[4] = {il ? x1 : x4, il ? x3 : x5, il ? x5 : x6, x7};
-  float u[4], w[4];
+  if (r.interleaved) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    u[e] = a[e] * A.c[e] - b[e] * A.s[e];
-    w[e] = b[e] * A.c[e] + a[e] * A.s[e];
+    for (int e = 0; e < 4; ++e) {
+      const float a = x[2 * e], b = x[2 * e + 1];
+      x[2 * e] = a * A.c[e] - b * A.s[e];
+      x[2 * e + 1] = b * A.c[e] + a * A.s[e];
+    }
+    asm volatile("");  // (else the two orders are merged into one that indexes x in memory)
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float a = x[e], b = x[4 + e];
+      x[e] = a * A.c[e] - b * A.s[e];
+      x[4 + e] = b * A.c[e] + a * A.s[e];
+    }
   }
-  x[0] = u[0];
-  x[1] = il ? w[0] : u[1];
-  x[2] = il ? u[1] : u[2];
-  x[3] = il ? w[1] : u[3];
-  x[4] = il ? u[2] : w[0];
-  x[5] = il ? w[2] : w[1];
-  x[6] = il ? u[3] : w[2];
-  x[7] = w[3];
 }
 
 // Rows [r0, r1) of one token, four at a time with 16 lanes each, kRows in flight per lane:
