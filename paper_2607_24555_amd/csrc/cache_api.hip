@@ -64,26 +64,29 @@ int append_args(const locks_cfg_t* c, const locks_rows_t* rows, const locks_rope
   return LOCKS_OK;
 }
 
-// Equal shares for 512 blocks (two of the three that a compute unit holds: 8 ragged sequences,
-// 272K tokens, 111 us; 256 blocks 120, 768 114, 1,024 122), of at least 8 units (a pair per
-// wave), fewer where the workspace holds fewer partials (they may take it up to the checked
-// tables).  A block per list, without partials, where there are 512 lists of at most 64 units
-// (64 sequences x 8 KV heads, 16 units: 12 us against 20 with a merge), or the workspace holds
-// none.
+// Equal shares for 512 blocks, two of the three that a compute unit holds (8 ragged sequences,
+// 272K tokens, 8 heads: 111 us; 256 blocks 120, 768 114, 1,024 122), but for 256 where a share
+// is 8 to 64 units and there are no more lists than that (65K tokens of one head 13.8 us
+// against 16.6, of eight 29.8 against 28.8); as many blocks as lists between 512 and 1,024 of
+// them; fewer where the workspace holds fewer partials (they may take it up to the checked
+// tables).
+// A block per list, without partials, up to the widths where that was no slower: 32 units with
+// few lists (64 lists: 9.3 us against 10.4, at 64 units 14.9 against 12.8), 64 from 128 lists
+// (15.1 against 16.0, at 128 units 23.9 against 20.3) and 256 from 512 (103 against 112).
 Q8Plan q8_plan(const locks_cfg_t& c, long list_units, bool listed) {
   const WsPlan p = plan_workspace(c);
   const long lists = (long)c.num_seqs * c.num_kv_heads;
   const size_t slot = (size_t)(c.num_q_heads / c.num_kv_heads) * (kDim + 2) * sizeof(float);
   const long room = (long)(p.chk_pt_off / slot) - lists;
   list_units = (list_units + 7) / 8 * 8;  // (as the kernel counts a list)
-  long blocks = lists * list_units / 8;
-  const long most = lists < 512 ? 512 : lists < 1024 ? lists : 1024;
-  blocks = blocks < most ? blocks : most;
+  const long all = lists * list_units, most = lists < 512 ? 512 : lists < 1024 ? lists : 1024;
+  long blocks = all / 8 < most ? all / 8 : most;
   blocks = blocks < room ? blocks : room;
-  if (list_units <= (lists >= 512 ? 256 : lists >= 128 ? 64 : 32) || blocks < 1) return Q8Plan{0, 0};
-  if (!listed) return Q8Plan{(int)blocks, 0};
-  const long share = ((lists * list_units + blocks - 1) / blocks + 7) / 8 * 8;
-  return Q8Plan{(int)((lists * list_units + share - 1) / share), (int)share};
+  if (list_units <= (lists >= 512 ? 256 : lists >= 128 ? 64 : 32) || blocks < 1)
+    return Q8Plan{(int)lists, 0, 0};
+  const long few = lists <= 256 && blocks > 256 ? 256 : blocks;
+  const long share = q8_share((unsigned)all, (unsigned)blocks, (unsigned)few);
+  return Q8Plan{(int)(listed ? (all + share - 1) / share : blocks), (int)blocks, (int)few};
 }
 
 int q8_attend(const locks_cfg_t* cfg, const void* q, const locks_q8_t* cache,

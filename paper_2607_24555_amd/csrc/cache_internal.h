@@ -27,13 +27,22 @@ hipError_t launch_rope_append(const locks_cfg_t& c, const RowArgs& a, const Rope
 hipError_t launch_q8_append(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& r,
                             const locks_q8_t& cache, const int32_t* page_table,
                             const int32_t* seq_lens, hipStream_t st);
-// How an attention over an 8-bit cache is split over blocks: `blocks` equal shares of all
-// lists' units, each of `share` units or (0) as many as the lengths come to; blocks = 0: one
-// block a list.
+// How an attention over an 8-bit cache is split: the lists' units, in order, in equal shares
+// for at most `blocks` blocks, of which `grid` are launched (fewer where the units are known);
+// blocks = 0: one block a list.
 struct Q8Plan {
-  int blocks, share;
+  int grid, blocks, few;
 };
-// page_ids == nullptr: every page.  partial: blocks + lists slots of [G][130] floats.
+// Units of a share, a multiple of 8 (a pair per wave): 8 while that takes 5/8 of `blocks` at
+// most, then what `few` blocks need (few <= blocks), but from 64 units on no more than `blocks`
+// need.  ceil(units / share) <= blocks.
+__host__ __device__ inline unsigned q8_share(unsigned units, unsigned blocks, unsigned few) {
+  if (units <= 5 * blocks) return 8;
+  const unsigned least = (units + blocks - 1) / blocks, cap = least < 64 ? 64 : least;
+  const unsigned share = (units + few - 1) / few;
+  return ((share < cap ? share : cap) + 7) / 8 * 8;  // (>= 8: units > 0 here)
+}
+// page_ids == nullptr: every page.  partial: plan.blocks + lists slots of [G][130] floats.
 hipError_t launch_q8_attend(const locks_cfg_t& c, const void* q, const locks_q8_t& cache,
                             const int32_t* page_table, const int32_t* seq_lens,
                             const int32_t* page_ids, const Q8Plan& plan, float* partial, float* out,

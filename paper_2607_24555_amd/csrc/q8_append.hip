@@ -270,9 +270,10 @@ hipError_t launch_typed(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& 
                         const int32_t* seq_lens, hipStream_t st) {
   const int hq = a.q ? c.num_q_heads : 0, P = c.page_size, waves = P / 16;
   const long slots = a.cu ? a.n_tokens / P + 2L * c.num_seqs : c.num_seqs;
-  // heads per unit: up to 4 while 4,096 waves remain
+  // heads per unit: up to 4 while 4,096 waves with tokens remain
+  const long busy = a.cu ? a.n_tokens / 16 + c.num_seqs : c.num_seqs;
   int heads = c.num_kv_heads < 4 ? c.num_kv_heads : 4;
-  while (heads > 1 && slots * 2 * waves * ((c.num_kv_heads + heads - 1) / heads) < 4096) --heads;
+  while (heads > 1 && busy * 2 * ((c.num_kv_heads + heads - 1) / heads) < 4096) --heads;
   const int head_parts = (c.num_kv_heads + heads - 1) / heads;
   const long units = slots * 2 * head_parts;
   const long page_blocks = (units + 4 / waves - 1) / (4 / waves);

@@ -110,18 +110,13 @@ __device__ __forceinline__ float rows_sum(float v) {
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
 __device__ __forceinline__ int exponent(float v) { return (int)(__float_as_uint(v) >> 23 & 255u) - 127; }
 
-// How the lists' units are cut: shares of `share` units (a multiple of 8; 0: a block per list,
-// no partials), or, where `blocks` is set, total / blocks rounded up to such a multiple.
+// How the lists' units are cut (see Q8Plan).
 struct Cut {
   int fixed_units;  // units of every list (a table's), or 0: the sequence's own
-  int share, blocks;
+  int blocks, few;
 };
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ int units_of(int len) { return max((len + kPage - 1) / kPage, 0); }
-// A list counts as a multiple of 8 units, so that at the smallest share no block holds a piece
-// of two lists, one after the other (8 heads over 4,099 tokens: 13.0 -> 11.2 us).
-__device__ __forceinline__ int padded(int units) { return (units + 7) & ~7; }
-
 __device__ __forceinline__ int wave_scan(int v) {  // inclusive sums over the wave
   v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
   v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
@@ -131,34 +126,30 @@ __device__ __forceinline__ int wave_scan(int v) {  // inclusive sums over the wa
   v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
   return v;
 }
-__device__ __forceinline__ unsigned share_of(const Cut& cut, unsigned units) {
-  if (!cut.blocks) return cut.share;
-  const unsigned per = (units + cut.blocks - 1) / cut.blocks;
-  return per < 8 ? 8 : (per + 7) / 8 * 8;
-}
 // The sequences' lengths and places in the lists' order (units of all lists fit 31 bits, which
 // the host checks).  Up to 64 sequences are one load and one scan, kept in a register.
+// A list counts as a multiple of 8 units, so that at the smallest share no block holds a piece
+// of two lists, one after the other (8 heads over 4,099 tokens: 13.0 -> 11.2 us).
 struct Order {
   const int32_t* seq_lens;
   int S, H_kv, fixed;
   int len, end;    // S <= 64, lane i: sequence i's length; units of one KV head up to and with it
   unsigned units;  // of all sequences and KV heads
+  unsigned share;
   __device__ __forceinline__ Order(const Cut& cut, const int32_t* sl, int S_, int H)
       : seq_lens(sl), S(S_), H_kv(H), fixed(cut.fixed_units) {
     const int lane = threadIdx.x & 63;
     len = S <= 64 && lane < S ? seq_lens[lane] : 0;
     end = 0;
-    if (fixed) {
-      units = (unsigned)S * padded(fixed) * H_kv;
-      return;
-    }
-    int sum = 0;
-    for (int s0 = 0; s0 < S; s0 += 64) {
+    int sum = fixed ? S * padded(fixed) : 0;
+    for (int s0 = 0; !fixed && s0 < S; s0 += 64) {
       end = scan_from(s0, sum);
       sum = __builtin_amdgcn_readlane(end, 63);
     }
     units = (unsigned)sum * H_kv;
+    share = cut.blocks ? q8_share(units, cut.blocks, cut.few) : 0;
   }
+  static __device__ __forceinline__ int padded(int n) { return (n + 7) & ~7; }
   __device__ __forceinline__ int scan_from(int s0, int sum) const {
     const int i = s0 + (threadIdx.x & 63);
     return sum + wave_scan(padded(units_of(S <= 64 ? len : (i < S ? seq_lens[i] : 0))));
@@ -230,13 +221,13 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   // ---- the block's share of the units (wave-uniform, on the scalar unit)
   const Order order(cut, seq_lens, S, H_kv);
   int s, h, at = 0, left;  // list (s, h), first unit within it, units of the share still to do
-  const bool whole = cut.share == 0 && cut.blocks == 0;
+  const bool whole = cut.blocks == 0;
   if (whole) {
     s = blockIdx.x / H_kv;
     h = blockIdx.x % H_kv;
     left = order.list_units(s);
   } else {
-    const unsigned share = share_of(cut, order.units), u0 = blockIdx.x * share;
+    const unsigned share = order.share, u0 = blockIdx.x * share;
     if (u0 >= order.units) return;
     left = uniform((int)min(share, order.units - u0));
     int before;
@@ -249,8 +240,8 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   while (true) {  // one piece: units [at, at + n) of list (s, h)
   const int L = uniform(order.length(s));
   const int real = order.fixed ? order.fixed : units_of(L);
-  const int taken = min(left, padded(real) - at), n = min(taken, real - at);
-  const bool complete = taken == padded(real);  // the whole list: its output is formed here
+  const int taken = min(left, order.padded(real) - at), n = min(taken, real - at);
+  const bool complete = taken == order.padded(real);  // the whole list: its output is formed here
   const int per_wave = ((n + 3) / 4 + 1) & ~1;
   const int w_begin = min(wave * per_wave, n), w_end = min(w_begin + per_wave, n);
 
@@ -514,7 +505,7 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void q8_merge_kern
   const int G = H_q / H_kv, s = (int)(row / H_q), h = (int)(row % H_q) / G, g = (int)(row % G);
   const Order order(cut, seq_lens, S, H_kv);
   const int mine = order.list_units(s);
-  const unsigned share = share_of(cut, order.units), u0 = (unsigned)order.before(s) * H_kv + h * mine;
+  const unsigned share = order.share, u0 = (unsigned)order.before(s) * H_kv + h * mine;
   const unsigned b0 = u0 / share;
   const int n_parts = mine > 0 ? (int)((u0 + mine - 1) / share - b0 + 1) : 0;
   if (n_parts == 1) return;
@@ -593,9 +584,9 @@ hipError_t launch_q8_attend(const locks_cfg_t& c, const void* q, const locks_q8_
                             const int32_t* page_table, const int32_t* seq_lens,
                             const int32_t* page_ids, const Q8Plan& plan, float* partial, float* out,
                             float* out_lse, hipStream_t st) {
-  const Cut cut{page_ids ? page_budget(c) << sub_page_log2(c) : 0, plan.share, plan.share ? 0 : plan.blocks};
+  const Cut cut{page_ids ? page_budget(c) << sub_page_log2(c) : 0, plan.blocks, plan.few};
   const int lists = c.num_seqs * c.num_kv_heads;
-  const dim3 grid(plan.blocks ? plan.blocks : lists);
+  const dim3 grid(plan.grid);
 #define LOCKS_Q8_ATTEND(QT, C)                                                                  \
   hipLaunchKernelGGL((q8_attend_kernel<QT, C>), grid, dim3(256), 0, st, c.num_seqs,              \
                      c.num_q_heads, c.num_kv_heads, c.max_pages_per_seq, page_budget(c),        \
@@ -618,8 +609,8 @@ hipError_t launch_q8_attend(const locks_cfg_t& c, const void* q, const locks_q8_
   hipLaunchKernelGGL(q8_merge_kernel<W>, dim3(GRID), dim3(BLOCK), 0, st, c.num_seqs, c.num_q_heads, \
                      c.num_kv_heads, cut, seq_lens, partial, out, out_lse)
   // waves a row by the partials of an average list
-  if (plan.blocks <= 2 * lists) LOCKS_Q8_MERGE(1, (rows + 3) / 4, 256);
-  else if (plan.blocks <= 64 * lists) LOCKS_Q8_MERGE(4, rows, 256);
+  if (plan.few <= 2 * lists) LOCKS_Q8_MERGE(1, (rows + 3) / 4, 256);
+  else if (plan.few <= 64 * lists) LOCKS_Q8_MERGE(4, rows, 256);
   else LOCKS_Q8_MERGE(16, rows, 1024);
 #undef LOCKS_Q8_MERGE
   return hipGetLastError();
