@@ -33,11 +33,11 @@ hipError_t launch_q8_append(const locks_cfg_t& c, const RowArgs& a, const RopeAr
 struct Q8Plan {
   int grid, blocks, few;
 };
-// Units of a share, a multiple of 8 (a pair per wave): 8 while that takes 5/8 of `blocks` at
-// most, then what `few` blocks need (few <= blocks), but from 64 units on no more than `blocks`
-// need.  ceil(units / share) <= blocks.
+// Units of a share, a multiple of 8 (a pair per wave): 8 for up to 320 blocks, then what `few`
+// blocks need (few <= blocks), but from 64 units on no more than `blocks` need.
+// ceil(units / share) <= blocks.
 __host__ __device__ inline unsigned q8_share(unsigned units, unsigned blocks, unsigned few) {
-  if (units <= 5 * blocks) return 8;
+  if (units <= 8 * blocks && units <= 8 * 320) return 8;
   const unsigned least = (units + blocks - 1) / blocks, cap = least < 64 ? 64 : least;
   const unsigned share = (units + few - 1) / few;
   return ((share < cap ? share : cap) + 7) / 8 * 8;  // (>= 8: units > 0 here)
