@@ -245,49 +245,54 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   const int per_wave = ((n + 3) / 4 + 1) & ~1;
   const int w_begin = min(wave * per_wave, n), w_end = min(w_begin + per_wave, n);
 
-  // ---- queries: B operand of step 2 a + b, scaled by a power of two per head so that the
-  // largest element is in [2^14, 2^15): f16 holds a bf16 element then to 2^-40 of the largest,
-  // and a float in two terms to 2^-21 of itself
+  // ---- queries: B operand of step 2 a + b, as stored until the first codes are on their way
   uint4 qb[kTerms][4];
-  float head_scale;  // logits in log2 units = products * head_scale * key scale
   {
     const QT* row = q + ((long)s * H_q + h * G + min(c16, G - 1)) * kDim + 16 * r4;
-    float x[4][8], big = 0.0f;
 #pragma unroll
-    for (int st = 0; st < 4; ++st) {
-      const QT* p = row + 64 * (st >> 1) + 8 * (st & 1);
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int u = 0; u < kTerms; ++u)
+        qb[u][st] = reinterpret_cast<const uint4*>(row + 64 * (st >> 1) + 8 * (st & 1))[u];
+  }
+  // Then scaled by a power of two per head so that the largest element is in [2^14, 2^15): f16
+  // holds a bf16 element then to 2^-40 of the largest, and a float in two terms to 2^-21 of itself.
+  bool scaled = false;
+  float head_scale = 0.0f;  // logits in log2 units = products * head_scale * key scale
+  auto scale_queries = [&]() {
+    auto element = [&](int st, int e) {
       if constexpr (sizeof(QT) == 2) {
-        const uint4 w = *reinterpret_cast<const uint4*>(p);
-        const uint32_t y[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[st][2 * e] = __uint_as_float(y[e] << 16);
-          x[st][2 * e + 1] = __uint_as_float(y[e] & 0xffff0000u);
-        }
+        const uint4 w = qb[0][st];
+        const uint32_t y = e < 2 ? w.x : (e < 4 ? w.y : (e < 6 ? w.z : w.w));
+        return __uint_as_float((e & 1) ? y & 0xffff0000u : y << 16);
       } else {
-        const float4 x0 = reinterpret_cast<const float4*>(p)[0], x1 = reinterpret_cast<const float4*>(p)[1];
-        x[st][0] = x0.x; x[st][1] = x0.y; x[st][2] = x0.z; x[st][3] = x0.w;
-        x[st][4] = x1.x; x[st][5] = x1.y; x[st][6] = x1.z; x[st][7] = x1.w;
+        const uint4 w = qb[e >> 2][st];
+        return __uint_as_float((e & 3) == 0 ? w.x : ((e & 3) == 1 ? w.y : ((e & 3) == 2 ? w.z : w.w)));
       }
+    };
+    float big = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(x[st][e]));
-    }
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(element(st, e)));
     const int e2 = min(14 - exponent(rows_max(big)), 126);
     const float up = pow2(e2);
     head_scale = pow2(-e2) * (kUnit<kCode> * kLog2e / 11.313708498984761f);  // / sqrt(128)
 #pragma unroll
     for (int st = 0; st < 4; ++st) {
+      float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[st][e] *= up;
+      for (int e = 0; e < 8; ++e) x[e] = element(st, e) * up;
 #pragma unroll
       for (int m = 0; m < kTerms; ++m) {
         uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = split_h2(x[st][2 * e], x[st][2 * e + 1]);
+        for (int e = 0; e < 4; ++e) w[e] = split_h2(x[2 * e], x[2 * e + 1]);
         qb[m][st] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
-  }
+    scaled = true;
+  };
   float m = -INFINITY, l = 0.0f;  // l: this lane's tokens only
   int ve = -126;                  // o is in units of 2^ve (times 2^-15 and the codes' unit)
   f4v o[8];
@@ -340,6 +345,7 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
     load_v(0, b0);
     load_v(1, b1);
   }
+  if (!scaled) scale_queries();
   // weights enter as f16 hi + lo of p * value scale, scaled so that the largest product so far
   // lies below 2^15 (a weight then keeps 21 bits, down to 2^-40 of the largest)
   {
@@ -445,37 +451,39 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   }
   }
 
-  // ---- the block's four waves combined (m in log2 units until here); the odd row pitch of
-  // sO keeps the layout's writes and the reads along d free of bank conflicts
+  // ---- the block's four waves combined (m in log2 units): each brings its sums to the block's
+  // maximum before it writes them; the odd row pitch of sO keeps the layout's writes and the
+  // reads along d free of bank conflicts
+  // (the addresses are formed here: kept across the loop they spill registers)
+  int t_here = tid;
+  asm volatile("" : "+v"(t_here));
+  const int c_here = t_here & 15, r_here = (t_here >> 4) & 3;
   l = rows_sum(l);
-  if (r4 == 0) { sM[wave][c16] = m; sL[wave][c16] = l; }
+  if (r_here == 0) sM[wave][c_here] = m;
+  __syncthreads();
   {
-    const float down = pow2(ve) * (kUnit<kCode> / 32768.0f);
+    const float mx = fmaxf(fmaxf(sM[0][c_here], sM[1][c_here]), fmaxf(sM[2][c_here], sM[3][c_here]));
+    const float wt = __builtin_amdgcn_exp2f(m - fmaxf(mx, -3.0e38f));
+    const float down = wt * pow2(ve) * (kUnit<kCode> / 32768.0f);
+    if (r_here == 0) sL[wave][c_here] = l * wt;
 #pragma unroll
     for (int n = 0; n < 8; ++n)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sO[wave][32 * r4 + 8 * j + n][c16] = o[n][j] * down;
+      for (int j = 0; j < 4; ++j) sO[wave][32 * r_here + 8 * j + n][c_here] = o[n][j] * down;
   }
   __syncthreads();
-  for (int e = tid; e < G * (kDim + 2); e += 256) {
-    const int g = e / (kDim + 2), c = e % (kDim + 2);
-    float mx = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sM[w][g]);
-    const float origin = fmaxf(mx, -3.0e38f);
-    float acc = 0.0f, ls = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float wt = __builtin_amdgcn_exp2f(sM[w][g] - origin);
-      ls += sL[w][g] * wt;
-      if (c < kDim) acc += sO[w][c][g] * wt;
-    }
+  for (int g = t_here >> 7, c = t_here & (kDim - 1); g < G; g += 2) {
+    const float acc = (sO[0][c][g] + sO[1][c][g]) + (sO[2][c][g] + sO[3][c][g]);
+    const float ls = (sL[0][g] + sL[1][g]) + (sL[2][g] + sL[3][g]);
+    const float mx = fmaxf(fmaxf(sM[0][g], sM[1][g]), fmaxf(sM[2][g], sM[3][g]));
     const long row = (long)s * H_q + h * G + g;
     if (complete) {
-      if (c < kDim) out[row * kDim + c] = ls == 0.0f ? 0.0f : acc / ls;
-      else if (c == kDim && out_lse) out_lse[row] = ls == 0.0f ? -INFINITY : mx * kLn2 + logf(ls);
+      out[row * kDim + c] = ls == 0.0f ? 0.0f : acc / ls;
+      if (c == 0 && out_lse) out_lse[row] = ls == 0.0f ? -INFINITY : mx * kLn2 + logf(ls);
     } else {
-      partial[((blockIdx.x + (long)s * H_kv + h) * G + g) * (kDim + 2) + c] = c < kDim ? acc : (c == kDim ? mx : ls);
+      float* pr = partial + ((blockIdx.x + (long)s * H_kv + h) * G + g) * (kDim + 2);
+      pr[c] = acc;
+      if (c < 2) pr[kDim + c] = c ? ls : mx;
     }
   }
   // ---- the next list with units
