@@ -12,10 +12,17 @@ namespace {
 
 constexpr int kRows = 4;  // rows in flight per 16 lanes
 
+// From this many written bytes on (more than the L2s hold), rows pass the caches' replacement.
+// Alone, and with a copy of q_out behind it as its reader, cached against streamed:
+// 1,024 bf16 tokens of 48 heads 8.2 / 11.9 us against 7.0 / 13.3; 4,096 24.7 / 36.1 against
+// 20.2 / 34.9; 16,384 78.7 / 133 against 71.5 / 122; 16,384 of 10 heads (42 MB) 27.2 / 38.3
+// against 25.6 / 40.0.
+constexpr long kStreamBytes = 48L << 20;
+
 // Wave (token, part), a token's parts in a row (15K prompt tokens of 48 heads: 71.2 us, with
 // a part's tokens in a row 75.8): q_parts of `rows` query rows, then of `rows` key
 // and value rows (keys first).
-template <typename QT, typename KT>
+template <typename QT, typename KT, bool kStream>
 __global__ __launch_bounds__(256) void rope_append_kernel(
     RowArgs a, RopeArgs rope, KT* __restrict__ k_cache, KT* __restrict__ v_cache,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ seq_lens, int S, int H_q,
@@ -36,8 +43,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(
   const KT* v = static_cast<const KT*>(a.v) + row * a.v_stride;
   auto q_src = [&](int r) { return q + r * kDim; };
   auto kv_src = [&](int r) { return r < H_kv ? k + r * kDim : v + (r - H_kv) * kDim; };
-  Mover<QT, kRows> mq;
-  Mover<KT, kRows> mk;
+  Mover<QT, kRows, kStream> mq;
+  Mover<KT, kRows, kStream> mk;
   if (is_q) mq.begin(ln, r0 + tg, r1, q_src);
   else mk.begin(ln, r0 + tg, r1, kv_src);
 
@@ -73,7 +80,9 @@ hipError_t launch_typed(const locks_cfg_t& c, const RowArgs& a, const RopeArgs& 
   const int q_parts = (hq + per - 1) / per, kv_parts = (hkv + per - 1) / per;
   const long waves = (long)a.n_tokens * (q_parts + kv_parts);
   if (waves + 3 > 0x7fffffffL) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((rope_append_kernel<QT, KT>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a, r,
+  const long bytes = (long)a.n_tokens * kDim * (hq * (long)sizeof(QT) + hkv * (long)sizeof(KT));
+  auto* kernel = bytes >= kStreamBytes ? rope_append_kernel<QT, KT, true> : rope_append_kernel<QT, KT, false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a, r,
                      static_cast<KT*>(k_cache), static_cast<KT*>(v_cache), page_table, seq_lens,
                      c.num_seqs, hq, c.num_kv_heads, c.max_pages_per_seq, c.num_blocks, c.page_size,
                      (unsigned)(q_parts + kv_parts), q_parts, per);

@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
     const int r0 = part * q_rows, r1 = min(r0 + q_rows, H_q);
     const QT* q = static_cast<const QT*>(a.q) + row * a.q_stride;
     auto src = [&](int r) { return q + r * kDim; };
-    Mover<QT, kRows> mq;
+    Mover<QT, kRows, false> mq;
     mq.begin(ln, r0 + tg, r1, src);
     const NewTokens t = tokens_of_row(a, seq_lens, S, row);
     if (t.s < 0) return;

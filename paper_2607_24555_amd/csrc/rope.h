@@ -24,18 +24,32 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 
 // A lane's eight elements of a row: chunks of four from a and from b, as stored, as floats,
 // and back.
+// kStream: past the cache levels' replacement.
+template <bool kStream, typename V, typename T>
+__device__ __forceinline__ V load_as(const T* p) {
+  if constexpr (kStream) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
+}
+template <bool kStream, typename V, typename T>
+__device__ __forceinline__ void store_as(V v, T* p) {
+  if constexpr (kStream) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
+  else *reinterpret_cast<V*>(p) = v;
+}
+
 template <typename T>
 struct Row8;
 template <>
 struct Row8<uint16_t> {
   u2v lo, hi;
+  template <bool kStream = false>
   __device__ __forceinline__ void load(const uint16_t* p, int a, int b) {
-    lo = *reinterpret_cast<const u2v*>(p + a);
-    hi = *reinterpret_cast<const u2v*>(p + b);
+    lo = load_as<kStream, u2v>(p + a);
+    hi = load_as<kStream, u2v>(p + b);
   }
+  template <bool kStream>
   __device__ __forceinline__ void store(uint16_t* p, int a, int b) const {
-    *reinterpret_cast<u2v*>(p + a) = lo;
-    *reinterpret_cast<u2v*>(p + b) = hi;
+    store_as<kStream>(lo, p + a);
+    store_as<kStream>(hi, p + b);
   }
   __device__ __forceinline__ void to(float (&x)[8]) const {
 #pragma unroll
@@ -54,13 +68,15 @@ struct Row8<uint16_t> {
 template <>
 struct Row8<float> {
   f4v lo, hi;
+  template <bool kStream = false>
   __device__ __forceinline__ void load(const float* p, int a, int b) {
-    lo = *reinterpret_cast<const f4v*>(p + a);
-    hi = *reinterpret_cast<const f4v*>(p + b);
+    lo = load_as<kStream, f4v>(p + a);
+    hi = load_as<kStream, f4v>(p + b);
   }
+  template <bool kStream>
   __device__ __forceinline__ void store(float* p, int a, int b) const {
-    *reinterpret_cast<f4v*>(p + a) = lo;
-    *reinterpret_cast<f4v*>(p + b) = hi;
+    store_as<kStream>(lo, p + a);
+    store_as<kStream>(hi, p + b);
   }
   __device__ __forceinline__ void to(float (&x)[8]) const {
 #pragma unroll
@@ -215,13 +231,13 @@ __device__ __forceinline__ void rotate(const RopeArgs& r, const Lane& ln, const 
 // Rows [r0, r1) of one token, four at a time with 16 lanes each, kRows in flight per lane:
 // those below n_turned are rotated.  begin() requests the first ones, which may come before
 // the token's place and angles are known.
-template <typename T, int kRows>
+template <typename T, int kRows, bool kStream>
 struct Mover {
   Row8<T> w[kRows];
   template <typename Src>
   __device__ __forceinline__ void begin(const Lane& ln, int r, int r1, Src src) {
 #pragma unroll
-    for (int u = 0; u < kRows; ++u) w[u].load(src(min(r + 4 * u, r1 - 1)), ln.a, ln.b);
+    for (int u = 0; u < kRows; ++u) w[u].template load<kStream>(src(min(r + 4 * u, r1 - 1)), ln.a, ln.b);
   }
   template <typename Src, typename Dst>
   __device__ __forceinline__ void move(const RopeArgs& rope, const Lane& ln, const Angles& A, int tg, int r0,
@@ -237,7 +253,7 @@ struct Mover {
           rotate(rope, ln, A, x);
           y.from(x);
         }
-        if (ru < r1) y.store(dst(ru), ln.a, ln.b);
+        if (ru < r1) y.template store<kStream>(dst(ru), ln.a, ln.b);
       }
       if (r + 4 * kRows >= r1) return;
       begin(ln, r + tg + 4 * kRows, r1, src);

@@ -5,10 +5,11 @@ definitions of tests/_cache_reference.py: rotated appends into bf16 / fp32 cache
 Bounds: a rotated float32 value is within 2^-22 (|a c| + |b s|) of the 64-bit one (three
 roundings), a bf16 result half a step (2^-8 relative) further, and codes and scales are
 the definition's own float32 operations, so they are equal bit for bit.  A logit is a sum
-of 128 exact products in float32 (with float32 queries of 3 x 128, each query within 2^-24
-of its three bf16 terms), off by at most dz = n 2^-24 sum |q k|; a weight is held to 2^-16
-of itself as two bf16 terms, so an output is within (2 dz + 2^-15) max |v| of the 64-bit
-one (numerator and denominator), and the LSE within dz + 2^-18 (|lse| + 1)."""
+of n exact products in float32 (n = 128, with float32 queries 2 x 128 and 8 more for a
+query's two f16 terms, which hold it to 2^-21: 385 is allowed), off by at most dz =
+n 2^-24 sum |q k|; a weight times its value scale is held to 2^-16 of itself (two f16
+terms hold 2^-21), so an output is within (2 dz + 2^-15) max |v| of the 64-bit one
+(numerator and denominator), and the LSE within dz + 2^-18 (|lse| + 1)."""
 import numpy as np
 import pytest
 import torch
@@ -135,6 +136,31 @@ def test_rope_append(q, kv, rot, inter, axes, shape):
     # (the half step is of the value before rounding: 2^-22 more covers the difference)
     assert bool(((kc.cpu().double() - want_k).abs() <= bound * (1 + 2.0 ** -7)).all())
     assert bool(((q_out.cpu().double() - want_q).abs() <= bound_q * (1 + 2.0 ** -7)).all())
+
+
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("fp32", "fp32"), ("bf16", "fp32"), ("fp32", "bf16")])
+@pytest.mark.parametrize("inter", [False, True])
+def test_rope_append_of_a_long_prompt(q, kv, inter):
+    """A step that writes more than 48 MiB (its rows bypass the caches): the same rows, bit for
+    bit, as in short calls, which the test above checks against the definition."""
+    st = Step([5, 0], [1300, 1210], H=8, G=8, q=q, kv=kv, pad=5, seed=9)
+    written = st.cu[-1] * D * (64 * st.q.element_size() + 16 * st.k.element_size())
+    assert written >= 48 << 20
+    _, _, rope = _rope(96, inter, 1, 1400)
+    kc, vc, kc2, vc2 = (torch.zeros(st.cfg.num_blocks, st.H, 16, D, dtype=DT[kv]).cuda() for _ in range(4))
+    qd, kd, vd = (st.strided(x) for x in (st.q, st.k, st.v))
+    out, out2 = (torch.full(st.q.shape, 7.0, dtype=DT[q]).cuda() for _ in range(2))
+    C.rope_append_kv(st.cfg, kd, vd, kc, vc, st.pt, st.sl, rope, cu_tokens=st.cu_dev, q=qd, q_out=out)
+    for s in range(2):
+        for a in range(st.cu[s], st.cu[s + 1], 300):
+            b = min(a + 300, st.cu[s + 1])
+            lens = torch.tensor([0, 0], dtype=torch.int32)
+            lens[s] = st.past[s] + b - st.cu[s]
+            cu = torch.tensor([0, b - a, b - a] if s == 0 else [0, 0, b - a], dtype=torch.int32)
+            C.rope_append_kv(st.cfg, kd[a:b], vd[a:b], kc2, vc2, st.pt, lens.cuda(), rope, cu_tokens=cu.cuda(),
+                             q=qd[a:b], q_out=out2[a:b])
+    assert torch.equal(out, out2) and torch.equal(kc, kc2) and torch.equal(vc, vc2)
+    assert bool((out[st.cu[-1]:] == 7.0).all()) and bool((out[:st.cu[-1]] != 7.0).flatten(1).any(1).all())
 
 
 def test_rope_append_in_place_and_without_queries():
