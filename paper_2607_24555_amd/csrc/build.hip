@@ -7,6 +7,8 @@
 // matrix cores with the same summation order for (i, j) and (j, i), so it is
 // exactly symmetric; its eigenpairs come from the register-resident tridiagonal
 // solver of tridiag16.h (one 16-lane DPP row per item).  Everything is fp32.
+#include <type_traits>
+
 #include "build_common.h"
 #include "cache_internal.h"
 #include "tridiag16.h"
@@ -57,17 +59,18 @@ __device__ __forceinline__ int group16_min_int(int v) {
 // kBuildLast builds only those pages and scores them for the step's query (Eq. 1
 // on the decoded summary), writing their page scores and one extra (max, sum)
 // partial per query head of their sequence.
-// ST: the cache's elements, KT or codes (with k_scale [num_blocks][H_kv]; KT is then float).
-template <typename KT, typename ST, bool kFactors, int kMode>
+// KT: the cache's elements; codes come with k_scale [num_blocks][H_kv].
+template <typename KT, bool kFactors, int kMode>
 __global__ __launch_bounds__(64) void build_kernel(
-    int S, int H_kv, int max_pages, int r, const ST* __restrict__ k_cache,
+    int S, int H_kv, int max_pages, int r, const KT* __restrict__ k_cache,
     const float* __restrict__ k_scale,
     const int32_t* __restrict__ page_table, const int32_t* __restrict__ seq_lens,
     const int32_t* __restrict__ build_list, int n_items, int all_pages,
     uint8_t* __restrict__ summaries, float* __restrict__ mu_out, float* __restrict__ basis_out,
     float* __restrict__ coef_out, float* __restrict__ sigma2_out, BuildStep bs, int basis) {
   constexpr bool kScore = kMode == kBuildLast;  // (int4 bases only)
-  // raw key rows (bf16 or fp32 as stored; deviations are formed on the fly as
+  // raw key rows (as stored: 2 x 128K tokens of 8 heads in int8 take 665 us, staged as fp32
+  // keys 1,204; deviations are formed on the fly as
   // float(k) - mu, the same fp32 value for every use) share LDS with the Gram A
   // and the eigenvectors U, which are written once the Gram is complete
   constexpr int kKRow = kDim + kKPad / (int)sizeof(KT);  // key row stride (elements)
@@ -130,25 +133,29 @@ __global__ __launch_bounds__(64) void build_kernel(
   // the scored builds run beside the scan and lead the step's critical path:
   // their instructions go first on a shared SIMD
   if (kMode == kBuildLast) __builtin_amdgcn_s_setprio(3);
+  // a lane's 8 dimensions of a key row: 16-byte pieces, of codes one of 8 bytes
+  using Slice = std::conditional_t<sizeof(KT) == 1, uint2, uint4>;
+  constexpr int kSliceVec = 8 * (int)sizeof(KT) / (int)sizeof(Slice);
+  constexpr int kSliceEl = 8 / kSliceVec;
   const long blk = active ? (long)page_table[(long)s * max_pages + j] : 0;
 
-  const float key_scale = sizeof(ST) == 1 && active ? k_scale[blk * H_kv + h] : 1.0f;
+  const float key_scale = sizeof(KT) == 1 && active ? k_scale[blk * H_kv + h] : 1.0f;
 
   // ---- load row li of the page (16-byte loads), track its squared norm
   float energy = 0.0f;
   {
     constexpr int kVec = 16 / sizeof(KT);  // elements per 16-byte load
-    const ST* src = k_cache + ((blk * H_kv + h) * kPage + li) * kDim;
+    const uint4* src = reinterpret_cast<const uint4*>(k_cache + ((blk * H_kv + h) * kPage + li) * kDim);
     uint4* dst = reinterpret_cast<uint4*>(&sK[grp][li][0]);
     uint4 w[kDim / kVec];
 #pragma unroll
-    for (int u = 0; u < kDim / kVec; ++u) w[u] = active ? load_keys<KT>(src, u * kVec, key_scale) : make_uint4(0, 0, 0, 0);
+    for (int u = 0; u < kDim / kVec; ++u) w[u] = active ? src[u] : make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int u = 0; u < kDim / kVec; ++u) dst[u] = w[u];
 #pragma unroll
     for (int u = 0; u < kDim / kVec; ++u) {
       float x[kVec];
-      chunk_to_f<KT>(w[u], x);
+      keys_to_f<KT>(w[u], key_scale, x);
 #pragma unroll
       for (int c = 0; c < kVec; ++c) energy = fmaf(x[c], x[c], energy);
     }
@@ -162,10 +169,9 @@ __global__ __launch_bounds__(64) void build_kernel(
     float v[kPage][8];
 #pragma unroll
     for (int i = 0; i < kPage; ++i) {
-      const uint4* row = reinterpret_cast<const uint4*>(&sK[grp][i][8 * li]);
+      const Slice* row = reinterpret_cast<const Slice*>(&sK[grp][i][8 * li]);
 #pragma unroll
-      for (int u = 0; u < 8 / (16 / (int)sizeof(KT)); ++u)
-        chunk_to_f<KT>(row[u], &v[i][u * (16 / (int)sizeof(KT))]);
+      for (int u = 0; u < kSliceVec; ++u) keys_to_f<KT>(row[u], key_scale, &v[i][u * kSliceEl]);
     }
 #pragma unroll
     for (int w = 8; w > 0; w >>= 1)
@@ -188,12 +194,13 @@ __global__ __launch_bounds__(64) void build_kernel(
 #pragma unroll
     for (int it = 0; it < kItems; ++it) {
       acc[it] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      const float item_scale = sizeof(KT) == 1 ? __shfl(key_scale, 16 * it) : 1.0f;
       constexpr int kVec = 16 / (int)sizeof(KT);
 #pragma unroll
       for (int ch = 0; ch < 32 / kVec; ++ch) {
         const int c0 = 32 * grp + kVec * ch;
         float x[kVec];
-        chunk_to_f<KT>(*reinterpret_cast<const uint4*>(&sK[it][li][c0]), x);
+        keys_to_f<KT>(*reinterpret_cast<const uint4*>(&sK[it][li][c0]), item_scale, x);
 #pragma unroll
         for (int m = 0; m < kVec; ++m) {
           const float d = x[m] - sMu[it][c0 + m];
@@ -236,16 +243,14 @@ __global__ __launch_bounds__(64) void build_kernel(
   // ---- basis columns V[:, l] = D^T u_l / sigma_l.  This lane's 8 dimensions of
   //      the 16 key rows are re-read from global memory (the page was just
   //      loaded, so they come from cache) and held in registers.
-  constexpr int kSliceVec = 8 * (int)sizeof(KT) / 16;  // 16-byte loads per 8-element slice
-  uint4 ks[kPage][kSliceVec];
+  Slice ks[kPage][kSliceVec];
   {
-    const ST* kpage = k_cache + (blk * H_kv + h) * kPage * kDim;
+    const Slice* kpage = reinterpret_cast<const Slice*>(k_cache + (blk * H_kv + h) * kPage * kDim);
 #pragma unroll
     for (int i = 0; i < kPage; ++i)
 #pragma unroll
       for (int u = 0; u < kSliceVec; ++u)
-        ks[i][u] = active ? load_keys<KT>(kpage, i * kDim + 8 * li + u * (16 / (int)sizeof(KT)), key_scale)
-                          : make_uint4(0, 0, 0, 0);
+        ks[i][u] = active ? kpage[(i * kDim + 8 * li) / kSliceEl + u] : Slice{};
   }
   float cabs = 0.0f;  // running max |C[li][:]| for the row scale
   float mu8[8];
@@ -267,7 +272,7 @@ __global__ __launch_bounds__(64) void build_kernel(
       const float ui[kMG] = {ua.x, ua.y, ua.z, ua.w};
       float x[8];
 #pragma unroll
-      for (int u = 0; u < kSliceVec; ++u) chunk_to_f<KT>(ks[i][u], &x[u * (16 / (int)sizeof(KT))]);
+      for (int u = 0; u < kSliceVec; ++u) keys_to_f<KT>(ks[i][u], key_scale, &x[u * kSliceEl]);
 #pragma unroll
       for (int cc = 0; cc < 8; ++cc) {
         const float dv = x[cc] - mu8[cc];
@@ -475,12 +480,11 @@ hipError_t launch_build(const locks_cfg_t& c, const void* k_cache, const int32_t
   if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks), block(64);
   const BuildStep bs = step ? *step : BuildStep{};
-#define LOCKS_BUILD_S(KT, ST, F, M)                                                            \
-  hipLaunchKernelGGL((build_kernel<KT, ST, F, M>), grid, block, 0, st, c.num_seqs, c.num_kv_heads, \
-                     c.max_pages_per_seq, c.rank, static_cast<const ST*>(k_cache), code_scale,  \
+#define LOCKS_BUILD(KT, F, M)                                                                  \
+  hipLaunchKernelGGL((build_kernel<KT, F, M>), grid, block, 0, st, c.num_seqs, c.num_kv_heads,  \
+                     c.max_pages_per_seq, c.rank, static_cast<const KT*>(k_cache), code_scale,  \
                      page_table, seq_lens, build_list, n_items, (int)all_pages,                 \
                      (uint8_t*)summaries, mu, basis, coef, sigma2, bs, c.basis)
-#define LOCKS_BUILD(KT, F, M) LOCKS_BUILD_S(KT, KT, F, M)
 #define LOCKS_BUILD_T(KT)                                     \
   if (factors) LOCKS_BUILD(KT, true, kBuildAll);              \
   else if (mode == kBuildInner) LOCKS_BUILD(KT, false, kBuildInner); \
@@ -488,8 +492,8 @@ hipError_t launch_build(const locks_cfg_t& c, const void* k_cache, const int32_t
   else LOCKS_BUILD(KT, false, kBuildAll)
   if (code_scale) {  // 8-bit keys: summaries only, and not within a step
     if (mode != kBuildAll || factors) return hipErrorInvalidValue;
-    if (code == LOCKS_Q8_INT8) LOCKS_BUILD_S(float, Int8Codes, false, kBuildAll);
-    else LOCKS_BUILD_S(float, E4m3Codes, false, kBuildAll);
+    if (code == LOCKS_Q8_INT8) LOCKS_BUILD(Int8Codes, false, kBuildAll);
+    else LOCKS_BUILD(E4m3Codes, false, kBuildAll);
   } else if (c.kv_dtype == LOCKS_BF16) {
     LOCKS_BUILD_T(uint16_t);
   } else {
@@ -497,7 +501,6 @@ hipError_t launch_build(const locks_cfg_t& c, const void* k_cache, const int32_t
   }
 #undef LOCKS_BUILD_T
 #undef LOCKS_BUILD
-#undef LOCKS_BUILD_S
   return hipGetLastError();
 }
 

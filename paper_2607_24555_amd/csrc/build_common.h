@@ -27,32 +27,49 @@ __device__ __forceinline__ void chunk_to_f<float>(const uint4& w, float* out) {
   out[2] = __uint_as_float(w.z); out[3] = __uint_as_float(w.w);
 }
 
-// Where a build's keys come from: a cache of KT (bf16 or fp32), or 8-bit codes of a page with
-// its scale, which count as the fp32 keys code * scale.
+// Where a build's keys come from: a cache of bf16 or fp32, or 8-bit codes of a page with its
+// scale, which count as the fp32 keys code * scale.
 struct Int8Codes { uint8_t bits; };
 struct E4m3Codes { uint8_t bits; };
-// The 16 bytes of KT keys from element `at` of the cache.
-template <typename KT, typename ST>
-__device__ __forceinline__ uint4 load_keys(const ST* cache, long at, float scale) {
-#pragma clang fp contract(off)  // code * scale is rounded: the key, whatever is done with it
-  if constexpr (sizeof(ST) > 1) {
-    return *reinterpret_cast<const uint4*>(cache + at);
-  } else {
-    static_assert(sizeof(KT) == 4, "codes are built from as fp32 keys");
-    const int w = *reinterpret_cast<const int*>(cache + at);
-    float x[4];
-    if constexpr (__is_same(ST, Int8Codes)) {
+// The keys of a word of codes.  The product is rounded, whatever is done with it: no
+// contraction.
+template <typename ST>
+__device__ __forceinline__ void codes_to_f(uint32_t w, float scale, float* out) {
+#pragma clang fp contract(off)
+  float x[4];
+  if constexpr (__is_same(ST, Int8Codes)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (float)(int8_t)(w >> (8 * e));
-    } else {
-      x[0] = __builtin_amdgcn_cvt_f32_fp8(w, 0);
-      x[1] = __builtin_amdgcn_cvt_f32_fp8(w, 1);
-      x[2] = __builtin_amdgcn_cvt_f32_fp8(w, 2);
-      x[3] = __builtin_amdgcn_cvt_f32_fp8(w, 3);
-    }
-    return make_uint4(__float_as_uint(x[0] * scale), __float_as_uint(x[1] * scale),
-                      __float_as_uint(x[2] * scale), __float_as_uint(x[3] * scale));
+    for (int e = 0; e < 4; ++e) x[e] = (float)(int8_t)(w >> (8 * e));
+  } else {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)w, 0);
+    x[1] = __builtin_amdgcn_cvt_f32_fp8((int)w, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
+    x[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[e] = x[e] * scale;
+}
+// Elements of a chunk (16 bytes, of codes also 8) as floats; scale: of codes only.
+template <typename ST, typename W>
+__device__ __forceinline__ void keys_to_f(const W& w, float scale, float* out) {
+  if constexpr (sizeof(ST) > 1) {
+    chunk_to_f<ST>(w, out);
+  } else {
+    codes_to_f<ST>(w.x, scale, out);
+    codes_to_f<ST>(w.y, scale, out + 4);
+    if constexpr (sizeof(W) == 16) {
+      codes_to_f<ST>(w.z, scale, out + 8);
+      codes_to_f<ST>(w.w, scale, out + 12);
+    }
+  }
+}
+// Four fp32 keys from the codes at element `at` of the cache.
+template <typename ST>
+__device__ __forceinline__ uint4 load_codes(const ST* cache, long at, float scale) {
+  float x[4];
+  codes_to_f<ST>(*reinterpret_cast<const uint32_t*>(cache + at), scale, x);
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                    __float_as_uint(x[3]));
 }
 
 __device__ __forceinline__ float f16_scale(float amax, float qmax) {

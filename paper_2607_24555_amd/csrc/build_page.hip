@@ -270,7 +270,7 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(B == 32 && k
   for (int t = 0; t < kI; ++t) key_scale[t] = sizeof(ST) == 1 && item[t].active ? k_scale[item[t].row] : 1.0f;
   auto key16 = [&](int t, int tok0, uint32_t off) {
     if constexpr (sizeof(ST) == 1) {
-      return item[t].active ? load_keys<KT>(kpage(t) + tok0 * kDim, off / sizeof(KT), key_scale[t])
+      return item[t].active ? load_codes(kpage(t) + tok0 * kDim, off / sizeof(KT), key_scale[t])
                             : make_uint4(0, 0, 0, 0);
     } else {
       const char* p = reinterpret_cast<const char*>(kpage(t) + tok0 * kDim);
