@@ -42,8 +42,8 @@ typedef struct locks_rope {
 /* The rows of a step's new tokens.  With cu_tokens (device [num_seqs + 1], ascending from
  * 0) sequence s's new tokens are rows [cu_tokens[s], cu_tokens[s + 1]) and are its last
  * ones, seq_lens[s] counting them; a sequence may have none, and rows from
- * cu_tokens[num_seqs] (at most n_tokens) on are padding: they are not read, and q_out's are left as they
- * were.  Without it, row s is the newest token of sequence s and n_tokens must be num_seqs
+ * cu_tokens[num_seqs] (at most n_tokens) on are padding: any values, and q_out's rows there
+ * are left as they were.  Without it, row s is the newest token of sequence s and n_tokens must be num_seqs
  * (a sequence of length 0 has none).
  * Row t, head h of a tensor starts stride * t + 128 * h elements from its pointer. */
 typedef struct locks_rows {

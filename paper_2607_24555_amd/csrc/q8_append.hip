@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
   }
   const int first = max(t.tok0, 0), L = t.tok0 + t.n;  // tokens [first, L) are new
   const int j = first / P + ahead;
-  live = live && t.s >= 0 && t.n > 0 && j < max_pages && (long)j * P < L;
+  live = live && t.s >= 0 && t.n > 0 && ahead >= 0 && j < max_pages && (long)j * P < L;
   // (the same for the block's waves of a page, so a page's waves leave together; pages of
   // several waves meet at the barriers below)
   if (kWaves == 1 && !live) return;

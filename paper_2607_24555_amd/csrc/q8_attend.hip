@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   // weights enter as f16 hi + lo of p * value scale, scaled so that the largest product so far
   // lies below 2^15 (a weight then keeps 21 bits, down to 2^-40 of the largest)
   {
-    const int e = exponent(warp_max(my_vs)) + 1;
+    const int e = exponent(warp_max(fabsf(my_vs))) + 1;
     if (e > ve) {
       const float down = pow2(ve - e);
 #pragma unroll

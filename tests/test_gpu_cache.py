@@ -669,3 +669,74 @@ def test_long_cache_offsets_pass_32_bits():
     st = Step([0], [T], H=H, G=1, P=P)
     st.table = torch.tensor([[0, 1, 2]])
     _check_attend(st, torch.int8, q, out, lse, kk, vv, ks, vs, lambda s, h: range(3))
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_q8_attend_scales_of_any_sign_and_size(code):
+    """Scales of both signs, over six orders of magnitude, and zero."""
+    st = Step([0, 0], [1500, 70], G=4, P=16, seed=8)
+    kc, vc, ks, vs = _cache_of(st, code, seed=8)
+    sign = torch.randint(0, 2, ks.shape, generator=st.gen) * 2.0 - 1.0
+    far = 10.0 ** torch.randint(-6, 1, ks.shape, generator=st.gen).float()
+    ks, vs = ks * sign, vs * sign.flip(0) * far
+    vs[st.table[0, 3]] = 0
+    cache = C.Q8Cache(kc.cuda(), vc.cuda(), ks.cuda(), vs.cuda())
+    q = torch.randn(2, 8, D, generator=st.gen).bfloat16()
+    ws = B.alloc_workspace(st.cfg)
+    out, lse = C.q8_dense_attend(st.cfg, q.cuda(), cache, st.pt, st.sl, ws)
+    torch.cuda.synchronize()
+    _check_attend(st, code, q, out, lse, kc, vc, ks, vs, lambda s, h: range(-(-st.lens[s] // 16)))
+    # value scales of one sign only
+    cache.v_scale.copy_(-vs.abs())
+    out, lse = C.q8_dense_attend(st.cfg, q.cuda(), cache, st.pt, st.sl, ws)
+    torch.cuda.synchronize()
+    _check_attend(st, code, q, out, lse, kc, vc, ks, -vs.abs(), lambda s, h: range(-(-st.lens[s] // 16)))
+
+
+@pytest.mark.parametrize("cu", [[0, 9, 3, 12], [0, -5, 40, 12], [4, 2, 0, 12], [12, 12, 12, 12], [0, 1 << 30, 1, 12]])
+@pytest.mark.parametrize("P", [16, 32])
+def test_appends_with_rows_out_of_order_stay_in_their_blocks(cu, P):
+    """cu_tokens that does not ascend: whatever is written lies in the table's blocks and in
+    the rows' outputs (many sequences search it in another way)."""
+    for S in (3, 90):
+        st = Step([5] * S, [4] * S, P=P, seed=1)
+        cud = torch.tensor(cu[:3] * (S // 3) + [cu[3]], dtype=torch.int32).cuda()
+        k = torch.ones(12, st.H, D, dtype=torch.bfloat16).cuda()
+        kc = torch.zeros(st.cfg.num_blocks, st.H, P, D, dtype=torch.bfloat16).cuda()
+        cache = C.alloc_q8_cache(st.cfg)
+        outside = torch.ones(st.cfg.num_blocks, dtype=torch.bool)
+        outside[st.table[st.table >= 0].long()] = False
+        C.rope_append_kv(st.cfg, k, k, kc, kc, st.pt, st.sl, cu_tokens=cud)
+        C.q8_append_kv(st.cfg, k, k, cache, st.pt, st.sl, cu_tokens=cud)
+        assert outside.any() and not kc[outside].any() and not cache.k[outside].any()
+        assert not cache.k_scale[outside].any() and not cache.v[outside].any()
+
+
+def test_two_calls_at_once():
+    """Two attentions and two appends on two streams, each with its own buffers."""
+    st = Step([0, 0, 0], [3000, 17, 900], G=4, seed=4)
+    made = []
+    for i, code in enumerate(CODES):
+        kc, vc, ks, vs = (x.cuda() for x in _cache_of(st, code, seed=i, poison=False))
+        q = torch.randn(3, 8, D, generator=st.gen).bfloat16().cuda()
+        store = C.Q8Cache(kc, vc, ks, vs)
+        want = C.q8_dense_attend(st.cfg, q, store, st.pt, st.sl, B.alloc_workspace(st.cfg))
+        attend = C.prepare_q8_dense_attend(st.cfg, q, store, st.pt, st.sl, B.alloc_workspace(st.cfg))
+        wide = Step([0, 0], [700, 900], seed=5 + i)
+        rows = [wide.k.cuda(), wide.v.cuda(), wide.q.cuda()]
+        twin = [C.alloc_q8_cache(wide.cfg, code) for _ in range(2)]
+        C.q8_append_kv(wide.cfg, rows[0], rows[1], twin[0], wide.pt, wide.sl, cu_tokens=wide.cu_dev)
+        append = C.prepare_q8_append_kv(wide.cfg, rows[0], rows[1], twin[1], wide.pt, wide.sl,
+                                        cu_tokens=wide.cu_dev)
+        made.append((want, attend, twin, append))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in made]
+    for _ in range(4):
+        for s, (_, attend, _, append) in zip(streams, made):
+            attend(s)
+            append(s)
+    torch.cuda.synchronize()
+    for want, attend, twin, _ in made:
+        assert torch.equal(attend.outputs[0], want[0]) and torch.equal(attend.outputs[1], want[1])
+        assert torch.equal(twin[0].k.view(torch.uint8), twin[1].k.view(torch.uint8))
+        assert torch.equal(twin[0].v_scale, twin[1].v_scale)
