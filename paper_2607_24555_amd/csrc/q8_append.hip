@@ -7,6 +7,12 @@
 // as rotated fp32 values, so that a page's largest magnitude, its scale and its codes come
 // from one read; the next head's rows are in flight meanwhile.  Only where the scale of a page
 // with earlier rows grows are those rows read and rounded again.
+// Prompts are bound by HBM: 15K bf16 tokens of 32 + 2 x 8 heads take 72.2 us, 4.9 TB/s (VALU
+// busy 0.32, three waves a SIMD); as many of 32 + 2 x 2 heads in 64-token pages 57.8 us, 4.6
+// TB/s.  The queries' rows stay cached: streamed past the caches, 8K tokens of 32 heads took
+// 42.1 us instead of 45.4, but with a reader behind them 69.9 instead of 67.2.  64 single tokens
+// are bound by latency: 4.5 us, of which an empty launch is 1.9 and the old page's scale and
+// codes one more round trip.
 #include <type_traits>
 
 #include "rope.h"

@@ -14,6 +14,13 @@
 // e4m3: 4 bits), the key scale multiplies the logits, the value scale the weights, which enter
 // as f16 hi + lo (21 bits; in bf16 hi + lo, 16 bits, they cost ten times the error: 2.7e-6
 // against 2.6e-7 over tables of 256 tokens).
+//
+// Long caches are bound by HBM, 256 bytes a token and head: 8 x 128K tokens of 8 heads 357 us,
+// 6.0 TB/s; 8 ragged sequences (272K tokens) 100.6 us, 5.6 TB/s; 1M tokens of two heads of 16
+// queries 94 us, 5.7 TB/s (VALU busy 0.31 to 0.38, matrix cores 0.11; a large copy reaches 5.1).
+// Tables and short caches are bound by latency, the chain length -> table -> page -> codes and
+// scale -> combine, and a merge where a list is split: 4,099 tokens of 8 heads 10.8 us, 2,048
+// tokens of 8 x 8 lists 13.1 us (attention 10.4 and merge 4.0 alone).
 #include "cache_internal.h"
 
 namespace locks {
