@@ -65,10 +65,10 @@ int append_args(const locks_cfg_t* c, const locks_rows_t* rows, const locks_rope
 }
 
 // Equal shares for 512 blocks, two of the three that a compute unit holds (8 ragged sequences,
-// 272K tokens, 8 heads: 111 us; 256 blocks 120, 768 114, 1,024 122), but for 256 where a share
-// is 8 to 64 units and there are no more lists than that (65K tokens of one head 13.8 us
-// against 16.6, of eight 29.8 against 28.8); as many blocks as lists between 512 and 1,024 of
-// them; fewer where the workspace holds fewer partials (they may take it up to the checked
+// 272K tokens, 8 heads: 98 us; 256 blocks 111, 640 110, 768 100, 1,024 101), but for 256 where
+// a share is 8 to 64 units and there are no more lists than that (65K tokens of one head 13.8
+// us against 16.6, of eight 29.8 against 28.8); as many blocks as lists between 512 and 1,024
+// of them; fewer where the workspace holds fewer partials (they may take it up to the checked
 // tables).
 // A block per list, without partials, up to the widths where that was no slower: 32 units with
 // few lists (64 lists: 9.3 us against 10.4, at 64 units 14.9 against 12.8), 64 from 128 lists
