@@ -19,8 +19,8 @@
 // 6.0 TB/s; 8 ragged sequences (272K tokens) 100.6 us, 5.6 TB/s; 1M tokens of two heads of 16
 // queries 94 us, 5.7 TB/s (VALU busy 0.31 to 0.38, matrix cores 0.11; a large copy reaches 5.1).
 // Tables and short caches are bound by latency, the chain length -> table -> page -> codes and
-// scale -> combine, and a merge where a list is split: 4,099 tokens of 8 heads 10.8 us, 2,048
-// tokens of 8 x 8 lists 13.1 us (attention 10.4 and merge 4.0 alone).
+// scale -> combine, and a merge where a list is split: 4,099 tokens of 8 heads 10.7 us, 2,048
+// tokens of 8 x 8 lists 12.8 us (attention 10.2 and merge 4.0 alone).
 #include "cache_internal.h"
 
 namespace locks {
@@ -117,7 +117,7 @@ __device__ __forceinline__ float rows_sum(float v) {
 
 // A read of codes.  kStream: of a whole cache, which the next step does not find in a cache
 // level anyway, past the levels' replacement (8 x 128K tokens: 383 -> 356 us, 6.0 TB/s); the
-// pages of a table are read again by the next steps and stay ordinary reads (13.1 us against
+// pages of a table are read again by the next steps and stay ordinary reads (13.0 us against
 // 14.4 where they are).
 template <bool kStream, typename V>
 __device__ __forceinline__ V load_codes(const uint8_t* p) {
@@ -220,7 +220,8 @@ struct Order {
 // Codes of two units, lane (c, r): k[u][a] token c, dims 64 a + 16 r .. + 15; v[u][j] token
 // 4 r + j, dims 8 c .. + 7.  Each half of the next pair is requested as soon as its registers
 // are free: the keys after the logits' products, the values after the outputs'.
-template <typename QT, int kCode, bool kStream>
+// kAll: the whole cache, else page_ids' pages.
+template <typename QT, int kCode, bool kAll>
 __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
     int S, int H_q, int H_kv, int max_pages, int k_list, int pgsz, int lg_sub, const QT* __restrict__ q,
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ v_codes,
@@ -257,8 +258,10 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   }
 
   while (true) {  // one piece: units [at, at + n) of list (s, h)
-  const int L = uniform(order.length(s));
-  const int real = order.fixed ? order.fixed : units_of(L);
+  // (of a table's list the length is only waited for once its pages are on their way: 13.0 ->
+  // 12.75 us of 64 lists)
+  int L = kAll ? uniform(order.length(s)) : 0;
+  const int real = kAll ? units_of(L) : order.fixed;
   const int taken = min(left, order.padded(real) - at), n = min(taken, real - at);
   const bool complete = taken == order.padded(real);  // the whole list: its output is formed here
   const int per_wave = ((n + 3) / 4 + 1) & ~1;
@@ -324,7 +327,10 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   const int t = at + i0 + lane, entry = t >> lg_sub;
   const bool mine = i0 + lane < w_end;
   int id = entry;
-  if (page_ids) id = mine && entry < k_list ? page_ids[((long)s * H_kv + h) * k_list + entry] : -1;
+  if constexpr (!kAll) {
+    id = mine && entry < k_list ? page_ids[((long)s * H_kv + h) * k_list + entry] : -1;
+    L = uniform(order.length(s));
+  }
   int my_tok = -1, my_blk = 0;
   float my_ks = 0.0f, my_vs = 0.0f;
   if (mine && id >= 0 && id < (L + pgsz - 1) / pgsz) {
@@ -351,11 +357,11 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   u2v vc[2][4];
   auto load_k = [&](int u, long base) {
 #pragma unroll
-    for (int a = 0; a < 2; ++a) kc[u][a] = load_codes<kStream, u4v>(k_codes + base + k_off + 64 * a);
+    for (int a = 0; a < 2; ++a) kc[u][a] = load_codes<kAll, u4v>(k_codes + base + k_off + 64 * a);
   };
   auto load_v = [&](int u, long base) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) vc[u][j] = load_codes<kStream, u2v>(v_codes + base + v_off + j * kDim);
+    for (int j = 0; j < 4; ++j) vc[u][j] = load_codes<kAll, u2v>(v_codes + base + v_off + j * kDim);
   };
   {
     const long b0 = unit_at(0), b1 = unit_at(1);
