@@ -17,9 +17,9 @@ constexpr int kRows = 4;  // rows in flight per 16 lanes
 
 // From this many written bytes on (more than the L2s hold), rows pass the caches' replacement.
 // Alone, and with a copy of q_out behind it as its reader, cached against streamed:
-// 1,024 bf16 tokens of 48 heads 8.2 / 11.9 us against 7.0 / 13.3; 4,096 24.7 / 36.1 against
-// 20.2 / 34.9; 16,384 78.7 / 133 against 71.5 / 122; 16,384 of 10 heads (42 MB) 27.2 / 38.3
-// against 25.6 / 40.0.
+// 1,024 bf16 tokens of 48 heads 8.2 / 11.9 us against 7.0 / 13.3; 4,096 (50 MB) 24.7 / 36.1
+// against 20.2 / 34.9; 8,192 43.2 / 66.7 against 37.7 / 65.0; 16,384 of 10 heads (42 MB)
+// 27.2 / 38.3 against 25.6 / 40.0.
 constexpr long kStreamBytes = 48L << 20;
 
 // Wave (token, part), a token's parts in a row (15K prompt tokens of 48 heads, cached stores:

@@ -160,6 +160,8 @@ def test_rope_append_of_a_long_prompt(q, kv, inter):
             C.rope_append_kv(st.cfg, kd[a:b], vd[a:b], kc2, vc2, st.pt, lens.cuda(), rope, cu_tokens=cu.cuda(),
                              q=qd[a:b], q_out=out2[a:b])
     assert torch.equal(out, out2) and torch.equal(kc, kc2) and torch.equal(vc, vc2)
+    C.rope_append_kv(st.cfg, kd, vd, kc, vc, st.pt, st.sl, rope, cu_tokens=st.cu_dev, q=qd, q_out=qd)  # in place
+    assert torch.equal(qd[:st.cu[-1]], out[:st.cu[-1]])
     assert bool((out[st.cu[-1]:] == 7.0).all()) and bool((out[:st.cu[-1]] != 7.0).flatten(1).any(1).all())
 
 
