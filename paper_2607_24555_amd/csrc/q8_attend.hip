@@ -115,10 +115,13 @@ __device__ __forceinline__ float rows_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// A read of codes.  kStream: of a whole cache, which the next step does not find in a cache
-// level anyway, past the levels' replacement (8 x 128K tokens: 383 -> 356 us, 6.0 TB/s); the
-// pages of a table are read again by the next steps and stay ordinary reads (13.0 us against
-// 14.4 where they are).
+// A read of codes.  kStream: past the cache levels' replacement.  Faster where the codes come
+// from HBM (8 x 128K tokens, a whole cache: 383 -> 356 us, 6.0 TB/s; 16 x 4K in 8 copies in
+// turn: 33.4 -> 31.5; 64 lists' tables, 35 of 34 MB in turn: 15.0 -> 14.3), slower where the last
+// level (256 MB) still holds them (16 x 4K again and again: 27.9 -> 30.6; 3 such tables in turn:
+// 13.2 -> 13.9).  A whole cache that fits there is small work and does not stay there beside a
+// model's weights; a table's pages are few and mostly the ones of the step before, so those
+// are left to the caches.
 template <bool kStream, typename V>
 __device__ __forceinline__ V load_codes(const uint8_t* p) {
   if constexpr (kStream) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
