@@ -163,18 +163,29 @@ struct Order {
     const int lane = threadIdx.x & 63;
     len = S <= 64 && lane < S ? seq_lens[lane] : 0;
     end = 0;
-    int sum = fixed ? S * padded(fixed) : 0;
-    for (int s0 = 0; !fixed && s0 < S; s0 += 64) {
-      end = scan_from(s0, sum);
-      sum = __builtin_amdgcn_readlane(end, 63);
+    units = share = 0;
+    if (!cut.blocks) return;  // a block a list: no shares (4,096 sequences: 140 -> 66 us)
+    int sum = S * padded(fixed);
+    if (!fixed) {
+      if (S <= 64) {
+        end = scan(len, 0);
+        sum = __builtin_amdgcn_readlane(end, 63);
+      } else {
+        sum = 0;
+#pragma unroll 4
+        for (int i = lane; i < S; i += 64) sum += padded(units_of(seq_lens[i]));
+        sum = __builtin_amdgcn_readlane(wave_scan(sum), 63);
+      }
     }
     units = (unsigned)sum * H_kv;
-    share = cut.blocks ? q8_share(units, cut.blocks, cut.few) : 0;
+    share = q8_share(units, cut.blocks, cut.few);
   }
   static __device__ __forceinline__ int padded(int n) { return (n + 7) & ~7; }
-  __device__ __forceinline__ int scan_from(int s0, int sum) const {
+  // Units of one KV head up to and with each lane's sequence, `sum` of them before the first's.
+  static __device__ __forceinline__ int scan(int lane_len, int sum) { return sum + wave_scan(padded(units_of(lane_len))); }
+  __device__ __forceinline__ int load(int s0) const {
     const int i = s0 + (threadIdx.x & 63);
-    return sum + wave_scan(padded(units_of(S <= 64 ? len : (i < S ? seq_lens[i] : 0))));
+    return i < S ? seq_lens[i] : 0;
   }
   // s is wave-uniform
   __device__ __forceinline__ int length(int s) const {
@@ -185,9 +196,10 @@ struct Order {
   __device__ __forceinline__ int before(int s) const {
     if (fixed) return s * padded(fixed);
     int e = end, sum = 0;
-    for (int s0 = 0; S > 64 && s0 <= s; s0 += 64) {
-      e = scan_from(s0, sum);
-      if (s0 + 64 <= s) sum = __builtin_amdgcn_readlane(e, 63);
+    if (S > 64) {
+      for (int i = threadIdx.x & 63; i < (s & ~63); i += 64) sum += padded(units_of(seq_lens[i]));
+      sum = __builtin_amdgcn_readlane(wave_scan(sum), 63);
+      e = scan(load(s & ~63), sum);
     }
     return (s & 63) ? __builtin_amdgcn_readlane(e, (s & 63) - 1) : sum;
   }
@@ -198,9 +210,13 @@ struct Order {
       bef = s * padded(fixed);
       return s;
     }
-    int e = end, sum = 0;
+    int e = end, sum = 0, next = S > 64 ? load(0) : 0;
     for (int s0 = 0; s0 < S; s0 += 64) {
-      if (S > 64) e = scan_from(s0, sum);
+      if (S > 64) {
+        const int now = next;
+        next = load(s0 + 64);  // (zeros past the last)
+        e = scan(now, sum);
+      }
       const unsigned long long past = __ballot((unsigned)e * H_kv > u);
       if (past) {
         const int i = __ffsll(past) - 1;

@@ -742,3 +742,55 @@ def test_two_calls_at_once():
         assert torch.equal(attend.outputs[0], want[0]) and torch.equal(attend.outputs[1], want[1])
         assert torch.equal(twin[0].k.view(torch.uint8), twin[1].k.view(torch.uint8))
         assert torch.equal(twin[0].v_scale, twin[1].v_scale)
+
+
+@pytest.mark.parametrize("wide", [1, 30])
+def test_thousands_of_sequences(wide):
+    """More sequences than one search round holds: appended without rotation and attended, in a
+    table of their width (a block a list) and in a wide one (shares)."""
+    S, P, H = 4500, 16, 1
+    g = torch.Generator().manual_seed(12)
+    past = torch.randint(0, 14, (S,), generator=g)
+    new = torch.randint(0, 3, (S,), generator=g)
+    sl = past + new
+    cfg = B.Config(S, 2, H, 8, 64, 20 * wide, S + 5, B.LOCKS_FP32, page_size=P)
+    pt = torch.full((S, 20 * wide), -1, dtype=torch.int32)
+    pt[:, 0] = torch.randperm(S + 5, generator=g)[:S].int()
+    cu = torch.cat([torch.zeros(1, dtype=torch.int64), new.cumsum(0)]).int()
+    n = int(cu[-1])
+    # rows whose largest magnitude is 127 in every page: the scale is 1 and codes are the rows
+    rows = torch.randint(-127, 128, (2, n, H, D), generator=g).float()
+    rows[..., 7] = 127.0
+    kc, vc = (torch.zeros(S + 5, H, P, D).cuda() for _ in range(2))
+    cache = C.alloc_q8_cache(cfg)
+    old = torch.randint(-127, 128, cache.k.shape, generator=g).to(torch.int8)
+    cache.k.copy_(old), cache.v.copy_(old.flip(0))
+    cache.k_scale.fill_(1.0), cache.v_scale.fill_(1.0)
+    want_k, want_v = old.float(), old.flip(0).float()
+    dev = [pt.cuda(), sl.int().cuda()]
+    for call, store in ((C.rope_append_kv, (kc, vc)), (C.q8_append_kv, (cache,))):
+        call(cfg, rows[0].cuda(), rows[1].cuda(), *store, *dev, cu_tokens=cu.cuda())
+    seq = torch.repeat_interleave(torch.arange(S), new)
+    at = past[seq] + torch.arange(n) - cu[seq].long()
+    blk = pt[seq, 0].long()
+    plain = torch.zeros(2, S + 5, H, P, D)
+    plain[0][blk, :, at], plain[1][blk, :, at] = rows[0], rows[1]
+    want_k[blk, :, at], want_v[blk, :, at] = rows[0], rows[1]
+    assert torch.equal(kc.cpu(), plain[0]) and torch.equal(vc.cpu(), plain[1])
+    assert torch.equal(cache.k.cpu().float(), want_k) and torch.equal(cache.v.cpu().float(), want_v)
+    assert bool((cache.k_scale == 1).all()) and bool((cache.v_scale == 1).all())
+    cfg.kv_dtype = B.LOCKS_BF16
+    q = (torch.randn(S, 2, D, generator=g) / 64).bfloat16()
+    out, lse = C.q8_dense_attend(cfg, q.cuda(), cache, *dev, B.alloc_workspace(cfg))
+    K, V = want_k[pt[:, 0].long(), 0].double(), want_v[pt[:, 0].long(), 0].double()
+    z = torch.matmul(q.double(), K.transpose(1, 2).contiguous()) / D ** 0.5
+    z = torch.where(torch.arange(P) < sl[:, None, None], z, -torch.inf)
+    big = torch.matmul(q.double().abs(), K.abs().transpose(1, 2).contiguous()).amax() / D ** 0.5
+    want = torch.matmul(torch.softmax(z, -1), V)
+    want[sl == 0] = 0
+    dz = 128 * 2.0 ** -24 * float(big)
+    assert bool(((out.cpu().double() - want).abs() <= (2 * dz + 2.0 ** -15) * 127).all())
+    lw = torch.logsumexp(z, -1)
+    assert torch.equal(torch.isneginf(lse.cpu()), torch.isneginf(lw))
+    live = sl > 0
+    assert bool(((lse.cpu().double() - lw)[live].abs() <= dz + 2.0 ** -18 * (lw[live].abs() + 1)).all())
