@@ -61,7 +61,7 @@ __device__ __forceinline__ uint2 codes_of(const float (&x)[8]) {
   }
 }
 
-// The same where there may be NaN among them: 0 (int8) or e4m3's NaN.
+// The same where there may be NaN among them: 0 (int8) or e4m3's NaN.  (Infinities saturate.)
 template <int kCode>
 __device__ __forceinline__ uint2 codes_of_any(const float (&x)[8]) {
   float y[8];
@@ -252,7 +252,12 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[e] = x[u][e] * inv;
       uint2 c = codes_of<kCode>(y);
-      if (odd) c = codes_of_any<kCode>(y);
+      if (odd) {
+        // an infinity stays one whatever the scale: the inverse of a page of zeros is 0
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = __builtin_isinf(x[u][e]) ? x[u][e] : y[e];
+        c = codes_of_any<kCode>(y);
+      }
       bool put = on[u];
       if (grew && i0 + 4 * u < earlier) {  // an earlier row under the larger scale
         values_of<kCode>(make_uint2(*reinterpret_cast<uint32_t*>(to + ln.a), *reinterpret_cast<uint32_t*>(to + ln.b)), y);
