@@ -12,8 +12,9 @@
 // merge.  A wave
 // takes two units a step on the matrix cores.  Codes are exact in f16 (int8: 7 bits and sign;
 // e4m3: 4 bits), the key scale multiplies the logits, the value scale the weights, which enter
-// as f16 hi + lo (21 bits; in bf16 hi + lo, 16 bits, they cost ten times the error: 2.7e-6
-// against 2.6e-7 over tables of 256 tokens).
+// as f16 hi + lo, both rounded to nearest: off by at most 2^-23, twice what a float is,
+// and to no side.  (Rounded toward zero, 2^-21, outputs were 2^-23 too small on average; bf16
+// hi + lo, 16 bits, cost ten times the error over tables of 256 tokens.)
 //
 // Long caches are bound by HBM, 256 bytes a token and head: 8 x 128K tokens of 8 heads 357 us,
 // 6.0 TB/s; 8 ragged sequences (272K tokens) 100.6 us, 5.6 TB/s; 1M tokens of two heads of 16
@@ -28,6 +29,7 @@ namespace {
 
 typedef _Float16 h8v __attribute__((ext_vector_type(8)));
 typedef _Float16 h2v __attribute__((ext_vector_type(2)));
+typedef float f2v __attribute__((ext_vector_type(2)));
 typedef float f4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
@@ -38,9 +40,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ h8v as_h8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(h8v, make_uint4(a, b, c, d));
 }
-// Two floats as f16 halves of a word, rounded toward zero, and what that leaves of them.
+// Two floats as f16 halves of a word, rounded to nearest, and what that leaves of them (of 24
+// bits at most 12 and a sign: the second term keeps 11 of them).
 __device__ __forceinline__ uint32_t split_h2(float& a, float& b) {
-  const h2v h = __builtin_bit_cast(h2v, __builtin_amdgcn_cvt_pkrtz(a, b));
+  const h2v h = __builtin_convertvector((f2v{a, b}), h2v);
   a -= (float)h[0];
   b -= (float)h[1];
   return __builtin_bit_cast(uint32_t, h);
@@ -296,8 +299,10 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
       for (int u = 0; u < kTerms; ++u)
         qb[u][st] = reinterpret_cast<const uint4*>(row + 64 * (st >> 1) + 8 * (st & 1))[u];
   }
-  // Then scaled by a power of two per head so that the largest element is in [2^14, 2^15): f16
-  // holds a bf16 element then to 2^-40 of the largest, and a float in two terms to 2^-21 of itself.
+  // Then scaled by a power of two per head so that the largest element is in [2^14, 2^15): f16's
+  // smallest step, 2^-24, is then at most 2^-38 of the largest.  A bf16 element is exact but for
+  // half of that step, 2^-39 of the largest; a float in two terms is held to 2^-23 of itself or to
+  // that, whichever is more.
   bool scaled = false;
   float head_scale = 0.0f;  // logits in log2 units = products * head_scale * key scale
   auto scale_queries = [&]() {
@@ -390,8 +395,9 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
     load_v(1, b1);
   }
   if (!scaled) scale_queries();
-  // weights enter as f16 hi + lo of p * value scale, scaled so that the largest product so far
-  // lies below 2^15 (a weight then keeps 21 bits, down to 2^-40 of the largest)
+  // weights enter as f16 hi + lo of p * value scale, scaled so that the largest scale so far lies
+  // in [2^14, 2^15): a weight is held to 2^-23 of itself or to half of f16's smallest step, 2^-39 of
+  // that scale, whichever is more
   {
     const int e = exponent(warp_max(fabsf(my_vs))) + 1;
     if (e > ve) {

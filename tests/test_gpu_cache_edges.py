@@ -90,3 +90,74 @@ def test_q8_append_infinities_beside_nothing_finite(code, kv, P):
         assert bool((cache.k_scale[b].cpu() == scale).all())
         _same(cache.k[b, :, n[s] + 1], torch.full((H, D), -most))
         _same(cache.v[b, :, n[s]], torch.full((H, D), -127.0 if code == torch.int8 else -384.0))
+
+
+# ---------------------------------------------------------------- attention's arithmetic
+
+def _one_page_store(S, H, code, codes, k_scale, v_scale):
+    """Sequence s's tokens lie in block s."""
+    k, v = codes
+    tab = torch.arange(S, dtype=torch.int32)[:, None].contiguous()
+    return C.Q8Cache(k.to(code).cuda(), v.to(code).cuda(), k_scale.cuda(), v_scale.cuda()), tab.cuda()
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+def test_weights_round_without_bias(code, q):
+    """Over values that are all the same the output is that value: the roundings of the weights
+    must not drift to one side.  Of 32,768 outputs (2,048 sequences of 32 tokens, 16 heads) the mean
+    signed error is less than half a float32 step, 2^-25: a weight in two f16 terms rounded to
+    nearest is off by at most 2^-23 with a mean of zero, and the few float32 sums stay below 2^-20
+    together, so the mean of N = 2^15 errors passes t = 2^-25 with a probability of at most
+    2 exp(-2 N t^2 / (2^-19)^2) = 2 exp(-16).  Terms rounded toward zero have a mean of -2^-23.7."""
+    S, H, G, P = 2048, 1, 16, 32
+    cfg = B.Config(S, G * H, H, 8, 2 * P, 1, S, B.LOCKS_FP32, LK[q], page_size=P)
+    g = torch.Generator().manual_seed(21)
+    k = torch.randint(-100, 100, (S, H, P, D), generator=g).float()
+    v = torch.full((S, H, P, D), 96.0)                                   # (a code of both kinds)
+    vs = torch.rand(S, H, generator=g) + 0.5
+    store, pt = _one_page_store(S, H, code, (k, v), torch.full((S, H), 1.0 / 128), vs)
+    qq = (torch.randn(S, G, D, generator=g) * 2).to(DT[q]).cuda()
+    sl = torch.full((S,), P, dtype=torch.int32).cuda()
+    out, _ = C.q8_dense_attend(cfg, qq, store, pt, sl, B.alloc_workspace(cfg))
+    want = 96.0 * vs.double()[:, :, None]
+    off = (out.cpu().double() - want) / want
+    print(f"[weights] {code} {q} mean 2^{np.log2(abs(float(off.mean()))):.1f} largest 2^"
+          f"{np.log2(float(off.abs().max())):.1f}", flush=True)
+    assert float(off.abs().max()) <= 2.0 ** -20
+    assert abs(float(off.mean())) <= 2.0 ** -25
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_fp32_queries_with_one_large_channel(code):
+    """fp32 queries in two f16 terms: an element is held to 2^-23 of itself or 2^-39 of the head's
+    largest (the second term's smallest step is 2^-24 where the largest is 2^14 or more, and half of
+    that is lost), whichever is more.  One channel of 2^20 meets keys that are zero there, so a
+    logit is off by sum |k| (2^-23 |q| + 2^-39 2^20) / sqrt d and the float32 sum's 256 2^-24
+    sum |q k| / sqrt d; outputs by twice that and 2^-19 for the weights and the sums."""
+    S, H, G, P = 40, 1, 4, 64
+    cfg = B.Config(S, G * H, H, 8, 2 * P, 1, S, B.LOCKS_FP32, B.LOCKS_FP32, page_size=P)
+    g = torch.Generator().manual_seed(22)
+    k = torch.randint(-100, 100, (S, H, P, D), generator=g).float()
+    k = k.to(code).float()
+    k[..., 77] = 0
+    v = torch.randint(-100, 100, (S, H, P, D), generator=g).to(code).float()
+    ks, vs = torch.full((S, H), 1.0 / 256), torch.full((S, H), 1.0 / 64)
+    store, pt = _one_page_store(S, H, code, (k, v), ks, vs)
+    qq = torch.randn(S, G, D, generator=g) * 2
+    qq[..., 77] = 2.0 ** 20
+    lens = torch.randint(1, P + 1, (S,), generator=g).int()
+    out, lse = C.q8_dense_attend(cfg, qq.cuda(), store, pt, lens.cuda(), B.alloc_workspace(cfg))
+    for s in range(S):
+        L = int(lens[s])
+        K, V, Q = k[s, 0, :L].double() / 256, v[s, 0, :L].double() / 64, qq[s].double()
+        z = Q @ K.t() / D ** 0.5
+        dz = ((Q.abs() * (2.0 ** -23 + 256 * 2.0 ** -24)) @ K.abs().t()
+              + 2.0 ** -19 * K.abs().sum(1)).amax(1) / D ** 0.5
+        # (the large channel's products are zero: they add nothing to a sum)
+        assert float((Q[:, 77, None] * K[None, :, 77]).abs().max()) == 0
+        want = torch.softmax(z, -1) @ V
+        bound = (2 * dz + 2.0 ** -19)[:, None] * V.abs().amax(0)
+        assert bool(((out[s].cpu().double() - want).abs() <= bound).all()), s
+        w = torch.logsumexp(z, -1)
+        assert bool(((lse[s].cpu().double() - w).abs() <= dz + 2.0 ** -20 * (w.abs() + 1)).all()), s
