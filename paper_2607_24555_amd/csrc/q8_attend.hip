@@ -401,13 +401,12 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   {
     const int e = exponent(warp_max(fabsf(my_vs))) + 1;
     if (e > ve) {
-      const float down = pow2(ve - e);
+      const float down = ldexpf(1.0f, ve - e);
 #pragma unroll
       for (int x = 0; x < 8; ++x) o[x] *= down;
       ve = e;
     }
-    my_vs *= pow2(-ve);
-    my_vs *= 32768.0f;
+    my_vs = ldexpf(my_vs, 15 - ve);  // (2^-ve alone may be too small for a float)
   }
 
   for (int j = 0; j < cnt; j += 2) {
@@ -514,7 +513,7 @@ __global__ __launch_bounds__(256, 3) void q8_attend_kernel(
   {
     const float mx = fmaxf(fmaxf(sM[0][c_here], sM[1][c_here]), fmaxf(sM[2][c_here], sM[3][c_here]));
     const float wt = __builtin_amdgcn_exp2f(m - fmaxf(mx, -3.0e38f));
-    const float down = wt * pow2(ve) * (kUnit<kCode> / 32768.0f);
+    const float down = ldexpf(wt * kUnit<kCode>, ve - 15);
     if (r_here == 0) sL[wave][c_here] = l * wt;
 #pragma unroll
     for (int n = 0; n < 8; ++n)

@@ -161,3 +161,29 @@ def test_fp32_queries_with_one_large_channel(code):
         assert bool(((out[s].cpu().double() - want).abs() <= bound).all()), s
         w = torch.logsumexp(z, -1)
         assert bool(((lse[s].cpu().double() - w).abs() <= dz + 2.0 ** -20 * (w.abs() + 1)).all()), s
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("exps", [(126, 127), (-149, -126), (-149, 127), (-100, 100)])
+def test_value_scales_of_any_exponent(code, exps):
+    """Value scales from the smallest subnormal to 2^127, codes of one step.  One token a
+    sequence and several of one page: weights are held to 2^-20 and the result to one more rounding
+    (2^-24, or half a subnormal, 2^-150)."""
+    S, H, G, P = 64, 1, 4, 16
+    cfg = B.Config(S, G, H, 8, 2 * P, 1, S, B.LOCKS_FP32, B.LOCKS_FP32, page_size=P)
+    g = torch.Generator().manual_seed(23)
+    k = torch.randint(-100, 100, (S, H, P, D), generator=g).float()
+    sign = torch.randint(0, 2, (S, H, 1, D), generator=g) * 2.0 - 1.0
+    v = sign.expand(S, H, P, D).contiguous()      # the same in every token: the output is +-scale
+    e = torch.tensor(exps)[torch.randint(0, 2, (S, H), generator=g)]
+    vs = torch.ldexp(torch.ones(S, H, dtype=torch.float64), e).float()
+    assert bool((vs > 0).all()) and bool(torch.isfinite(vs).all())
+    store, pt = _one_page_store(S, H, code, (k, v), torch.full((S, H), 1.0 / 64), vs)
+    for L in (1, 16):
+        if L > 1 and max(exps) > 123:
+            continue                # (weights times values, summed before the division, pass float32)
+        sl = torch.full((S,), L, dtype=torch.int32).cuda()
+        out, _ = C.q8_dense_attend(cfg, torch.randn(S, G, D, generator=g).cuda(), store, pt, sl,
+                                   B.alloc_workspace(cfg))
+        want = (sign[:, :, 0] * vs[..., None]).double().expand(S, G, D)
+        assert bool(((out.cpu().double() - want).abs() <= want.abs() * 2.0 ** -19 + 2.0 ** -149).all()), L
