@@ -84,11 +84,11 @@ typedef struct locks_q8 {
 /* locks_rope_append_kv into an 8-bit cache, quantised from the rotated fp32 values.  Of a
  * page, KV head and tensor let A be the largest magnitude of the call's new rows (0 if it
  * is under 2^-100).  A page that the call begins takes A's scale, one with earlier rows
- * the larger of A's and its own; where that grows, the earlier rows' codes become
- * Q(code * old scale * (1 / new scale)).  New codes are Q(x * (1 / scale)), 0 where the scale
- * is 0, Q rounding to the nearest code, ties to even, and saturating.  Elements that are not
- * finite do not count for A: an infinity takes the largest code of its sign whatever the scale,
- * a NaN becomes 0 (int8) or NaN (e4m3).
+ * keeps its own unless A's is larger than its magnitude; then it takes A's, and the earlier
+ * rows' codes become Q(code * old scale * (1 / new scale)).  New codes are Q(x * (1 / scale)),
+ * 0 where the scale is 0, Q rounding to the nearest code, ties to even, and saturating.
+ * Elements that are not finite do not count for A: an infinity takes the largest code whatever
+ * the scale (with the sign that keeps its own), a NaN becomes 0 (int8) or NaN (e4m3).
  * Scales and codes of rows past the sequence's end are left as they were, except that the
  * page's scale is theirs too.  Appending the same rows again changes nothing.
  * cfg->kv_dtype is the type of the rows.  Errors as in locks_rope_append_kv. */

@@ -240,11 +240,12 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
       for (int u = 0; u < kWaves; ++u) big = fmaxf(big, s_max[h & 1][wave / kWaves * kWaves + u]);
     }
     if (!live || big < 0.0f || h >= h1) continue;
+    // (a page's scale may have either sign: its magnitude is what rows have to fit)
     float scale = page_scale<kCode>(big);
-    if (earlier > 0 && !(scale > before)) scale = before;
-    const float inv = scale > 0.0f ? 1.0f / scale : 0.0f;
+    const bool grew = earlier > 0 && scale > fabsf(before);
+    if (earlier > 0 && !grew) scale = before;
+    const float inv = fabsf(scale) > 0.0f ? 1.0f / scale : 0.0f;
     uint8_t* codes = (kv ? v_codes : k_codes) + at * (P * kDim);
-    const bool grew = earlier > 0 && scale > before;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       uint8_t* to = codes + (i0 + 4 * u) * kDim;
@@ -253,9 +254,9 @@ __global__ __launch_bounds__(256) void q8_append_kernel(
       for (int e = 0; e < 8; ++e) y[e] = x[u][e] * inv;
       uint2 c = codes_of<kCode>(y);
       if (odd) {
-        // an infinity stays one whatever the scale: the inverse of a page of zeros is 0
+        // an infinity stays one where the page has no scale, whose inverse is 0 here
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = __builtin_isinf(x[u][e]) ? x[u][e] : y[e];
+        for (int e = 0; e < 8; ++e) y[e] = inv == 0.0f && __builtin_isinf(x[u][e]) ? x[u][e] : y[e];
         c = codes_of_any<kCode>(y);
       }
       bool put = on[u];

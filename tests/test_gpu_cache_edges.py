@@ -187,3 +187,39 @@ def test_value_scales_of_any_exponent(code, exps):
                                    B.alloc_workspace(cfg))
         want = (sign[:, :, 0] * vs[..., None]).double().expand(S, G, D)
         assert bool(((out.cpu().double() - want).abs() <= want.abs() * 2.0 ** -19 + 2.0 ** -149).all()), L
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("P", [16, 64])
+def test_q8_append_behind_a_negative_scale(code, P):
+    """Attention takes scales of either sign, so appends do too: behind rows whose page has a
+    negative scale, a smaller row is coded with it, and a larger one makes its magnitude grow;
+    either way the earlier rows keep their values."""
+    S, H = 3, 2
+    cfg = B.Config(S, H, H, 8, 2 * P, 1, S, B.LOCKS_FP32, B.LOCKS_FP32, page_size=P)
+    g = torch.Generator().manual_seed(24)
+    cache = C.alloc_q8_cache(cfg, code)
+    old = torch.randint(-8, 9, (S, H, P, D), generator=g).float()
+    for c, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        c.copy_(old)
+        s.fill_(-1.0)
+    x = torch.ones(S, H, D)
+    x[0] = 0.0                                   # nothing to scale by
+    x[1] *= 5.0                                  # fits the page's scale
+    x[2] *= 4.0 * _most(code)                    # needs four times of it
+    pt = torch.arange(S, dtype=torch.int32)[:, None].contiguous().cuda()
+    C.q8_append_kv(cfg, x.cuda(), x.cuda(), cache, pt, torch.full((S,), 4, dtype=torch.int32).cuda())
+    for c, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        c, scale = c.cpu().float(), scale.cpu()
+        assert bool((scale[:2] == -1.0).all()) and bool((scale[2] == 4.0).all())
+        values = c * scale[..., None, None]
+        assert torch.equal(values[:2, :, :3], -old[:2, :, :3])
+        assert bool(((values[2, :, :3] + old[2, :, :3]).abs() <= (2.0 if code == torch.int8 else 0.0)).all())
+        assert torch.equal(values[:, :, 3], x)
+    z = torch.full((S, H, D), -INF)              # an infinity keeps its sign
+    C.q8_append_kv(cfg, z.cuda(), z.cuda(), cache, pt, torch.full((S,), 5, dtype=torch.int32).cuda())
+    for c, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        c, scale = c.cpu().float(), scale.cpu()
+        assert bool((scale[:2] == -1.0).all()) and bool((scale[2] == 4.0).all())
+        assert torch.equal((c * scale[..., None, None])[:, :, 4],
+                           (-_most(code) * scale.abs())[..., None].expand(S, H, D))
