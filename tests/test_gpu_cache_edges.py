@@ -223,3 +223,69 @@ def test_q8_append_behind_a_negative_scale(code, P):
         assert bool((scale[:2] == -1.0).all()) and bool((scale[2] == 4.0).all())
         assert torch.equal((c * scale[..., None, None])[:, :, 4],
                            (-_most(code) * scale.abs())[..., None].expand(S, H, D))
+
+
+# ---------------------------------------------------------------- one token a sequence
+
+ONE_TOKEN_LENS = [[1], [33], [16, 0, 17, 1, 64], [0, 0], [1 + 7 * i % 50 if i % 9 else 0 for i in range(150)]]
+
+
+@pytest.mark.parametrize("lens", range(len(ONE_TOKEN_LENS)))
+@pytest.mark.parametrize("rot,inter,axes,given", [(0, False, 1, False), (128, False, 1, False), (64, True, 1, True),
+                                                  (48, False, 2, True), (112, True, 3, True)])
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("fp32", "fp32"), ("bf16", "fp32"), ("fp32", "bf16")])
+def test_rope_append_of_one_token_a_sequence(q, kv, rot, inter, axes, given, lens):
+    """Without cu_tokens row s is the newest token of sequence s; a sequence of length 0 has none,
+    its output row stays.  Values are within 2^-22 (|a c| + |b s|) of the 64-bit ones, bf16 half a
+    step more."""
+    lens = ONE_TOKEN_LENS[lens]
+    S, H, G = len(lens), 2, (4, 7, 1)[len(lens) % 3]
+    P = (16, 32, 64)[S % 3]
+    g = torch.Generator().manual_seed(S)
+    mp = max(lens) // P + 2
+    tab = torch.randperm(S * mp + 3, generator=g).int()[:S * mp].reshape(S, mp)
+    cfg = B.Config(S, G * H, H, 8, 2 * P, mp, S * mp + 3, LK[kv], LK[q], page_size=P)
+    print(f"[one token] S={S} P={P} {q}/{kv} rot={rot} inter={inter} axes={axes}", flush=True)
+    wide = torch.randn(S, G * H + 2 * H + 1, D, generator=g)
+    qr, kr, vr = wide[:, :G * H].to(DT[q]), wide[:, G * H:G * H + H].to(DT[kv]), wide[:, G * H + H:-1].to(DT[kv])
+    kc, vc = (torch.randn(cfg.num_blocks, H, P, D, generator=g).to(DT[kv]) for _ in range(2))
+    q_out = torch.full((S, G * H, D), 7.0, dtype=DT[q])
+    rope = pos = None
+    half = rot // 2
+    split = {1: [half], 2: [5, half - 5], 3: [half // 4, 3, half - half // 4 - 3]}[axes]
+    if rot:
+        rope = C.Rope(C.rope_table(300, rot), inter, None if axes == 1 else split)
+        if given:
+            pos = torch.randint(0, 300, (axes, S), generator=g, dtype=torch.int32)
+    kd, vd, qo = kc.cuda(), vc.cuda(), q_out.cuda()
+    # rows as slices of wider buffers
+    src = [torch.nn.functional.pad(t, (0, 0, 1, 2), value=NAN).cuda()[:, 1:-2] for t in (qr, kr, vr)]
+    got = C.rope_append_kv(cfg, src[1], src[2], kd, vd, tab.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(),
+                           rope, positions=None if pos is None else pos.cuda(), q=src[0], q_out=qo)
+    assert got is qo
+    want_q, want_k, bound_q, bound_k = q_out.double(), kc.double(), torch.zeros(q_out.shape, dtype=torch.float64), \
+        torch.zeros(kc.shape, dtype=torch.float64)
+    first, second = (list(range(0, rot, 2)), list(range(1, rot, 2))) if inter else (list(range(half)), list(range(half, rot)))
+    axis = [a for a, n in enumerate(split) for _ in range(n)]
+    for s, L in enumerate(lens):
+        if L == 0:
+            continue
+        b, i = int(tab[s, (L - 1) // P]), (L - 1) % P
+        vc[b, :, i] = vr[s]
+        for x, want, bound, at, dt in ((qr[s], want_q, bound_q, (s,), q), (kr[s], want_k, bound_k, (b, slice(None), i), kv)):
+            x = x.double()
+            y, e = x.clone(), torch.zeros_like(x)
+            if rot:
+                p = [L - 1] * axes if pos is None else pos[:, s].tolist()
+                rows = rope.table.cpu().double()[[p[a] for a in axis]]
+                c, sn = (rows[range(half), [o + i for i in range(half)]] for o in (0, half))
+                xa, xb = x[:, first], x[:, second]
+                y[:, first], y[:, second] = xa * c - xb * sn, xb * c + xa * sn
+                e[:, first] = ((xa * c).abs() + (xb * sn).abs()) * 2.0 ** -22
+                e[:, second] = ((xb * c).abs() + (xa * sn).abs()) * 2.0 ** -22
+                if dt == "bf16":
+                    e[:, :rot] = e[:, :rot] * (1 + 2.0 ** -8) + y[:, :rot].abs() * 2.0 ** -8
+            want[at], bound[at] = y, e
+    assert torch.equal(vd.cpu(), vc)
+    assert bool(((kd.cpu().double() - want_k).abs() <= bound_k).all())
+    assert bool(((qo.cpu().double() - want_q).abs() <= bound_q).all())
