@@ -3,10 +3,12 @@ appends with rotary positions, a cache held in 8 bits, and decode attention over
 
 As in `locks`: argument checks and marshalling only, tensors are torch device tensors on
 the current device, work goes to the given or current stream, and the prepare_* forms do
-the checks once for loops over fixed buffers.
+the checks once for loops over fixed buffers.  Outputs that a call allocates are allocated on
+the stream it runs on, those of a prepare_* form on the current one.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -111,6 +113,12 @@ def _current_device(*ts):
         raise LocksError("liblocks takes device tensors")
     if dev.index != torch.cuda.current_device():
         raise LocksError(f"tensors on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _allocating_on(stream):
+    """What is allocated within belongs to `stream`: memory of the current one may still be in
+    use by the work queued there when a call on another stream writes it."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 def _q8(cfg: Config, cache: Q8Cache) -> _Q8:
@@ -230,8 +238,9 @@ def rope_append_kv(cfg: Config, k_new, v_new, k_cache, v_cache, page_table, seq_
     into the paged caches -- locks_rope_append_kv.  k_new / v_new [n][H_kv][128], q
     [n][H_q][128] with any token stride; cu_tokens [S + 1] for ragged runs (one token per
     sequence without).  Returns the rotated queries (q_out; None without q)."""
-    call = prepare_rope_append_kv(cfg, k_new, v_new, k_cache, v_cache, page_table, seq_lens, rope,
-                                  positions, cu_tokens, q, q_out)
+    with _allocating_on(stream):
+        call = prepare_rope_append_kv(cfg, k_new, v_new, k_cache, v_cache, page_table, seq_lens, rope,
+                                      positions, cu_tokens, q, q_out)
     call(stream)
     return call.outputs
 
@@ -253,8 +262,9 @@ def q8_append_kv(cfg: Config, k_new, v_new, cache: Q8Cache, page_table, seq_lens
                  rope: Optional[Rope] = None, positions=None, cu_tokens=None, q=None, q_out=None,
                  stream=None):
     """rope_append_kv into an 8-bit cache -- locks_q8_append_kv."""
-    call = prepare_q8_append_kv(cfg, k_new, v_new, cache, page_table, seq_lens, rope, positions,
-                                cu_tokens, q, q_out)
+    with _allocating_on(stream):
+        call = prepare_q8_append_kv(cfg, k_new, v_new, cache, page_table, seq_lens, rope, positions,
+                                    cu_tokens, q, q_out)
     call(stream)
     return call.outputs
 
@@ -304,7 +314,8 @@ def prepare_q8_dense_attend(cfg: Config, q, cache: Q8Cache, page_table, seq_lens
 def q8_dense_attend(cfg: Config, q, cache: Q8Cache, page_table, seq_lens, ws, out=None, out_lse=None,
                     stream=None):
     """Decode attention over every token of an 8-bit cache -- locks_q8_dense_attend."""
-    call = prepare_q8_dense_attend(cfg, q, cache, page_table, seq_lens, ws, out, out_lse)
+    with _allocating_on(stream):
+        call = prepare_q8_dense_attend(cfg, q, cache, page_table, seq_lens, ws, out, out_lse)
     call(stream)
     return call.outputs
 
@@ -319,6 +330,7 @@ def q8_sparse_attend(cfg: Config, q, cache: Q8Cache, page_table, seq_lens, page_
                      out_lse=None, stream=None):
     """Decode attention over the listed pages of an 8-bit cache (page_ids as select returns
     them) -- locks_q8_sparse_attend."""
-    call = prepare_q8_sparse_attend(cfg, q, cache, page_table, seq_lens, page_ids, ws, out, out_lse)
+    with _allocating_on(stream):
+        call = prepare_q8_sparse_attend(cfg, q, cache, page_table, seq_lens, page_ids, ws, out, out_lse)
     call(stream)
     return call.outputs

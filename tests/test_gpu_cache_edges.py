@@ -289,3 +289,45 @@ def test_rope_append_of_one_token_a_sequence(q, kv, rot, inter, axes, given, len
     assert torch.equal(vd.cpu(), vc)
     assert bool(((kd.cpu().double() - want_k).abs() <= bound_k).all())
     assert bool(((qo.cpu().double() - want_q).abs() <= bound_q).all())
+
+
+# ---------------------------------------------------------------- streams
+
+def _stream_of(t):
+    """The stream that a tensor's memory was allocated on."""
+    for seg in torch.cuda.memory_snapshot():
+        if seg["address"] <= t.data_ptr() < seg["address"] + seg["total_size"]:
+            return seg["stream"]
+
+
+def test_outputs_belong_to_the_stream_of_their_call():
+    """Outputs that a call on another stream allocates are that stream's memory: the current
+    stream's may still be in use by the work queued there."""
+    S, H, G, P = 64, 2, 8, 16
+    cfg = B.Config(S, G * H, H, 8, 2 * P, 4, 4 * S, page_size=P)
+    g = torch.Generator().manual_seed(31)
+    q, k, v = (torch.randn(S, h, D, generator=g).bfloat16().cuda() for h in (G * H, H, H))
+    pt = torch.arange(4 * S, dtype=torch.int32).reshape(S, 4).cuda()
+    sl = torch.full((S,), 5, dtype=torch.int32).cuda()
+    ids = torch.zeros(S, H, cfg.k, dtype=torch.int32).cuda()
+    ids[..., 1:] = -1
+    kc, vc = (torch.zeros(4 * S, H, P, D, dtype=torch.bfloat16).cuda() for _ in range(2))
+    store, ws, side = C.alloc_q8_cache(cfg), B.alloc_workspace(cfg), torch.cuda.Stream()
+    calls = [lambda s: C.rope_append_kv(cfg, k, v, kc, vc, pt, sl, q=q, stream=s),
+             lambda s: C.q8_append_kv(cfg, k, v, store, pt, sl, q=q, stream=s),
+             lambda s: C.q8_dense_attend(cfg, q, store, pt, sl, ws, stream=s),
+             lambda s: C.q8_sparse_attend(cfg, q, store, pt, sl, ids, ws, stream=s)]
+    torch.cuda.synchronize()
+    for call in calls:
+        want = call(None)
+        torch.cuda.synchronize()
+        got = call(side)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            again = call(None)
+        torch.cuda.synchronize()
+        want, got, again = (x if isinstance(x, tuple) else (x,) for x in (want, got, again))
+        for a, b, c in zip(want, got, again):
+            assert torch.equal(a, b) and torch.equal(a, c)
+            assert _stream_of(a) == torch.cuda.current_stream().cuda_stream
+            assert _stream_of(b) == _stream_of(c) == side.cuda_stream
