@@ -62,7 +62,8 @@ enum {
   LOCKS_E_UNSUPPORTED = -2,  /* head_dim != 128, page_size not 16, 32 or 64, an
                                 int8 / bf16 basis or KIVI with page_size != 16,
                                 G > 16, dtype unknown, or a summary store of
-                                4 GiB or more (num_blocks * num_kv_heads * stride) */
+                                4 GiB or more (num_blocks * num_kv_heads * stride;
+                                but for the calls of locks_cache.h that read none) */
   LOCKS_E_WORKSPACE = -3,    /* ws null or smaller than locks_workspace_bytes    */
   LOCKS_E_HIP = -4           /* a HIP launch failed; see locks_last_hip_error    */
 };

@@ -10,6 +10,8 @@
  * multiple of 16 bytes; LOCKS_E_INVAL otherwise.  Where a call trusts page tables (table checks
  * off, or a call without a workspace), the appends still leave out every token whose
  * page, block, input row or position lies outside its table: nothing of it is written.
+ * The appends and the attentions touch no summaries, so they take caches whose summary store
+ * would be too large too.
  */
 #ifndef LOCKS_CACHE_H
 #define LOCKS_CACHE_H

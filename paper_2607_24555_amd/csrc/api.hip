@@ -180,7 +180,7 @@ hipError_t build_pages(const locks_cfg_t& c, const void* k_cache, const int32_t*
 
 }  // namespace
 
-int validate(const locks_cfg_t* c) {
+int validate(const locks_cfg_t* c, bool summaries) {
   if (!c) return LOCKS_E_INVAL;
   if (c->head_dim != kDim) return LOCKS_E_UNSUPPORTED;
   if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64) return LOCKS_E_UNSUPPORTED;
@@ -200,7 +200,7 @@ int validate(const locks_cfg_t* c) {
   if (c->max_pages_per_seq < 1 || c->num_blocks < 1) return LOCKS_E_INVAL;
   if ((long)c->num_seqs * c->num_q_heads > 0x7fffffffL / kDim) return LOCKS_E_INVAL;
   // record offsets are 32-bit: the summary store must stay below 4 GiB
-  if (summary_store_bytes(*c) > 0xffffffffull) return LOCKS_E_UNSUPPORTED;
+  if (summaries && summary_store_bytes(*c) > 0xffffffffull) return LOCKS_E_UNSUPPORTED;
   return LOCKS_OK;
 }
 
@@ -319,7 +319,7 @@ size_t locks_summary_stride_page(int32_t rank, int32_t basis, int32_t page_size)
 }
 
 size_t locks_workspace_bytes(const locks_cfg_t* cfg) {
-  if (validate(cfg) != LOCKS_OK) return 0;
+  if (validate(cfg, false) != LOCKS_OK) return 0;
   return plan_workspace(*cfg).total;
 }
 
@@ -617,7 +617,7 @@ int locks_set_table_checks(int32_t enable) {
 }
 
 size_t locks_table_error_offset(const locks_cfg_t* cfg) {
-  if (validate(cfg) != LOCKS_OK) return (size_t)-1;
+  if (validate(cfg, false) != LOCKS_OK) return (size_t)-1;
   return plan_workspace(*cfg).chk_err_off;
 }
 

@@ -24,7 +24,7 @@ bool rows_valid(const void* p, int64_t stride, int heads, int bytes) {
 // Checks the rows and the rotation of an append and lays them out for the kernels.
 int append_args(const locks_cfg_t* c, const locks_rows_t* rows, const locks_rope_t* rope,
                 const int32_t* page_table, const int32_t* seq_lens, RowArgs* a, RopeArgs* r) {
-  int rc = validate(c);
+  int rc = validate(c, false);
   if (rc) return rc;
   if (!rows || !page_table || !seq_lens || rows->n_tokens < 0) return LOCKS_E_INVAL;
   if (!rows->cu_tokens && rows->n_tokens != c->num_seqs) return LOCKS_E_INVAL;
@@ -92,7 +92,7 @@ Q8Plan q8_plan(const locks_cfg_t& c, long list_units, bool listed) {
 int q8_attend(const locks_cfg_t* cfg, const void* q, const locks_q8_t* cache,
               const int32_t* page_table, const int32_t* seq_lens, const int32_t* page_ids,
               bool listed, float* out, float* out_lse, void* ws, size_t ws_bytes, void* stream) {
-  int rc = validate(cfg);
+  int rc = validate(cfg, false);
   if (rc) return rc;
   if ((rc = q8_valid(cache))) return rc;
   if (!q || !aligned16(q) || !page_table || !seq_lens || !out || !aligned16(out) ||

@@ -136,8 +136,9 @@ inline int scan_blocks(const locks_cfg_t& c) {
 
 // ---------------------------------------------------------------- host checks (api.hip)
 
-// LOCKS_OK, or the status of a configuration that no call takes.
-int validate(const locks_cfg_t* c);
+// LOCKS_OK, or the status of a configuration that no call takes, or (summaries) one that none of
+// the calls takes whose kernels address the summary store.
+int validate(const locks_cfg_t* c, bool summaries = true);
 // A HIP result as a status; a failure is kept for locks_last_hip_error.
 int hip_status(hipError_t e);
 int check_ws(const locks_cfg_t* c, void* ws, size_t ws_bytes);
