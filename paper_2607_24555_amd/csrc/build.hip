@@ -72,7 +72,7 @@ __global__ __launch_bounds__(64) __attribute__((aligned(8192))) void build_kerne
     uint8_t* __restrict__ summaries, float* __restrict__ mu_out, float* __restrict__ basis_out,
     float* __restrict__ coef_out, float* __restrict__ sigma2_out, BuildStep bs, int basis) {
   constexpr bool kScore = kMode == kBuildLast;  // (int4 bases only)
-  // raw key rows (as stored: 2 x 128K tokens of 8 heads in int8 take 665 us, staged as fp32
+  // raw key rows (as stored: 2 x 128K tokens of 8 heads in int8 take 652 us, staged as fp32
   // keys 1,204; deviations are formed on the fly as
   // float(k) - mu, the same fp32 value for every use) share LDS with the Gram A
   // and the eigenvectors U, which are written once the Gram is complete

@@ -36,6 +36,10 @@ struct Q8Plan {
 // Units of a share, a multiple of 8 (a pair per wave): 8 for up to 320 blocks, then what `few`
 // blocks need (few <= blocks), but from 64 units on no more than `blocks` need.
 // ceil(units / share) <= blocks.
+// 320 stands between two kinds of batch, with blocks of 8 units against the 256 of `few`: eight
+// lists take 11.1 us against 12.7 at 264 blocks and 11.3 against 13.3 at 312, and still 11.4
+// against 13.1 at 328, from 352 on the same; one long list 14.2 against 12.9 at 275, 14.7 against
+// 13.6 at 313 and 15.0 against 13.6 at 338; 64 short ones 11.0 against 10.7 at 384.
 __host__ __device__ inline unsigned q8_share(unsigned units, unsigned blocks, unsigned few) {
   if (units <= 8 * blocks && units <= 8 * 320) return 8;
   const unsigned least = (units + blocks - 1) / blocks, cap = least < 64 ? 64 : least;

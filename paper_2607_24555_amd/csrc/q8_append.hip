@@ -11,8 +11,11 @@
 // busy 0.32, three waves a SIMD); as many of 32 + 2 x 2 heads in 64-token pages 57.8 us, 4.6
 // TB/s.  The queries' rows stay cached: streamed past the caches, 8K tokens of 32 heads took
 // 42.1 us instead of 45.4, but with a reader behind them 69.9 instead of 67.2.  64 single tokens
-// are bound by latency: 4.5 us, of which an empty launch is 1.9 and the old page's scale and
-// codes one more round trip.
+// are bound by latency: 4.5 us where the pages' scales hold, of which an empty launch is 1.9 and
+// the rest the chain length -> table -> the page's scale -> codes written.  Where scales grow, the
+// earlier codes are one more round trip: as kernels on their own, after a copy that sets the cache
+// back, 6.8 us where a third of the pages grow and 7.1 where all do against 5.2 to 6.0 where none
+// does.
 #include <type_traits>
 
 #include "rope.h"

@@ -19,6 +19,9 @@
 // Long caches are bound by HBM, 256 bytes a token and head: 8 x 128K tokens of 8 heads 357 us,
 // 6.0 TB/s; 8 ragged sequences (272K tokens) 100.6 us, 5.6 TB/s; 1M tokens of two heads of 16
 // queries 94 us, 5.7 TB/s (VALU busy 0.31 to 0.38, matrix cores 0.11; a large copy reaches 5.1).
+// Many sequences in a table far wider than they are cost more, every block and row summing the
+// lengths: 512 of 512 tokens, 8 heads, 133 us (in a table of their width 112, their bytes 104),
+// 4,096 of 256 tokens, one head, 148 (70, 52).
 // Tables and short caches are bound by latency, the chain length -> table -> page -> codes and
 // scale -> combine, and a merge where a list is split: 4,099 tokens of 8 heads 10.7 us, 2,048
 // tokens of 8 x 8 lists 12.8 us (attention 10.2 and merge 4.0 alone).
@@ -167,7 +170,7 @@ struct Order {
     len = S <= 64 && lane < S ? seq_lens[lane] : 0;
     end = 0;
     units = share = 0;
-    if (!cut.blocks) return;  // a block a list: no shares (4,096 sequences: 140 -> 66 us)
+    if (!cut.blocks) return;  // a block a list: no shares (4,096 sequences: 140 -> 70 us)
     int sum = S * padded(fixed);
     if (!fixed) {
       if (S <= 64) {
