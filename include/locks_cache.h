@@ -111,11 +111,12 @@ int locks_q8_build_summaries(const locks_cfg_t* cfg, const locks_q8_t* cache,
  * and table checks.  Rows past a sequence's end may hold any codes, and so may blocks that
  * its table does not reach.  A NaN in a query or in a scale of a live page gives NaN in its
  * outputs.
- * Sums, maxima and outputs are fp32 (weights times values are summed before the division by the
- * weights' sum, at most the tokens' number, and have to stay finite).  Codes enter as they are; queries and weights (the softmax
- * weight times its value scale) as f16 terms: a bf16 query element in one, exact but for 2^-39 of
- * its head's largest; an fp32 one, and a weight, in two, off by at most 2^-23 of itself or 2^-39 of
- * the head's largest element or the largest value scale, whichever is more.
+ * Sums, maxima and outputs are fp32 (weights times values are summed before the division by
+ * the weights' sum, at most the tokens' number, and have to stay finite).  Codes enter as they
+ * are; queries and weights (the softmax weight times its value scale) as f16 terms: a bf16
+ * query element in one, exact but for 2^-39 of its head's largest; an fp32 one, and a weight,
+ * in two, off by at most 2^-23 of itself or 2^-39 of the head's largest element or the largest
+ * value scale, whichever is more.
  * Returns LOCKS_E_INVAL for a null or misaligned pointer, LOCKS_E_UNSUPPORTED for
  * tables of 2^31 sixteen-token units or more over all sequences and KV heads. */
 int locks_q8_dense_attend(const locks_cfg_t* cfg, const void* q, const locks_q8_t* cache,
