@@ -244,12 +244,12 @@ def prepare(case, seed):
             st["call"] = T.prepare_token_mass(cfg, st["q"], st["lse"], st["k"], table, st["sl"], st["mass"],
                                               cu_tokens=st["cu"], mask=st["mask"], decay=case["decay"])
         elif case["op"] == "pick":
-            ws = T.alloc_pick_workspace(cfg, case["keep"], dev)
+            ws = T.alloc_pick_workspace(cfg, dev)
             st["call"] = T.prepare_pick_tokens(cfg, st["mass"], st["sl"], case["keep"], case["sink"],
                                                case["recent"], ws)
         else:
-            st["call"] = T.prepare_keep_tokens(cfg, st["kept"], st["k"], st["v"], table, st["sl"],
-                                               start=st["start"], mass=st["mass"], out_lens=st["lens"])
+            st["call"] = T.prepare_keep_tokens(cfg, st["kept"], st["k"], st["v"], table, start=st["start"],
+                                               mass=st["mass"], out_lens=st["lens"])
     return st
 
 
