@@ -1,0 +1,53 @@
+// Internal declarations of the calls on single tokens (include/locks_tokens.h).
+#pragma once
+
+#include "../../include/locks_tokens.h"
+#include "locks_internal.h"
+
+namespace locks {
+
+// The new tokens and the cache as the kernels take them.
+struct DraftArgs {
+  const void* q;
+  const int32_t* cu;
+  const uint32_t* mask;
+  const int32_t* page_table;
+  const int32_t* seq_lens;
+  long q_stride;
+  int n_tokens, words;
+  int S, H, G, pgsz, max_pages, num_blocks;
+};
+
+// A sequence's rows of the new tokens, held to [0, n_tokens].
+__device__ __forceinline__ int2 draft_rows(const DraftArgs& a, int s) {
+  if (!a.cu) return make_int2(s, s + 1);
+  const int b = min(max(a.cu[s], 0), a.n_tokens), e = min(max(a.cu[s + 1], 0), a.n_tokens);
+  return make_int2(b, max(b, e));
+}
+__device__ __forceinline__ int draft_len(const DraftArgs& a, int s) {
+  return min(max(a.seq_lens[s], 0), a.max_pages * a.pgsz);
+}
+// Whether new token i (mask row `row`) sees token t, `first` being the first new token's
+// index (t < L is the caller's).
+__device__ __forceinline__ bool draft_sees(const DraftArgs& a, int row, int i, int t, int first) {
+  const int j = t - first;
+  if (j < 0) return true;
+  if (!a.mask) return j <= i;
+  return j < 32 * a.words && (a.mask[(long)row * a.words + (j >> 5)] >> (j & 31) & 1);
+}
+
+size_t tree_scratch_bytes(const locks_cfg_t& c, int n_tokens);
+hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& a, const void* k_cache,
+                              const void* v_cache, void* out, bool out_bf16, float* out_lse,
+                              void* scratch, hipStream_t st);
+hipError_t launch_token_mass(const locks_cfg_t& c, const DraftArgs& a, const float* lse,
+                             const void* k_cache, float decay, float* mass, hipStream_t st);
+size_t pick_scratch_bytes(const locks_cfg_t& c);
+hipError_t launch_pick_tokens(const locks_cfg_t& c, const float* mass, const int32_t* seq_lens,
+                              int n_keep, int n_sink, int n_recent, int32_t* out_ids, void* scratch,
+                              hipStream_t st);
+hipError_t launch_keep_tokens(const locks_cfg_t& c, const int32_t* kept, int heads, int n_keep,
+                              const int32_t* start, void* k_cache, void* v_cache, float* mass,
+                              const int32_t* page_table, int32_t* out_lens, hipStream_t st);
+
+}  // namespace locks

@@ -1,0 +1,185 @@
+"""The calls on single cached tokens are exported as include/locks_tokens.h declares them and
+refuse bad arguments on the host before any launch; the binding checks tensors first, and
+tree_mask is right (no GPU)."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2607_24555_amd import locks as B
+from paper_2607_24555_amd import tokens as T
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "locks_tokens.h")
+FAKE, OTHER, ODD = ctypes.c_void_p(0x1000), ctypes.c_void_p(0x2000), ctypes.c_void_p(0x1008)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(B.LIB_PATH):
+        import __graft_entry__
+        __graft_entry__.build()
+    return T.lib()
+
+
+def cfg(**kw):
+    c = B.Config(num_seqs=2, num_q_heads=8, num_kv_heads=2, rank=8, budget_tokens=256,
+                 max_pages_per_seq=64, num_blocks=128)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+def draft(**kw):
+    d = T._Draft(0x1000, 0x1000, 0x1000, 1024, 5, 1)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def _tree(lib, c, d, k=FAKE, v=FAKE, pt=FAKE, sl=FAKE, out=OTHER, dt=1, ws=FAKE, n=None):
+    if n is None:
+        n = 1 << 40
+    return lib.locks_tree_attend(_ref(c), _ref(d), k, v, pt, sl, out, dt, None, ws, n, None)
+
+
+def _mass(lib, c, d, lse=FAKE, k=FAKE, pt=FAKE, sl=FAKE, decay=1.0, mass=OTHER):
+    return lib.locks_token_mass(_ref(c), _ref(d), lse, k, pt, sl, decay, mass, None)
+
+
+def test_every_declared_symbol_is_exported(lib):
+    src = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(locks_[a-z_0-9]+)\s*\(", src))
+    assert names == set(T._SIGS), "binding and header disagree"
+    for n in names:
+        assert hasattr(lib, n), n
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(q=None), -1), (dict(q=0x1008), -1), (dict(q_stride=1023), -1), (dict(q_stride=1028), -1),
+    (dict(q_stride=-1024), -1), (dict(q_stride=1 << 41), -1), (dict(n_tokens=-1), -1),
+    (dict(cu_tokens=None), -1),                     # five rows, two sequences
+    (dict(mask_words=0), -1), (dict(mask_words=-3), -1), (dict(mask_words=1 << 26), -2),
+    (dict(n_tokens=1 << 29), -2),
+])
+def test_bad_drafts_are_rejected(lib, bad, code):
+    c = cfg().c()
+    assert (_tree(lib, c, draft(**bad)), _mass(lib, c, draft(**bad))) == (code, code)
+
+
+def test_null_arguments_and_empty_batches(lib):
+    c = cfg().c()
+    for call in (_tree, _mass):
+        assert call(lib, None, draft()) == call(lib, c, None) == -1
+        assert call(lib, c, draft(), pt=None) == call(lib, c, draft(), sl=None) == -1
+        assert call(lib, c, draft(), k=None) == call(lib, c, draft(), k=ODD) == -1
+        assert call(lib, cfg(head_dim=64).c(), draft()) == call(lib, cfg(q_dtype=4).c(), draft()) == -2
+        wide = cfg(num_seqs=16, num_kv_heads=8, max_pages_per_seq=1 << 24).c()
+        assert call(lib, wide, draft()) == -2
+        # nothing new: no launch
+        assert call(lib, c, draft(n_tokens=0)) == call(lib, c, draft(n_tokens=0, q=None)) == 0
+        assert call(lib, cfg(num_seqs=0).c(), draft(n_tokens=0, cu_tokens=None)) == 0
+    assert _tree(lib, c, draft(), v=None) == _tree(lib, c, draft(), v=ODD) == -1
+    assert _tree(lib, c, draft(), out=None) == _tree(lib, c, draft(), out=ODD) == -1
+    assert _tree(lib, c, draft(), out=FAKE) == -1   # out is q
+    assert _tree(lib, c, draft(), dt=2) == _tree(lib, c, draft(), dt=-1) == -2
+    assert _mass(lib, c, draft(), lse=None) == _mass(lib, c, draft(), mass=None) == _mass(lib, c, draft(), mass=ODD) == -1
+    assert _mass(lib, c, draft(), decay=float("nan")) == _mass(lib, c, draft(), decay=float("inf")) == -1
+
+
+def test_workspaces(lib):
+    c = cfg().c()
+    need = lib.locks_tree_workspace_bytes(_ref(c), 5)
+    assert need >= lib.locks_workspace_bytes(_ref(c)) > 0
+    assert lib.locks_tree_workspace_bytes(_ref(c), -1) == lib.locks_tree_workspace_bytes(_ref(cfg(rank=0).c()), 5) == 0
+    assert _tree(lib, c, draft(), n=need - 1) == _tree(lib, c, draft(), ws=None) == -3
+    assert _tree(lib, c, draft(), ws=ctypes.c_void_p(0x1010)) == -3
+    assert lib.locks_pick_workspace_bytes(_ref(c)) > 0 and lib.locks_pick_workspace_bytes(None) == 0
+
+
+def test_pick_arguments(lib):
+    c = cfg().c()
+    need = lib.locks_pick_workspace_bytes(_ref(c))
+
+    def pick(c=c, mass=FAKE, sl=FAKE, keep=8, sink=2, recent=3, out=FAKE, ws=FAKE, n=need):
+        return lib.locks_pick_tokens(_ref(c), mass, sl, keep, sink, recent, out, ws, n, None)
+    assert pick(c=None) == pick(mass=None) == pick(mass=ODD) == pick(sl=None) == pick(out=None) == -1
+    assert pick(keep=0) == pick(keep=-1) == pick(sink=-1) == pick(recent=-1) == -1
+    assert pick(sink=5, recent=4) == pick(sink=9, recent=0) == pick(sink=1 << 30, recent=1 << 30) == -1
+    assert pick(keep=1 << 30) == -2
+    assert pick(ws=None) == pick(ws=ODD) == pick(n=need - 1) == -3
+    z = cfg(num_seqs=0).c()
+    assert pick(c=z, n=1 << 40) == 0
+
+
+def test_keep_arguments(lib):
+    c = cfg().c()
+
+    def keep(c=c, kept=FAKE, heads=2, n=8, start=None, k=FAKE, v=FAKE, mass=None, pt=FAKE, lens=None):
+        return lib.locks_keep_tokens(_ref(c), kept, heads, n, start, k, v, mass, pt, lens, None)
+    assert keep(c=None) == keep(kept=None) == keep(n=-1) == keep(heads=0) == keep(heads=3) == -1
+    assert keep(k=None) == keep(v=None) == keep(k=ODD) == keep(v=ODD) == keep(pt=None) == -1
+    assert keep(start=FAKE, lens=FAKE) == -1
+    assert keep(n=1 << 30) == -2
+    assert keep(c=cfg(num_seqs=0).c()) == 0
+
+
+@pytest.mark.parametrize("over,msg", [
+    (dict(q=torch.zeros(2, 8, 128)), "q: dtype"),
+    (dict(q=torch.zeros(3, 8, 128, dtype=torch.bfloat16)), "without cu_tokens"),
+    (dict(q=torch.zeros(2, 1024, dtype=torch.bfloat16)), "q: expected"),
+    (dict(cu=torch.zeros(2, dtype=torch.int32)), "device tensors|cu_tokens: shape"),
+])
+def test_binding_checks_queries(over, msg):
+    c = cfg(num_blocks=6, max_pages_per_seq=3)
+    t = dict(q=torch.zeros(2, 8, 128, dtype=torch.bfloat16), pt=torch.zeros(2, 3, dtype=torch.int32),
+             sl=torch.zeros(2, dtype=torch.int32), k=torch.zeros(6, 2, 16, 128, dtype=torch.bfloat16), cu=None)
+    t.update(over)
+    with pytest.raises(B.LocksError, match=msg):
+        T.tree_attend(c, t["q"], t["k"], t["k"], t["pt"], t["sl"], torch.zeros(8, dtype=torch.uint8),
+                      cu_tokens=t["cu"])
+
+
+def test_binding_checks_lists():
+    c = cfg(num_blocks=6, max_pages_per_seq=3)
+    k = torch.zeros(6, 2, 16, 128, dtype=torch.bfloat16)
+    pt, sl = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    ws = torch.zeros(8, dtype=torch.uint8)
+    with pytest.raises(B.LocksError, match="kept: expected"):
+        T.keep_tokens(c, torch.zeros(2, 3, 4, dtype=torch.int32), k, k, pt)
+    with pytest.raises(B.LocksError, match="kept: dtype"):
+        T.keep_tokens(c, torch.zeros(2, 2, 4, dtype=torch.int64), k, k, pt)
+    with pytest.raises(B.LocksError, match="mass: shape"):
+        T.keep_tokens(c, torch.zeros(2, 2, 4, dtype=torch.int32), k, k, pt, mass=torch.zeros(2, 2, 40))
+    with pytest.raises(B.LocksError, match="mass: shape"):
+        T.pick_tokens(c, torch.zeros(2, 2, 40), sl, 8, 1, 1, ws)
+    with pytest.raises(B.LocksError, match="device tensors"):
+        T.pick_tokens(c, torch.zeros(2, 2, 48), sl, 8, 1, 1, ws)
+    with pytest.raises(B.LocksError, match="out: shape"):
+        T.pick_tokens(c, torch.zeros(2, 2, 48), sl, 8, 1, 1, ws, out=torch.zeros(2, 2, 7, dtype=torch.int32))
+
+
+def test_tree_mask():
+    #  0        a tree of 34: row 33 follows 32, which follows the cached tokens
+    parents = [-1, 0, 0, 1] + [3] * 28 + [-1, 32] + [-1, -1]
+    mask, depth = T.tree_mask(parents, [0, 34, 34, 36], device="cpu")
+    assert mask.shape == (36, 2) and mask.dtype == torch.int32
+    word = lambda r, w: int(mask[r, w]) & 0xffffffff
+    assert [word(r, 0) for r in (0, 1, 2, 3)] == [0b1, 0b11, 0b101, 0b1011]
+    assert word(31, 0) == 0b1011 | 1 << 31 and word(31, 1) == 0
+    assert (word(32, 0), word(32, 1)) == (0, 1) and (word(33, 0), word(33, 1)) == (0, 3)
+    assert [word(34, 0), word(35, 0)] == [1, 2]
+    assert depth.tolist() == [0, 1, 1, 2] + [3] * 28 + [0, 1] + [0, 0]
+    assert T.tree_mask([], [0, 0], device="cpu")[0].shape == (0, 1)
+    for bad in ([0], [-2], [-1, 1]):
+        with pytest.raises(B.LocksError, match="parents"):
+            T.tree_mask(bad, [0, len(bad)], device="cpu")
+    for cu in ([0, 1], [1, 2], [], [0, 2, 1, 2]):
+        with pytest.raises(B.LocksError, match="cu_tokens"):
+            T.tree_mask([-1, -1], cu, device="cpu")
