@@ -1,71 +1,740 @@
 // Attention of several new tokens of a sequence over the paged cache:
 //   o_i = sum_{t seen by i} softmax_t(q_i . k_t / sqrt d) v_t.
-// One wave per (new token, query head), a token after the other, two dimensions a lane, with
-// the running maximum and sum of an online softmax in fp32.
+//
+// The new tokens' query heads of one KV head are the rows of a matrix product (row
+// r = i G + g), in tiles of 32 RW rows; a block goes through units of 32 NB TW tokens, its
+// waves RW by rows and TW by tokens.  Per 32 rows and 32 tokens a wave computes
+//   S^T = K Q^T   (M = token, N = row), whose result has a row per lane column, so that the
+//                 online softmax (running maximum and sum, fp32) needs one lane swap,
+//   O^T += V^T P  (M = dimension, N = row, K = token), with P exactly as S^T left it.
+// Keys and values pass through registers into LDS, the next unit's while one is computed;
+// their 16-byte pieces are permuted by the token, so that neither the key reads nor the
+// transposed value reads meet on a bank.
+//
+// All (sequence, KV head, tile) items' units, in order, are cut into equal shares, one a
+// block (every block derives the cut from the lengths), so ragged batches and long lists
+// fill the chip; an item within a share writes its output, others leave partials (o, max,
+// sum), which merge_kernel combines in order.
+//
+// What a row does not see is masked by one 32-bit window per row and 32 tokens, the
+// ancestors' bits shifted to the tile; only units that hold new tokens look at it.
 #include "tokens_internal.h"
 
 namespace locks {
 namespace {
 
-template <typename TQ, typename TK>
-__global__ __launch_bounds__(256) void tree_simple_kernel(DraftArgs a, const TK* __restrict__ k_cache,
-                                                          const TK* __restrict__ v_cache,
-                                                          void* __restrict__ out, int out_bf16,
-                                                          float* __restrict__ out_lse) {
-  const int Hq = a.H * a.G, lane = threadIdx.x & 63;
-  const long unit = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int row = (int)(unit / Hq), hq = (int)(unit % Hq), h = hq / a.G;
-  if (row >= a.n_tokens) return;
-  int s = 0;
-  while (s < a.S && draft_rows(a, s).y <= row) ++s;
-  if (s == a.S || draft_rows(a, s).x > row) return;  // padding
-  const int2 rows = draft_rows(a, s);
-  const int i = row - rows.x, L = draft_len(a, s), first = L - (rows.y - rows.x);
-  const TQ* q = static_cast<const TQ*>(a.q) + (long)row * a.q_stride + hq * kDim + 2 * lane;
-  const float q0 = load_elem(q, 0), q1 = load_elem(q, 1), scale = 1.0f / sqrtf((float)kDim);
-  float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (int t = 0; t < L; ++t) {
-    if (!draft_sees(a, row, i, t, first)) continue;
-    int blk = a.page_table[(long)s * a.max_pages + t / a.pgsz];
-    if ((unsigned)blk >= (unsigned)a.num_blocks) blk = 0;
-    const long at = (((long)blk * a.H + h) * a.pgsz + t % a.pgsz) * kDim + 2 * lane;
-    const float z = warp_sum(fmaf(q0, load_elem(k_cache + at, 0), q1 * load_elem(k_cache + at, 1))) * scale;
-    const float mx = fmaxf(m, z);
-    const float sc = m == -INFINITY ? 0.0f : expf(m - mx), w = z == -INFINITY ? 0.0f : expf(z - mx);
-    l = fmaf(l, sc, w);
-    o0 = fmaf(o0, sc, w * load_elem(v_cache + at, 0));
-    o1 = fmaf(o1, sc, w * load_elem(v_cache + at, 1));
-    m = mx;
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+constexpr int kTiles = 512;        // row tiles of a launch whose items are cut into shares
+constexpr int kTreeBlocks = 512;   // two per compute unit
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct TreeArgs {
+  DraftArgs d;
+  const void *k, *v;
+  void* out;
+  float* lse;
+  float* po;       // [2 blocks][rows][128]
+  float* pml;      // [2 blocks][rows][2]
+  int32_t* rec;    // [blocks][8]: the item that begins in a block and ends in a later one
+  int tiles;       // most row tiles there can be
+  int split, out_bf16;
+};
+
+__device__ __forceinline__ float swap_max(float v) {
+  auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float swap_sum(float v) {
+  auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+__device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// Exclusive prefix sum of one value a thread over a 256-thread block; total in `sum`.
+__device__ __forceinline__ long scan256(long v, long* lds, long& sum) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  long x = v;
+  for (int o = 1; o < 64; o <<= 1) {
+    const long y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-  const long to = ((long)row * Hq + hq) * kDim + 2 * lane;
-  if (out_bf16) {
-    static_cast<__bf16*>(out)[to] = (__bf16)(o0 * inv);
-    static_cast<__bf16*>(out)[to + 1] = (__bf16)(o1 * inv);
+  __syncthreads();
+  if (lane == 63) lds[wave] = x;
+  __syncthreads();
+  long before = 0;
+  sum = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += lds[w];
+    sum += lds[w];
+  }
+  return before + x - v;
+}
+
+// Position of a 16-byte piece within a token's row in LDS: an exclusive or with this.  Any 8
+// tokens in a row differ in the lower three bits (key reads), any 4 in bits 1 and 2 (the
+// transposed reads of two pieces each).
+__device__ __forceinline__ int piece_xor(int tok) { return ((tok & 3) << 1) | ((tok >> 2) & 1) | (tok & 8); }
+
+// kF32: products in fp32 (32x32x2 MFMA), else bf16 (32x32x16), the weights in NT terms.
+template <bool kF32, typename TQ, typename TK, int NT, int RW, int TW, int NB>
+struct Tree {
+  static constexpr int kRows = 32 * RW, kGroup = 32 * NB, kUnit = kGroup * TW;
+  static constexpr int kThreads = 64 * RW;                 // of a group of waves with the same tokens
+  static constexpr int kPieces = kF32 ? 32 : 16;           // of a row: 4 floats, or 8 bf16
+  static constexpr int kLoads = kGroup * kPieces / kThreads;
+  static constexpr int kTokStep = kThreads / kPieces;      // tokens between a thread's loads
+  static constexpr int kKRow = kF32 ? 132 * 4 : 256, kVRow = kF32 ? 512 : 256;  // bytes
+  static constexpr int kTile = kGroup * (kKRow + kVRow);   // of one group's unit
+  static constexpr int kBufs = RW > 1 ? 2 : 1;
+  static constexpr int kJoin = TW > 1 ? TW * kRows * 132 * 4 : 0;
+  static constexpr int kLds = kTile * TW * kBufs > kJoin ? kTile * TW * kBufs : kJoin;
+};
+
+struct Segment {
+  int s, h, tile;
+  int u0, count, units;
+};
+
+template <bool kF32, typename TQ, typename TK, int NT, int RW, int TW, int NB, int kWaves>
+__global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
+  using C = Tree<kF32, TQ, TK, NT, RW, TW, NB>;
+  static_assert(RW * TW == 4, "four waves");
+  __shared__ __align__(16) unsigned char lds[C::kLds];
+  __shared__ long s_units[kTiles + 1], s_sum[4];
+  __shared__ int s_first[kTiles + 1];
+  __shared__ float s_m[TW][C::kRows], s_l[TW][C::kRows];
+  const DraftArgs& d = a.d;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = wave % RW, wt = wave / RW;
+  const int col = lane & 31, half = lane >> 5;
+  const int Hq = d.H * d.G;
+  const float zs = kLog2e / sqrtf((float)kDim);
+
+  auto tiles_of = [&](int n) { return (int)(((long)n * d.G + C::kRows - 1) / C::kRows); };
+  // tokens that a tile's rows can see
+  auto reach = [&](int n, int L, int tile) {
+    if (d.mask) return L;
+    const long last = min((long)n, ((long)(tile + 1) * C::kRows - 1) / d.G + 1);
+    return (int)min((long)L, L - n + last);
+  };
+  auto units_of = [&](int n, int L, int tile) { return max(1, (reach(n, L, tile) + C::kUnit - 1) / C::kUnit); };
+
+  // ---- one segment: units [u0, u0 + count) of an item
+  auto process = [&](const Segment& g, long lb) {
+    const int s = g.s, h = g.h;
+    const int2 rows = draft_rows(d, s);
+    const int n = rows.y - rows.x, L = draft_len(d, s), first = L - n;
+    const int r = g.tile * C::kRows + wr * 32 + col;
+    const bool live = r < n * d.G;
+    const int i = live ? r / d.G : 0, hg = h * d.G + (live ? r % d.G : 0);
+    const long row = rows.x + i;
+    const uint32_t* mask = d.mask ? d.mask + row * d.words : nullptr;
+
+    // this lane's query: dimensions 16 ks + 8 half + 0 .. 7, or 8 u + 4 half + 0 .. 3
+    bf8 qb[kF32 ? 1 : 8];
+    float qf[kF32 ? 64 : 1];
+    {
+      const TQ* q = static_cast<const TQ*>(d.q) + row * d.q_stride + hg * kDim;
+      if constexpr (kF32) {
+#pragma unroll
+        for (int u = 0; u < 16; ++u)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) qf[4 * u + j] = live ? load_elem(q, 8 * u + 4 * half + j) : 0.0f;
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          const u4 w = *reinterpret_cast<const u4*>(q + 16 * ks + 8 * half), none = {};
+          qb[ks] = __builtin_bit_cast(bf8, live ? w : none);
+        }
+      }
+    }
+
+    // ---- staging
+    using Raw = typename std::conditional<kF32 && sizeof(TK) == 2, u2, u4>::type;
+    Raw kr[C::kLoads], vr[C::kLoads];
+    int blk[2 * NB];
+    const int gt = wr * 64 + lane, piece = gt % C::kPieces, tok_in = gt / C::kPieces;
+    const int32_t* table = d.page_table + (long)s * d.max_pages;
+    const int lgP = d.pgsz == 64 ? 6 : d.pgsz == 32 ? 5 : 4;
+    auto look_up = [&](int u) {
+#pragma unroll
+      for (int b = 0; b < 2 * NB; ++b) {
+        const int t = min(u * C::kUnit + wt * C::kGroup + 16 * b, L - 1);
+        const int x = table[t >> lgP];
+        blk[b] = (unsigned)x < (unsigned)d.num_blocks ? x : 0;
+      }
+    };
+    auto load = [&](int u) {
+#pragma unroll
+      for (int j = 0; j < C::kLoads; ++j) {
+        constexpr int kElems = kF32 ? 4 : 8;
+        const int t = min(u * C::kUnit + wt * C::kGroup + j * C::kTokStep + tok_in, L - 1);
+        const long base = ((long)blk[j * C::kTokStep / 16] * d.H + h) * d.pgsz * kDim;
+        const int at = (t & (d.pgsz - 1)) * kDim + kElems * piece;
+        kr[j] = *reinterpret_cast<const Raw*>(static_cast<const TK*>(a.k) + base + at);
+        vr[j] = *reinterpret_cast<const Raw*>(static_cast<const TK*>(a.v) + base + at);
+      }
+    };
+    auto tile_at = [&](int u) { return lds + (wt * C::kBufs + (C::kBufs > 1 ? u & 1 : 0)) * C::kTile; };
+    // writes the loaded unit; returns whether this thread's values are all finite (where asked)
+    auto store = [&](int u, bool check) -> bool {
+      unsigned char* kt = tile_at(u);
+      unsigned char* vt = kt + C::kGroup * C::kKRow;
+      bool ok = true;
+#pragma unroll
+      for (int j = 0; j < C::kLoads; ++j) {
+        const int tok = j * C::kTokStep + tok_in;
+        if constexpr (kF32) {
+          float4 kf, vf;
+          if constexpr (sizeof(TK) == 2) {
+            kf = make_float4(__uint_as_float(kr[j].x << 16), __uint_as_float(kr[j].x & 0xffff0000u),
+                             __uint_as_float(kr[j].y << 16), __uint_as_float(kr[j].y & 0xffff0000u));
+            vf = make_float4(__uint_as_float(vr[j].x << 16), __uint_as_float(vr[j].x & 0xffff0000u),
+                             __uint_as_float(vr[j].y << 16), __uint_as_float(vr[j].y & 0xffff0000u));
+          } else {
+            kf = __builtin_bit_cast(float4, kr[j]);
+            vf = __builtin_bit_cast(float4, vr[j]);
+          }
+          if (check) ok = ok && finite(vf.x) && finite(vf.y) && finite(vf.z) && finite(vf.w);
+          *reinterpret_cast<float4*>(kt + tok * C::kKRow + 16 * piece) = kf;
+          *reinterpret_cast<float4*>(vt + tok * C::kVRow + 16 * piece) = vf;
+        } else {
+          const int at = 16 * (piece ^ piece_xor(tok));
+          if (check) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              ok = ok && (vr[j][e] & 0x7f80u) != 0x7f80u && (vr[j][e] & 0x7f800000u) != 0x7f800000u;
+          }
+          *reinterpret_cast<u4*>(kt + tok * C::kKRow + at) = kr[j];
+          *reinterpret_cast<u4*>(vt + tok * C::kVRow + at) = vr[j];
+        }
+      }
+      return ok;
+    };
+
+    // ---- which of the 32 tokens from tb on this lane's row sees
+    auto window = [&](int tb) -> uint32_t {
+      const int e = L - tb, j0 = tb - first;
+      if (e <= 0) return 0u;
+      const uint32_t lim = e >= 32 ? ~0u : (1u << e) - 1u;
+      if (j0 <= -32) return lim;
+      uint32_t seen = j0 < 0 ? (1u << -j0) - 1u : 0u;
+      if (mask) {
+        const int w = j0 >> 5, sh = j0 & 31;
+        const uint32_t lo = (unsigned)w < (unsigned)d.words ? mask[w] : 0u;
+        const uint32_t hi = (unsigned)(w + 1) < (unsigned)d.words ? mask[w + 1] : 0u;
+        seen |= sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
+      } else {
+        const int c = i - j0;
+        if (c >= 0) seen |= c >= 31 ? ~0u : (2u << c) - 1u;
+      }
+      return seen & lim;
+    };
+
+    float m = -INFINITY, l = 0.0f;
+    f16v o[4];
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
+
+    if (L > 0) {
+      __syncthreads();  // (the tiles' last readers: the segment before)
+      look_up(g.u0);
+      load(g.u0);
+      if (g.count > 1) look_up(g.u0 + 1);
+      for (int u = g.u0; u < g.u0 + g.count; ++u) {
+        const int t_unit = u * C::kUnit, t0 = t_unit + wt * C::kGroup;
+        const bool tail = t_unit + C::kUnit > first;
+        // (a wave that owns its tile needs no barrier, its LDS accesses being in order; the
+        // fences keep the compiler's order)
+        if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        bool bad = !store(u, tail);
+        if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (u + 1 < g.u0 + g.count) {
+          load(u + 1);
+          if (u + 2 < g.u0 + g.count) look_up(u + 2);
+        }
+        if constexpr (RW > 1) {
+          if (tail) bad = __syncthreads_or(bad);
+          else __syncthreads();
+        } else {
+          bad = tail && __any(bad);
+        }
+        unsigned char* kt = tile_at(u);
+        unsigned char* vt = kt + C::kGroup * C::kKRow;
+
+        // ---- logits
+        f16v z[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[b][e] = 0.0f;
+          const unsigned char* kp = kt + (32 * b + col) * C::kKRow;
+          if constexpr (kF32) {
+#pragma unroll
+            for (int u8 = 0; u8 < 16; ++u8) {
+              const float4 x = *reinterpret_cast<const float4*>(kp + 32 * u8 + 16 * half);
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, qf[4 * u8], z[b], 0, 0, 0);
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, qf[4 * u8 + 1], z[b], 0, 0, 0);
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, qf[4 * u8 + 2], z[b], 0, 0, 0);
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, qf[4 * u8 + 3], z[b], 0, 0, 0);
+            }
+          } else {
+            const int px = piece_xor(col) ^ half;
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) {
+              const u4 x = *reinterpret_cast<const u4*>(kp + 16 * (px ^ (2 * ks)));
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, x), qb[ks], z[b], 0, 0, 0);
+            }
+          }
+        }
+        // ---- masks (element e of a lane: token 8 (e / 4) + 4 half + e % 4)
+        if (tail) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const uint32_t seen = window(t0 + 32 * b) >> (4 * half);
+            if (!__all(seen == (~0u >> (4 * half)))) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                z[b][e] = seen >> (8 * (e / 4) + e % 4) & 1u ? z[b][e] : -INFINITY;
+            }
+          }
+        }
+        // ---- online softmax; the maximum follows only where a row grows by more than 2^8
+        float big = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) big = fmaxf(big, z[b][e]);
+        big = swap_max(big) * zs;
+        if (__any(big > m + 8.0f)) {
+          const float mn = fmaxf(m, big);
+          const float sc = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
+          m = mn;
+          l *= sc;
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[dt][e] *= sc;
+        }
+        const float ms = m == -INFINITY ? 0.0f : m;
+        float ps = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            z[b][e] = __builtin_amdgcn_exp2f(fmaf(z[b][e], zs, -ms));
+            ps += z[b][e];
+          }
+        l += ps;
+
+        // ---- values that are not finite, among the new tokens: 0 times them would reach rows
+        // that do not see them, so they are added by hand and leave the tile
+        auto value = [&](int tok, int dim) -> float {
+          if constexpr (kF32) return *reinterpret_cast<const float*>(vt + tok * C::kVRow + 4 * dim);
+          else
+            return bf16_bits_to_f32(*reinterpret_cast<const uint16_t*>(
+                vt + tok * C::kVRow + 16 * ((dim >> 3) ^ piece_xor(tok)) + 2 * (dim & 7)));
+        };
+        auto row_bad = [&](int tok) { return __any(!finite(value(tok, 2 * lane)) || !finite(value(tok, 2 * lane + 1))); };
+        if (bad) {
+          if constexpr (RW > 1) __syncthreads();  // (the keys' last readers)
+          float* w = reinterpret_cast<float*>(kt) + wr * 1024;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[(8 * (e / 4) + 4 * half + e % 4) * 32 + col] = z[b][e];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int t = 0; t < 32; ++t) {
+              if (!row_bad(32 * b + t)) continue;
+              const float p = w[t * 32 + col];
+#pragma unroll
+              for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const float x = value(32 * b + t, 32 * dt + 8 * (e / 4) + 4 * half + e % 4);
+                  o[dt][e] += p != 0.0f ? p * x : 0.0f;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          }
+          if constexpr (RW > 1) __syncthreads();
+          for (int t = wr; t < C::kGroup; t += RW)
+            if (row_bad(t)) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const int dim = 2 * lane + e;
+                if constexpr (kF32) *reinterpret_cast<float*>(vt + t * C::kVRow + 4 * dim) = 0.0f;
+                else
+                  *reinterpret_cast<uint16_t*>(vt + t * C::kVRow + 16 * ((dim >> 3) ^ piece_xor(t)) + 2 * (dim & 7)) = 0;
+              }
+            }
+          if constexpr (RW > 1) __syncthreads();
+          else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+
+        // ---- values
+        if constexpr (kF32) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const unsigned char* vp = vt + (32 * b + 8 * (e / 4) + 4 * half + e % 4) * C::kVRow + 4 * col;
+#pragma unroll
+              for (int dt = 0; dt < 4; ++dt)
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(vp + 128 * dt),
+                                                             z[b][e], o[dt], 0, 0, 0);
+            }
+        } else {
+          // 16 lanes read 4 tokens x 16 dimensions transposed: lane c gets dimension c of each
+          const int c = lane & 15, tv = 4 * half + (c >> 2);
+          const int p0 = (2 * ((lane >> 4) & 1) + ((c & 3) >> 1)) ^ piece_xor(tv);
+          const unsigned char* vp = vt + tv * C::kVRow + 8 * (c & 1);
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              bf8 p[NT];
+              float rest[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) rest[e] = z[b][8 * t + e];
+#pragma unroll
+              for (int k = 0; k < NT; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  p[k][e] = (__bf16)rest[e];
+                  rest[e] -= (float)p[k][e];
+                }
+#pragma unroll
+              for (int dt = 0; dt < 4; ++dt) {
+                using LdsS4 = __attribute__((address_space(3))) s4;
+                const unsigned char* vb = vp + (32 * b + 16 * t) * C::kVRow;
+                const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)(vb + 16 * (p0 ^ (4 * dt))));
+                const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (LdsS4*)(vb + 8 * C::kVRow + 16 * (p0 ^ (4 * dt) ^ 8)));
+                const bf8 x = __builtin_bit_cast(bf8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int k = 0; k < NT; ++k)
+                  o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[k], o[dt], 0, 0, 0);
+              }
+            }
+        }
+      }
+    }
+
+    // ---- the item's output, or a partial
+    l = swap_sum(l);
+    const bool whole = g.count == g.units;
+    const long slot = g.u0 > 0 ? 2 * lb : 2 * lb + 1;
+    auto emit = [&](int rr, int dim, float x0, float x1, float x2, float x3, float mm, float ll, bool stats) {
+      // four dimensions of row rr of the tile
+      const int rg = g.tile * C::kRows + rr;
+      if (rg >= n * d.G) return;
+      if (whole) {
+        const long to = (long)(rows.x + rg / d.G) * Hq + h * d.G + rg % d.G;
+        const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;
+        if (a.out_bf16) {
+          typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
+          const bf4 y = {(__bf16)(x0 * inv), (__bf16)(x1 * inv), (__bf16)(x2 * inv), (__bf16)(x3 * inv)};
+          *reinterpret_cast<bf4*>(static_cast<__bf16*>(a.out) + to * kDim + dim) = y;
+        } else {
+          *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to * kDim + dim) =
+              make_float4(x0 * inv, x1 * inv, x2 * inv, x3 * inv);
+        }
+        if (stats && a.lse) a.lse[to] = ll == 0.0f ? -INFINITY : kLn2 * mm + logf(ll);
+      } else {
+        *reinterpret_cast<float4*>(a.po + (slot * C::kRows + rr) * kDim + dim) = make_float4(x0, x1, x2, x3);
+        if (stats) *reinterpret_cast<float2*>(a.pml + (slot * C::kRows + rr) * 2) = make_float2(mm, ll);
+      }
+    };
+    if constexpr (TW == 1) {
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          emit(wr * 32 + col, 32 * dt + 2 * e + 4 * half, o[dt][e], o[dt][e + 1], o[dt][e + 2], o[dt][e + 3], m, l,
+               dt == 0 && e == 0 && half == 0);
+    } else {
+      if (half == 0) {
+        s_m[wt][wr * 32 + col] = m;
+        s_l[wt][wr * 32 + col] = l;
+      }
+      __syncthreads();
+      float mx = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < TW; ++w) mx = fmaxf(mx, s_m[w][wr * 32 + col]);
+      const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mx);
+      float* to = reinterpret_cast<float*>(lds) + (wt * C::kRows + wr * 32 + col) * 132;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<float4*>(to + 32 * dt + 2 * e + 4 * half) =
+              make_float4(o[dt][e] * f, o[dt][e + 1] * f, o[dt][e + 2] * f, o[dt][e + 3] * f);
+      __syncthreads();
+      for (int e = tid; e < C::kRows * 32; e += 256) {
+        const int rr = e >> 5, dim = 4 * (e & 31);
+        float M = -INFINITY, ll = 0.0f;
+        float4 x = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < TW; ++w) M = fmaxf(M, s_m[w][rr]);
+#pragma unroll
+        for (int w = 0; w < TW; ++w) {
+          const float mw = s_m[w][rr];
+          ll += mw == -INFINITY ? 0.0f : s_l[w][rr] * __builtin_amdgcn_exp2f(mw - M);
+          const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<float*>(lds) + (w * C::kRows + rr) * 132 + dim);
+          x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+        }
+        emit(rr, dim, x.x, x.y, x.z, x.w, M, ll, dim == 0);
+      }
+      __syncthreads();
+    }
+    if (!whole && g.u0 == 0 && tid == 0) {
+      int32_t* rec = a.rec + 8 * lb;
+      rec[0] = 1;
+      rec[1] = rows.x;
+      rec[2] = min(n * d.G - g.tile * C::kRows, C::kRows);
+      rec[3] = g.tile * C::kRows;
+      rec[4] = h;
+      rec[5] = g.units - g.count;  // units left to the next blocks
+    }
+  };
+
+  // ---- what this block computes
+  long x = 0, end = 1, lb = 0;
+  Segment g{};
+  if (!a.split) {
+    // an item a block: tile slots, s + cu[s] G / rows on for sequence s, some of them empty
+    const int slot = blockIdx.x / d.H, h = blockIdx.x % d.H;
+    auto base = [&](int s) { return s + (int)((long)draft_rows(d, s).x * d.G / C::kRows); };
+    int lo = 0, hi = d.S;  // the last sequence whose slots begin at `slot` or before
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 63) / 64, s = lo + lane * step;
+      const unsigned long long ok = __ballot(s < hi && base(s) <= slot);
+      const int k = max(0, (int)__popcll(ok) - 1);
+      lo += k * step;
+      hi = min(hi, lo + step);
+    }
+    const int2 rows = draft_rows(d, lo);
+    const int n = rows.y - rows.x, tile = slot - base(lo);
+    if (tile < 0 || tile >= tiles_of(n)) return;
+    const int units = units_of(n, draft_len(d, lo), tile);
+    g = Segment{lo, h, tile, 0, units, units};
   } else {
-    static_cast<float*>(out)[to] = o0 * inv;
-    static_cast<float*>(out)[to + 1] = o1 * inv;
+    // the cut: tiles before each sequence, units before each tile
+    constexpr int kPer = kTiles / 256;
+    long before[kPer], sum = 0, v = 0, total;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int s = tid * kPer + e;
+      before[e] = v;
+      if (s < d.S) {
+        const int2 rows = draft_rows(d, s);
+        v += tiles_of(rows.y - rows.x);
+      }
+    }
+    const long at = scan256(v, s_sum, total);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int s = tid * kPer + e;
+      if (s < d.S) s_first[s] = (int)(at + before[e]);
+    }
+    if (tid == 0) s_first[d.S] = (int)total;
+    __syncthreads();
+    const int T = min((int)total, kTiles);
+    v = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int t = tid * kPer + e;
+      before[e] = v;
+      if (t < T) {
+        int lo = 0, hi = d.S;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (s_first[mid] <= t) lo = mid;
+          else hi = mid;
+        }
+        const int2 rows = draft_rows(d, lo);
+        v += units_of(rows.y - rows.x, draft_len(d, lo), t - s_first[lo]);
+      }
+    }
+    const long ut = scan256(v, s_sum, sum);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) s_units[tid * kPer + e] = ut + before[e];
+    if (tid == 0) s_units[kTiles] = sum;
+    __syncthreads();
+    const long all = s_units[kTiles] * d.H, share = (all + gridDim.x - 1) / gridDim.x;
+    // (blocks that share an item or its keys run on one XCD)
+    lb = (gridDim.x & 7) ? blockIdx.x : (long)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    x = lb * share;
+    end = min(all, x + share);
+    if (tid == 0) {
+      a.rec[8 * lb] = 0;
+      a.rec[8 * lb + 6] = (int)min(share, (long)0x7fffffff);
+    }
   }
-  if (out_lse && lane == 0) out_lse[(long)row * Hq + hq] = l > 0.0f ? m + logf(l) : -INFINITY;
+  while (x < end) {
+    if (a.split) {
+      int lo = 0, hi = d.S;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (s_units[s_first[mid]] * d.H <= x) lo = mid;
+        else hi = mid;
+      }
+      const int t0 = s_first[lo], t1 = s_first[lo + 1];
+      const long first = s_units[t0], per = s_units[t1] - first, in = x - first * d.H;
+      const int h = (int)(in / per);
+      const long rest = in % per + first;
+      int tl = t0, th = t1;
+      while (th - tl > 1) {
+        const int mid = (tl + th) / 2;
+        if (s_units[mid] <= rest) tl = mid;
+        else th = mid;
+      }
+      const int units = (int)(s_units[tl + 1] - s_units[tl]), u0 = (int)(rest - s_units[tl]);
+      const int count = (int)min(end - x, (long)(units - u0));
+      g = Segment{lo, h, tl - t0, u0, count, units};
+    }
+    g = Segment{__builtin_amdgcn_readfirstlane(g.s), __builtin_amdgcn_readfirstlane(g.h),
+                __builtin_amdgcn_readfirstlane(g.tile), __builtin_amdgcn_readfirstlane(g.u0),
+                __builtin_amdgcn_readfirstlane(g.count), __builtin_amdgcn_readfirstlane(g.units)};
+    process(g, lb);
+    x += g.count;
+    if (!a.split) break;
+  }
+}
+
+// The items that end in a later block than they begin in; grid (blocks, rows / 16), a wave
+// four rows.  Block lb's own partial is in slot 2 lb + 1, the later ones' in 2 (lb + 1), ...
+__global__ __launch_bounds__(256) void tree_merge_kernel(const int32_t* __restrict__ recs,
+                                                         const float* __restrict__ po,
+                                                         const float* __restrict__ pml, int tile_rows, int G,
+                                                         int Hq, void* __restrict__ out, int out_bf16,
+                                                         float* __restrict__ out_lse) {
+  const int lb = blockIdx.x, lane = threadIdx.x & 63;
+  const int32_t* rec = recs + 8 * lb;
+  if (!rec[0]) return;
+  const int count = rec[2], share = rec[6], parts = 1 + (rec[5] + share - 1) / share;
+  auto slot = [&](int p) { return p ? 2L * (lb + p) : 2L * lb + 1; };
+  for (int e = 0; e < 4; ++e) {
+    const int rr = blockIdx.y * 16 + (threadIdx.x >> 6) * 4 + e;
+    if (rr >= count) return;
+    float mx = -INFINITY;
+    for (int p0 = 0; p0 < parts; p0 += 64)
+      if (p0 + lane < parts) mx = fmaxf(mx, pml[(slot(p0 + lane) * tile_rows + rr) * 2]);
+    mx = warp_max(mx);
+    float x = 0.0f, y = 0.0f, l = 0.0f;
+    for (int p0 = 0; p0 < parts; p0 += 64) {
+      float2 st = make_float2(-INFINITY, 0.0f);
+      if (p0 + lane < parts)
+        st = *reinterpret_cast<const float2*>(pml + (slot(p0 + lane) * tile_rows + rr) * 2);
+      const float w = st.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.x - mx);
+      l += warp_sum(w * st.y);
+      const int np = min(64, parts - p0);
+#pragma unroll 8
+      for (int p = 0; p < np; ++p) {
+        const float2 v = *reinterpret_cast<const float2*>(po + (slot(p0 + p) * tile_rows + rr) * kDim + 2 * lane);
+        const float f = __shfl(w, p, 64);
+        x = fmaf(f, v.x, x);
+        y = fmaf(f, v.y, y);
+      }
+    }
+    const int rg = rec[3] + rr;
+    const long to = (long)(rec[1] + rg / G) * Hq + rec[4] * G + rg % G;
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    if (out_bf16) {
+      typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+      const bf2 v = {(__bf16)(x * inv), (__bf16)(y * inv)};
+      *reinterpret_cast<bf2*>(static_cast<__bf16*>(out) + to * kDim + 2 * lane) = v;
+    } else {
+      *reinterpret_cast<float2*>(static_cast<float*>(out) + to * kDim + 2 * lane) = make_float2(x * inv, y * inv);
+    }
+    if (out_lse && lane == 0) out_lse[to] = l == 0.0f ? -INFINITY : kLn2 * mx + logf(l);
+  }
+}
+
+struct Plan {
+  int rows, unit;      // of a tile, of a unit
+  int blocks, split;
+  long tiles;
+  size_t po, pml;
+};
+
+// Rows of a tile by the average sequence's rows.
+Plan tree_plan(const locks_cfg_t& c, int n_tokens) {
+  const int G = c.num_q_heads / c.num_kv_heads, S = c.num_seqs > 0 ? c.num_seqs : 1;
+  const bool f32 = c.q_dtype != LOCKS_BF16 || c.kv_dtype != LOCKS_BF16;
+  const long rows = ((long)n_tokens * G + S - 1) / S;
+  Plan p{};
+  p.rows = rows <= 32 ? 32 : rows <= 64 && !f32 ? 64 : 128;
+  p.unit = p.rows == 32 ? 128 : f32 ? 32 : 64;
+  p.tiles = S + (long)n_tokens * G / p.rows;
+  p.split = p.tiles <= kTiles;
+  if (p.split) {
+    const long units = ((long)c.max_pages_per_seq * c.page_size + p.unit - 1) / p.unit;
+    const long most = p.tiles * units * c.num_kv_heads;
+    p.blocks = (int)(most < kTreeBlocks ? (most + 7) / 8 * 8 : kTreeBlocks);
+    p.po = (size_t)2 * p.blocks * p.rows * kDim * sizeof(float);
+    p.pml = (size_t)2 * p.blocks * p.rows * 2 * sizeof(float);
+  }
+  return p;
+}
+
+template <bool kF32, typename TQ, typename TK, int NT, int RW, int TW, int NB, int kWaves>
+void launch_one(const TreeArgs& a, const Plan& p, hipStream_t st) {
+  const unsigned grid = p.split ? (unsigned)p.blocks : (unsigned)(p.tiles * a.d.H);
+  hipLaunchKernelGGL((tree_kernel<kF32, TQ, TK, NT, RW, TW, NB, kWaves>), dim3(grid), dim3(256), 0, st, a);
+}
+
+template <typename TQ, typename TK>
+void launch_f32(const TreeArgs& a, const Plan& p, hipStream_t st) {
+  if (p.rows == 32) launch_one<true, TQ, TK, 1, 1, 4, 1, 1>(a, p, st);
+  else launch_one<true, TQ, TK, 1, 4, 1, 1, 2>(a, p, st);
+}
+template <int NT>
+void launch_bf16(const TreeArgs& a, const Plan& p, hipStream_t st) {
+  if (p.rows == 32) launch_one<false, uint16_t, uint16_t, NT, 1, 4, 1, 2>(a, p, st);
+  else if (p.rows == 64) launch_one<false, uint16_t, uint16_t, NT, 2, 2, 1, 2>(a, p, st);
+  else launch_one<false, uint16_t, uint16_t, NT, 4, 1, 2, 2>(a, p, st);
 }
 
 }  // namespace
 
-size_t tree_scratch_bytes(const locks_cfg_t&, int) { return 0; }
+// (what no smaller number of tokens needs more than: a workspace serves up to n_tokens)
+size_t tree_scratch_bytes(const locks_cfg_t& c, int n_tokens) {
+  return (size_t)kTreeBlocks * (2 * tree_plan(c, n_tokens).rows * (kDim + 2) * sizeof(float) + 8 * sizeof(int32_t));
+}
 
-hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& a, const void* k_cache,
+hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& d, const void* k_cache,
                               const void* v_cache, void* out, bool out_bf16, float* out_lse,
-                              void*, hipStream_t st) {
-  const dim3 grid((unsigned)(((long)a.n_tokens * c.num_q_heads + 3) / 4)), block(256);
-#define TREE(TQ, TK)                                                                             \
-  hipLaunchKernelGGL((tree_simple_kernel<TQ, TK>), grid, block, 0, st, a,                        \
-                     static_cast<const TK*>(k_cache), static_cast<const TK*>(v_cache), out,      \
-                     out_bf16 ? 1 : 0, out_lse)
-  if (c.q_dtype == LOCKS_BF16 && c.kv_dtype == LOCKS_BF16) TREE(uint16_t, uint16_t);
-  else if (c.q_dtype == LOCKS_BF16) TREE(uint16_t, float);
-  else if (c.kv_dtype == LOCKS_BF16) TREE(float, uint16_t);
-  else TREE(float, float);
-#undef TREE
+                              void* scratch, hipStream_t st) {
+  const Plan p = tree_plan(c, d.n_tokens);
+  char* w = static_cast<char*>(scratch);
+  const TreeArgs a{d, k_cache, v_cache, out, out_lse, reinterpret_cast<float*>(w),
+                   reinterpret_cast<float*>(w + p.po), reinterpret_cast<int32_t*>(w + p.po + p.pml),
+                   (int)p.tiles, p.split, out_bf16 ? 1 : 0};
+  if (c.q_dtype == LOCKS_BF16 && c.kv_dtype == LOCKS_BF16) {
+    if (out_bf16) launch_bf16<2>(a, p, st);
+    else launch_bf16<3>(a, p, st);
+  } else if (c.q_dtype == LOCKS_BF16) {
+    launch_f32<uint16_t, float>(a, p, st);
+  } else if (c.kv_dtype == LOCKS_BF16) {
+    launch_f32<float, uint16_t>(a, p, st);
+  } else {
+    launch_f32<float, float>(a, p, st);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.split) return e;
+  hipLaunchKernelGGL(tree_merge_kernel, dim3(p.blocks, p.rows / 16), dim3(256), 0, st, a.rec, a.po, a.pml, p.rows,
+                     d.G, d.H * d.G, out, a.out_bf16, out_lse);
   return hipGetLastError();
 }
 
