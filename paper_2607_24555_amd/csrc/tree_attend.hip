@@ -91,7 +91,10 @@ struct Tree {
   static constexpr int kLoads = kGroup * kPieces / kThreads;
   static constexpr int kTokStep = kThreads / kPieces;      // tokens between a thread's loads
   static constexpr int kKRow = kF32 ? 132 * 4 : 256, kVRow = kF32 ? 512 : 256;  // bytes
-  static constexpr int kTile = kGroup * (kKRow + kVRow);   // of one group's unit
+  // a wave of its own reads its keys from memory as the product takes them
+  static constexpr bool kDirect = !kF32 && RW == 1;
+  static constexpr int kKeys = kDirect ? 4096 : kGroup * kKRow;  // (4 KB of scratch at least)
+  static constexpr int kTile = kKeys + kGroup * kVRow;     // of one group's unit
   static constexpr int kBufs = RW > 1 ? 2 : 1;
   static constexpr int kJoin = TW > 1 ? TW * kRows * 132 * 4 : 0;
   static constexpr int kLds = kTile * TW * kBufs > kJoin ? kTile * TW * kBufs : kJoin;
@@ -118,21 +121,27 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
   const float zs = kLog2e / sqrtf((float)kDim);
 
   auto tiles_of = [&](int n) { return (int)(((long)n * d.G + C::kRows - 1) / C::kRows); };
+  // rows of a sequence's tiles, in whole 32s and as even as they go
+  auto tile_rows = [&](int n) {
+    const int tiles = tiles_of(n), b = (int)(((long)n * d.G + 31) / 32);
+    return tiles > 1 ? 32 * ((b + tiles - 1) / tiles) : C::kRows;
+  };
   // tokens that a tile's rows can see
   auto reach = [&](int n, int L, int tile) {
     if (d.mask) return L;
-    const long last = min((long)n, ((long)(tile + 1) * C::kRows - 1) / d.G + 1);
+    const long last = min((long)n, ((long)(tile + 1) * tile_rows(n) - 1) / d.G + 1);
     return (int)min((long)L, L - n + last);
   };
   auto units_of = [&](int n, int L, int tile) { return max(1, (reach(n, L, tile) + C::kUnit - 1) / C::kUnit); };
 
   // ---- one segment: units [u0, u0 + count) of an item
-  auto process = [&](const Segment& g, long lb) {
+  auto process = [&](const Segment& g, long lb, long share) {
     const int s = g.s, h = g.h;
     const int2 rows = draft_rows(d, s);
     const int n = rows.y - rows.x, L = draft_len(d, s), first = L - n;
-    const int r = g.tile * C::kRows + wr * 32 + col;
-    const bool live = r < n * d.G;
+    const int tr = tile_rows(n), r0 = g.tile * tr, count_rows = min(n * d.G - r0, tr);
+    const int r = r0 + wr * 32 + col;
+    const bool live = wr * 32 + col < count_rows, busy = wr * 32 < count_rows;
     const int i = live ? r / d.G : 0, hg = h * d.G + (live ? r % d.G : 0);
     const long row = rows.x + i;
     const uint32_t* mask = d.mask ? d.mask + row * d.words : nullptr;
@@ -159,6 +168,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     // ---- staging
     using Raw = typename std::conditional<kF32 && sizeof(TK) == 2, u2, u4>::type;
     Raw kr[C::kLoads], vr[C::kLoads];
+    static_assert(!C::kDirect || C::kLoads == 8, "a lane's half of a key row");
     int blk[2 * NB];
     const int gt = wr * 64 + lane, piece = gt % C::kPieces, tok_in = gt / C::kPieces;
     const int32_t* table = d.page_table + (long)s * d.max_pages;
@@ -167,26 +177,40 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
 #pragma unroll
       for (int b = 0; b < 2 * NB; ++b) {
         const int t = min(u * C::kUnit + wt * C::kGroup + 16 * b, L - 1);
-        const int x = table[t >> lgP];
-        blk[b] = (unsigned)x < (unsigned)d.num_blocks ? x : 0;
+        blk[b] = table[t >> lgP];
       }
     };
+    long base[2 * NB];  // (the same in every lane)
     auto load = [&](int u) {
+#pragma unroll
+      for (int b = 0; b < 2 * NB; ++b) {
+        const int x = __builtin_amdgcn_readfirstlane(blk[b]);
+        base[b] = ((long)((unsigned)x < (unsigned)d.num_blocks ? x : 0) * d.H + h) * d.pgsz * kDim;
+      }
 #pragma unroll
       for (int j = 0; j < C::kLoads; ++j) {
         constexpr int kElems = kF32 ? 4 : 8;
         const int t = min(u * C::kUnit + wt * C::kGroup + j * C::kTokStep + tok_in, L - 1);
-        const long base = ((long)blk[j * C::kTokStep / 16] * d.H + h) * d.pgsz * kDim;
-        const int at = (t & (d.pgsz - 1)) * kDim + kElems * piece;
-        kr[j] = *reinterpret_cast<const Raw*>(static_cast<const TK*>(a.k) + base + at);
-        vr[j] = *reinterpret_cast<const Raw*>(static_cast<const TK*>(a.v) + base + at);
+        const unsigned at = (t & (d.pgsz - 1)) * kDim + kElems * piece;
+        if constexpr (!C::kDirect)
+          kr[j] = *reinterpret_cast<const Raw*>(static_cast<const TK*>(a.k) + base[j * C::kTokStep / 16] + at);
+        vr[j] = *reinterpret_cast<const Raw*>(static_cast<const TK*>(a.v) + base[j * C::kTokStep / 16] + at);
+      }
+    };
+    // (direct) this lane's half of its token's key, of the unit whose values were loaded last
+    auto load_keys = [&](int u) {
+      if constexpr (C::kDirect) {
+        const int t = min(u * C::kUnit + wt * C::kGroup + col, L - 1);
+        const TK* p = static_cast<const TK*>(a.k) + (col < 16 ? base[0] : base[1]) + (t & (d.pgsz - 1)) * kDim + 8 * half;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const Raw*>(p + 16 * j);
       }
     };
     auto tile_at = [&](int u) { return lds + (wt * C::kBufs + (C::kBufs > 1 ? u & 1 : 0)) * C::kTile; };
     // writes the loaded unit; returns whether this thread's values are all finite (where asked)
     auto store = [&](int u, bool check) -> bool {
       unsigned char* kt = tile_at(u);
-      unsigned char* vt = kt + C::kGroup * C::kKRow;
+      unsigned char* vt = kt + C::kKeys;
       bool ok = true;
 #pragma unroll
       for (int j = 0; j < C::kLoads; ++j) {
@@ -212,7 +236,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
             for (int e = 0; e < 4; ++e)
               ok = ok && (vr[j][e] & 0x7f80u) != 0x7f80u && (vr[j][e] & 0x7f800000u) != 0x7f800000u;
           }
-          *reinterpret_cast<u4*>(kt + tok * C::kKRow + at) = kr[j];
+          if constexpr (!C::kDirect) *reinterpret_cast<u4*>(kt + tok * C::kKRow + at) = kr[j];
           *reinterpret_cast<u4*>(vt + tok * C::kVRow + at) = vr[j];
         }
       }
@@ -249,6 +273,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
       __syncthreads();  // (the tiles' last readers: the segment before)
       look_up(g.u0);
       load(g.u0);
+      load_keys(g.u0);
       if (g.count > 1) look_up(g.u0 + 1);
       for (int u = g.u0; u < g.u0 + g.count; ++u) {
         const int t_unit = u * C::kUnit, t0 = t_unit + wt * C::kGroup;
@@ -268,8 +293,9 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         } else {
           bad = tail && __any(bad);
         }
+        if (!busy && !bad) continue;  // (no rows: the wave only loads)
         unsigned char* kt = tile_at(u);
-        unsigned char* vt = kt + C::kGroup * C::kKRow;
+        unsigned char* vt = kt + C::kKeys;
 
         // ---- logits
         f16v z[NB];
@@ -287,6 +313,11 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
               z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, qf[4 * u8 + 2], z[b], 0, 0, 0);
               z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, qf[4 * u8 + 3], z[b], 0, 0, 0);
             }
+          } else if constexpr (C::kDirect) {
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, kr[ks]), qb[ks], z[b], 0, 0, 0);
+            if (u + 1 < g.u0 + g.count) load_keys(u + 1);
           } else {
             const int px = piece_xor(col) ^ half;
 #pragma unroll
@@ -436,8 +467,8 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     const long slot = g.u0 > 0 ? 2 * lb : 2 * lb + 1;
     auto emit = [&](int rr, int dim, float x0, float x1, float x2, float x3, float mm, float ll, bool stats) {
       // four dimensions of row rr of the tile
-      const int rg = g.tile * C::kRows + rr;
-      if (rg >= n * d.G) return;
+      const int rg = r0 + rr;
+      if (rr >= count_rows) return;
       if (whole) {
         const long to = (long)(rows.x + rg / d.G) * Hq + h * d.G + rg % d.G;
         const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;
@@ -499,17 +530,16 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     }
     if (!whole && g.u0 == 0 && tid == 0) {
       int32_t* rec = a.rec + 8 * lb;
-      rec[0] = 1;
-      rec[1] = rows.x;
-      rec[2] = min(n * d.G - g.tile * C::kRows, C::kRows);
-      rec[3] = g.tile * C::kRows;
+      rec[0] = count_rows;
+      rec[1] = 1 + (int)((g.units - g.count + share - 1) / share);
+      rec[2] = rows.x;
+      rec[3] = r0;
       rec[4] = h;
-      rec[5] = g.units - g.count;  // units left to the next blocks
     }
   };
 
   // ---- what this block computes
-  long x = 0, end = 1, lb = 0;
+  long x = 0, end = 1, lb = 0, share = 1;
   Segment g{};
   if (!a.split) {
     // an item a block: tile slots, s + cu[s] G / rows on for sequence s, some of them empty
@@ -571,15 +601,13 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     for (int e = 0; e < kPer; ++e) s_units[tid * kPer + e] = ut + before[e];
     if (tid == 0) s_units[kTiles] = sum;
     __syncthreads();
-    const long all = s_units[kTiles] * d.H, share = (all + gridDim.x - 1) / gridDim.x;
+    const long all = s_units[kTiles] * d.H;
+    share = (all + gridDim.x - 1) / gridDim.x;
     // (blocks that share an item or its keys run on one XCD)
     lb = (gridDim.x & 7) ? blockIdx.x : (long)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     x = lb * share;
     end = min(all, x + share);
-    if (tid == 0) {
-      a.rec[8 * lb] = 0;
-      a.rec[8 * lb + 6] = (int)min(share, (long)0x7fffffff);
-    }
+    if (tid == 0) a.rec[8 * lb] = 0;
   }
   while (x < end) {
     if (a.split) {
@@ -606,58 +634,122 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     g = Segment{__builtin_amdgcn_readfirstlane(g.s), __builtin_amdgcn_readfirstlane(g.h),
                 __builtin_amdgcn_readfirstlane(g.tile), __builtin_amdgcn_readfirstlane(g.u0),
                 __builtin_amdgcn_readfirstlane(g.count), __builtin_amdgcn_readfirstlane(g.units)};
-    process(g, lb);
+    process(g, lb, share);
     x += g.count;
     if (!a.split) break;
   }
 }
 
-// The items that end in a later block than they begin in; grid (blocks, rows / 16), a wave
-// four rows.  Block lb's own partial is in slot 2 lb + 1, the later ones' in 2 (lb + 1), ...
-__global__ __launch_bounds__(256) void tree_merge_kernel(const int32_t* __restrict__ recs,
+// The items that end in a later block than they begin in (rec: rows, parts, first row of the
+// input, first row of the sequence's, KV head).  All their rows, in order, are cut into equal
+// runs, one a block; 32 lanes have a row's 128 dimensions, and where a block has fewer than 16
+// rows several such groups share a row's parts.  Block lb's own part is in slot 2 lb + 1, the
+// later ones' in 2 (lb + 1), ...  (A wave a row, its loads behind its weights: 10 us instead of
+// 5 for 8 items of 20 rows in 33 parts, 51 instead of 20 for 512 items of 128 rows in two.)
+constexpr int kMergeBlocks = 1024;
+__global__ __launch_bounds__(512) void tree_merge_kernel(const int32_t* __restrict__ recs, int blocks,
                                                          const float* __restrict__ po,
                                                          const float* __restrict__ pml, int tile_rows, int G,
                                                          int Hq, void* __restrict__ out, int out_bf16,
                                                          float* __restrict__ out_lse) {
-  const int lb = blockIdx.x, lane = threadIdx.x & 63;
-  const int32_t* rec = recs + 8 * lb;
-  if (!rec[0]) return;
-  const int count = rec[2], share = rec[6], parts = 1 + (rec[5] + share - 1) / share;
-  auto slot = [&](int p) { return p ? 2L * (lb + p) : 2L * lb + 1; };
-  for (int e = 0; e < 4; ++e) {
-    const int rr = blockIdx.y * 16 + (threadIdx.x >> 6) * 4 + e;
-    if (rr >= count) return;
-    float mx = -INFINITY;
-    for (int p0 = 0; p0 < parts; p0 += 64)
-      if (p0 + lane < parts) mx = fmaxf(mx, pml[(slot(p0 + lane) * tile_rows + rr) * 2]);
-    mx = warp_max(mx);
-    float x = 0.0f, y = 0.0f, l = 0.0f;
-    for (int p0 = 0; p0 < parts; p0 += 64) {
-      float2 st = make_float2(-INFINITY, 0.0f);
-      if (p0 + lane < parts)
-        st = *reinterpret_cast<const float2*>(pml + (slot(p0 + lane) * tile_rows + rr) * 2);
-      const float w = st.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.x - mx);
-      l += warp_sum(w * st.y);
-      const int np = min(64, parts - p0);
-#pragma unroll 8
-      for (int p = 0; p < np; ++p) {
-        const float2 v = *reinterpret_cast<const float2*>(po + (slot(p0 + p) * tile_rows + rr) * kDim + 2 * lane);
-        const float f = __shfl(w, p, 64);
-        x = fmaf(f, v.x, x);
-        y = fmaf(f, v.y, y);
+  __shared__ int s_end[kTreeBlocks], s_wave[8];
+  __shared__ float s_o[16][132], s_l[16];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = tid & 31, grp = tid >> 5;
+  // rows up to each block's item
+  int v = tid < blocks ? recs[8 * tid] : 0;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(v, o, 64);
+    if (lane >= o) v += y;
+  }
+  if (lane == 63) s_wave[tid >> 6] = v;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    if (w < (tid >> 6)) v += s_wave[w];
+    total += s_wave[w];
+  }
+  s_end[tid] = v;
+  __syncthreads();
+  int per = (total + gridDim.x - 1) / gridDim.x;
+  if (per < 16) per = per <= 1 ? 1 : 1 << (32 - __clz(per - 1));
+  const int groups = per < 16 ? 16 / per : 1, part0 = grp % groups;
+  const int row_end = min(total, (int)(blockIdx.x + 1) * per);
+  for (int row = blockIdx.x * per + grp / groups; row - grp / groups < row_end; row += 16 / groups) {
+    const bool live = row < row_end;
+    float4 acc = make_float4(0, 0, 0, 0);
+    float mx = -INFINITY, l = 0.0f;
+    long to = 0;
+    if (live) {
+      int lo = 0, hi = blocks - 1;  // the first block whose rows end behind `row`
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (s_end[mid] > row) hi = mid;
+        else lo = mid + 1;
+      }
+      const int32_t* rec = recs + 8 * lo;
+      const int rows = rec[0], parts = rec[1], rr = row - (s_end[lo] - rows), rg = rec[3] + rr;
+      to = (long)(rec[2] + rg / G) * Hq + rec[4] * G + rg % G;
+      auto slot = [&](int p) { return p ? 2L * (lo + p) : 2L * lo + 1; };
+      for (int p0 = 0; p0 < parts; p0 += 32)
+        if (p0 + l32 < parts) mx = fmaxf(mx, pml[(slot(p0 + l32) * tile_rows + rr) * 2]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+      const int mine = (parts - part0 + groups - 1) / groups;  // parts part0, part0 + groups, ..
+      for (int k0 = 0; k0 < mine; k0 += 32) {
+        float w = 0.0f;
+        if (k0 + l32 < mine) {
+          const float2 st =
+              *reinterpret_cast<const float2*>(pml + (slot(part0 + (k0 + l32) * groups) * tile_rows + rr) * 2);
+          w = st.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.x - mx);
+          l += w * st.y;
+        }
+        const int nk = min(32, mine - k0);
+        for (int k = 0; k < nk; k += 8) {
+          float4 x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            x[e] = *reinterpret_cast<const float4*>(
+                po + (slot(part0 + (k0 + min(k + e, nk - 1)) * groups) * tile_rows + rr) * kDim + 4 * l32);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float f = __shfl(w, min(k + e, 31), 32);
+            if (k + e < nk) {
+              acc.x = fmaf(f, x[e].x, acc.x);
+              acc.y = fmaf(f, x[e].y, acc.y);
+              acc.z = fmaf(f, x[e].z, acc.z);
+              acc.w = fmaf(f, x[e].w, acc.w);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+    }
+    if (groups > 1) {
+      *reinterpret_cast<float4*>(&s_o[grp][4 * l32]) = acc;
+      if (l32 == 0) s_l[grp] = l;
+      __syncthreads();
+      if (part0 == 0) {
+        for (int g = 1; g < groups; ++g) {
+          const float4 x = *reinterpret_cast<const float4*>(&s_o[grp + g][4 * l32]);
+          acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
+          l += s_l[grp + g];
+        }
       }
     }
-    const int rg = rec[3] + rr;
-    const long to = (long)(rec[1] + rg / G) * Hq + rec[4] * G + rg % G;
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-    if (out_bf16) {
-      typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-      const bf2 v = {(__bf16)(x * inv), (__bf16)(y * inv)};
-      *reinterpret_cast<bf2*>(static_cast<__bf16*>(out) + to * kDim + 2 * lane) = v;
-    } else {
-      *reinterpret_cast<float2*>(static_cast<float*>(out) + to * kDim + 2 * lane) = make_float2(x * inv, y * inv);
+    if (live && part0 == 0) {
+      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+      if (out_bf16) {
+        typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
+        const bf4 y = {(__bf16)(acc.x * inv), (__bf16)(acc.y * inv), (__bf16)(acc.z * inv), (__bf16)(acc.w * inv)};
+        *reinterpret_cast<bf4*>(static_cast<__bf16*>(out) + to * kDim + 4 * l32) = y;
+      } else {
+        *reinterpret_cast<float4*>(static_cast<float*>(out) + to * kDim + 4 * l32) =
+            make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+      }
+      if (out_lse && l32 == 0) out_lse[to] = l == 0.0f ? -INFINITY : kLn2 * mx + logf(l);
     }
-    if (out_lse && lane == 0) out_lse[to] = l == 0.0f ? -INFINITY : kLn2 * mx + logf(l);
   }
 }
 
@@ -733,8 +825,9 @@ hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& d, const vo
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.split) return e;
-  hipLaunchKernelGGL(tree_merge_kernel, dim3(p.blocks, p.rows / 16), dim3(256), 0, st, a.rec, a.po, a.pml, p.rows,
-                     d.G, d.H * d.G, out, a.out_bf16, out_lse);
+  const long rows = (long)p.blocks * p.rows;  // at most
+  hipLaunchKernelGGL(tree_merge_kernel, dim3((unsigned)(rows < kMergeBlocks ? rows : kMergeBlocks)), dim3(512), 0, st,
+                     a.rec, p.blocks, a.po, a.pml, p.rows, d.G, d.H * d.G, out, a.out_bf16, out_lse);
   return hipGetLastError();
 }
 
