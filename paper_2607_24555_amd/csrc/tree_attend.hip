@@ -18,6 +18,8 @@
 //
 // What a row does not see is masked by one 32-bit window per row and 32 tokens, the
 // ancestors' bits shifted to the tile; only units that hold new tokens look at it.
+#include <type_traits>
+
 #include "tokens_internal.h"
 
 namespace locks {
@@ -275,9 +277,9 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
       load(g.u0);
       load_keys(g.u0);
       if (g.count > 1) look_up(g.u0 + 1);
-      for (int u = g.u0; u < g.u0 + g.count; ++u) {
-        const int t_unit = u * C::kUnit, t0 = t_unit + wt * C::kGroup;
-        const bool tail = t_unit + C::kUnit > first;
+      auto step = [&](int u, auto tail_unit) {
+        constexpr bool tail = decltype(tail_unit)::value;
+        const int t0 = u * C::kUnit + wt * C::kGroup;
         // (a wave that owns its tile needs no barrier, its LDS accesses being in order; the
         // fences keep the compiler's order)
         if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -288,12 +290,12 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
           if (u + 2 < g.u0 + g.count) look_up(u + 2);
         }
         if constexpr (RW > 1) {
-          if (tail) bad = __syncthreads_or(bad);
+          if constexpr (tail) bad = __syncthreads_or(bad);
           else __syncthreads();
         } else {
           bad = tail && __any(bad);
         }
-        if (!busy && !bad) continue;  // (no rows: the wave only loads)
+        if (!busy && !(tail && bad)) return;  // (no rows: the wave only loads)
         unsigned char* kt = tile_at(u);
         unsigned char* vt = kt + C::kKeys;
 
@@ -320,15 +322,26 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
             if (u + 1 < g.u0 + g.count) load_keys(u + 1);
           } else {
             const int px = piece_xor(col) ^ half;
+            u4 x[8];
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-              const u4 x = *reinterpret_cast<const u4*>(kp + 16 * (px ^ (2 * ks)));
-              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, x), qb[ks], z[b], 0, 0, 0);
-            }
+            for (int ks = 0; ks < 8; ++ks) x[ks] = *reinterpret_cast<const u4*>(kp + 16 * (px ^ (2 * ks)));
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, x[ks]), qb[ks], z[b], 0, 0, 0);
           }
         }
+        if constexpr (!kF32 && !C::kDirect) {
+          // four key pieces ahead of the products
+          __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+          for (int e = 0; e < 8 * NB - 4; ++e) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          }
+          __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+        }
         // ---- masks (element e of a lane: token 8 (e / 4) + 4 half + e % 4)
-        if (tail) {
+        if constexpr (tail) {
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             const uint32_t seen = window(t0 + 32 * b) >> (4 * half);
@@ -357,15 +370,17 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
             for (int e = 0; e < 16; ++e) o[dt][e] *= sc;
         }
         const float ms = m == -INFINITY ? 0.0f : m;
-        float ps = 0.0f;
+        auto weigh = [&](int b, int e0, int e1) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
+          for (int e = e0; e < e1; ++e) {
             z[b][e] = __builtin_amdgcn_exp2f(fmaf(z[b][e], zs, -ms));
-            ps += z[b][e];
+            l += z[b][e];
           }
-        l += ps;
+        };
+        if constexpr (kF32 || tail) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) weigh(b, 0, 16);
+        }
 
         // ---- values that are not finite, among the new tokens: 0 times them would reach rows
         // that do not see them, so they are added by hand and leave the tile
@@ -376,7 +391,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
                 vt + tok * C::kVRow + 16 * ((dim >> 3) ^ piece_xor(tok)) + 2 * (dim & 7)));
         };
         auto row_bad = [&](int tok) { return __any(!finite(value(tok, 2 * lane)) || !finite(value(tok, 2 * lane + 1))); };
-        if (bad) {
+        if (tail && bad) {
           if constexpr (RW > 1) __syncthreads();  // (the keys' last readers)
           float* w = reinterpret_cast<float*>(kt) + wr * 1024;
 #pragma unroll
@@ -429,36 +444,61 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
           const int c = lane & 15, tv = 4 * half + (c >> 2);
           const int p0 = (2 * ((lane >> 4) & 1) + ((c & 3) >> 1)) ^ piece_xor(tv);
           const unsigned char* vp = vt + tv * C::kVRow + 8 * (c & 1);
+          // In pieces of 16 tokens: between the products of one, the next one's values are
+          // fetched and its weights formed.
+          using LdsS4 = __attribute__((address_space(3))) s4;
+          bf8 x[2][4], p[2][NT];
+          auto fetch = [&](int c) {
+            const unsigned char* vb = vp + 16 * c * C::kVRow;
 #pragma unroll
-          for (int b = 0; b < NB; ++b)
+            for (int dt = 0; dt < 4; ++dt) {
+              const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)(vb + 16 * (p0 ^ (4 * dt))));
+              const s4 hi =
+                  __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)(vb + 8 * C::kVRow + 16 * (p0 ^ (4 * dt) ^ 8)));
+              x[c & 1][dt] = __builtin_bit_cast(bf8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+          };
+          auto form = [&](int c) {
+            if constexpr (!tail) weigh(c / 2, 8 * (c & 1), 8 * (c & 1) + 8);
+            float rest[8];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              bf8 p[NT];
-              float rest[8];
+            for (int e = 0; e < 8; ++e) rest[e] = z[c / 2][8 * (c & 1) + e];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) rest[e] = z[b][8 * t + e];
+            for (int k = 0; k < NT; ++k)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                p[c & 1][k][e] = (__bf16)rest[e];
+                rest[e] -= (float)p[c & 1][k][e];
+              }
+          };
+          fetch(0);
+          form(0);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int c = 0; c < 2 * NB; ++c) {
+            if (c + 1 < 2 * NB) fetch(c + 1);
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
               for (int k = 0; k < NT; ++k)
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c & 1][dt], p[c & 1][k], o[dt], 0, 0, 0);
+            if (c + 1 < 2 * NB) {
+              form(c + 1);
+              __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  p[k][e] = (__bf16)rest[e];
-                  rest[e] -= (float)p[k][e];
-                }
-#pragma unroll
-              for (int dt = 0; dt < 4; ++dt) {
-                using LdsS4 = __attribute__((address_space(3))) s4;
-                const unsigned char* vb = vp + (32 * b + 16 * t) * C::kVRow;
-                const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)(vb + 16 * (p0 ^ (4 * dt))));
-                const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (LdsS4*)(vb + 8 * C::kVRow + 16 * (p0 ^ (4 * dt) ^ 8)));
-                const bf8 x = __builtin_bit_cast(bf8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                for (int k = 0; k < NT; ++k)
-                  o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[k], o[dt], 0, 0, 0);
+              for (int e = 0; e < 4 * NT; ++e) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(0x402, 6, 1);
               }
             }
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
-      }
+      };
+      // units in front of the new tokens, then the others
+      const int u_end = g.u0 + g.count, u_tail = min(u_end, max(g.u0, first > 0 ? first / C::kUnit : 0));
+      for (int u = g.u0; u < u_tail; ++u) step(u, std::false_type{});
+      for (int u = u_tail; u < u_end; ++u) step(u, std::true_type{});
     }
 
     // ---- the item's output, or a partial
