@@ -99,7 +99,9 @@ struct Tree {
   static constexpr int kTile = kKeys + kGroup * kVRow;     // of one group's unit
   static constexpr int kBufs = RW > 1 ? 2 : 1;
   static constexpr int kJoin = TW > 1 ? TW * kRows * 132 * 4 : 0;
-  static constexpr int kLds = kTile * TW * kBufs > kJoin ? kTile * TW * kBufs : kJoin;
+  // (direct) the rows' queries lie behind the tiles, to leave the registers to the loads
+  static constexpr int kUsed = kTile * TW * kBufs + (kDirect ? 32 * 256 : 0);
+  static constexpr int kLds = kUsed > kJoin ? kUsed : kJoin;
 };
 
 struct Segment {
@@ -149,9 +151,22 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     const uint32_t* mask = d.mask ? d.mask + row * d.words : nullptr;
 
     // this lane's query: dimensions 16 ks + 8 half + 0 .. 7, or 8 u + 4 half + 0 .. 3
-    bf8 qb[kF32 ? 1 : 8];
+    bf8 qb[kF32 || C::kDirect ? 1 : 8];
     float qf[kF32 ? 64 : 1];
-    {
+    unsigned char* const q_lds = lds + C::kTile * TW * C::kBufs;
+    if constexpr (C::kDirect) {
+      __syncthreads();  // (the queries' last readers)
+      const int rr = tid >> 3, rg = r0 + rr;  // 32 rows, two pieces a thread
+      const bool there = rr < count_rows;
+      const TQ* q = static_cast<const TQ*>(d.q) +
+                    (long)(rows.x + (there ? rg / d.G : 0)) * d.q_stride + (h * d.G + (there ? rg % d.G : 0)) * kDim;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int pc = (tid & 7) + 8 * e;
+        const u4 w = *reinterpret_cast<const u4*>(q + 8 * pc), none = {};
+        *reinterpret_cast<u4*>(q_lds + rr * 256 + 16 * (pc ^ piece_xor(rr))) = there ? w : none;
+      }
+    } else {
       const TQ* q = static_cast<const TQ*>(d.q) + row * d.q_stride + hg * kDim;
       if constexpr (kF32) {
 #pragma unroll
@@ -272,10 +287,10 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
       for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
 
     if (L > 0) {
-      __syncthreads();  // (the tiles' last readers: the segment before)
       look_up(g.u0);
       load(g.u0);
       load_keys(g.u0);
+      __syncthreads();  // (the tiles' last readers: the segment before)
       if (g.count > 1) look_up(g.u0 + 1);
       auto step = [&](int u, auto tail_unit) {
         constexpr bool tail = decltype(tail_unit)::value;
@@ -317,8 +332,11 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
             }
           } else if constexpr (C::kDirect) {
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, kr[ks]), qb[ks], z[b], 0, 0, 0);
+            for (int ks = 0; ks < 8; ++ks) {
+              const u4 y = *reinterpret_cast<const u4*>(q_lds + col * 256 + 16 * (piece_xor(col) ^ half ^ (2 * ks)));
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, kr[ks]), __builtin_bit_cast(bf8, y),
+                                                             z[b], 0, 0, 0);
+            }
             if (u + 1 < g.u0 + g.count) load_keys(u + 1);
           } else {
             const int px = piece_xor(col) ^ half;
@@ -831,11 +849,19 @@ void launch_f32(const TreeArgs& a, const Plan& p, hipStream_t st) {
   if (p.rows == 32) launch_one<true, TQ, TK, 1, 1, 4, 1, 1>(a, p, st);
   else launch_one<true, TQ, TK, 1, 4, 1, 1, 2>(a, p, st);
 }
-template <int NT>
+// Terms of a weight: three for fp32 outputs (2^-24); one for bf16 ones, whose own rounding is as
+// large (prompts 728 us in two terms, 580 in one), but two where the tile is bound by memory.
 void launch_bf16(const TreeArgs& a, const Plan& p, hipStream_t st) {
-  if (p.rows == 32) launch_one<false, uint16_t, uint16_t, NT, 1, 4, 1, 2>(a, p, st);
-  else if (p.rows == 64) launch_one<false, uint16_t, uint16_t, NT, 2, 2, 1, 2>(a, p, st);
-  else launch_one<false, uint16_t, uint16_t, NT, 4, 1, 2, 2>(a, p, st);
+  if (p.rows == 32) {
+    if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 2, 1, 4, 1, 2>(a, p, st);
+    else launch_one<false, uint16_t, uint16_t, 3, 1, 4, 1, 2>(a, p, st);
+  } else if (p.rows == 64) {
+    if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 1, 2, 2, 1, 2>(a, p, st);
+    else launch_one<false, uint16_t, uint16_t, 3, 2, 2, 1, 2>(a, p, st);
+  } else {
+    if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 1, 4, 1, 2, 2>(a, p, st);
+    else launch_one<false, uint16_t, uint16_t, 3, 4, 1, 2, 2>(a, p, st);
+  }
 }
 
 }  // namespace
@@ -854,8 +880,7 @@ hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& d, const vo
                    reinterpret_cast<float*>(w + p.po), reinterpret_cast<int32_t*>(w + p.po + p.pml),
                    (int)p.tiles, p.split, out_bf16 ? 1 : 0};
   if (c.q_dtype == LOCKS_BF16 && c.kv_dtype == LOCKS_BF16) {
-    if (out_bf16) launch_bf16<2>(a, p, st);
-    else launch_bf16<3>(a, p, st);
+    launch_bf16(a, p, st);
   } else if (c.q_dtype == LOCKS_BF16) {
     launch_f32<uint16_t, float>(a, p, st);
   } else if (c.kv_dtype == LOCKS_BF16) {

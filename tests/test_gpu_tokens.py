@@ -5,8 +5,9 @@ Bounds.  A logit is a sum of 128 products in float32, in any order, off by at mo
 dz = 130 2^-24 sum |q k| / sqrt d, its scaling and the hardware's power of two by 2^-22 (1 + |z|)
 more; N weights are added with N + 64 roundings.  So with e = 2 (dz + 2^-22 (1 + |z|max)) +
 (N + 64) 2^-23 an output is within (e + w) max |v| of the 64-bit one, w the weights' own
-rounding (2^-16 for two bf16 terms, 2^-22 for three, both sides of the division), and a bf16
-output half a step (2^-8 of itself) further; the LSE within e + 2^-22 (|lse| + 1).  A token's
+rounding in the product with the values (their sum is of unrounded ones): half a bf16 step, 2^-8
+of each, for bf16 outputs, three terms (2^-24; 2^-22 is allowed) for fp32 ones; and a bf16 output
+is half a step (2^-8 of itself) further off; the LSE within e + 2^-22 (|lse| + 1).  A token's
 mass is a sum of R weights exp(z - lse), each within dz + 2^-21 (1 + |z| + |lse|) of itself,
 added with R + 64 roundings, and its old part one product and one sum."""
 import itertools
@@ -109,7 +110,7 @@ class Batch:
             N = self.lens[s]
             zmax = np.abs(q @ K.T).max() / np.sqrt(D)
             e = 2 * (130 * 2.0 ** -24 * big + 2.0 ** -22 * (1 + zmax)) + (N + 64) * 2.0 ** -23
-            w = 2.0 ** -16 if out == "bf16" else 2.0 ** -22
+            w = 2.0 ** -8 if out == "bf16" else 2.0 ** -22
             bound = (e + w) * np.abs(V[np.isfinite(V).all(1)]).max()
             if out == "bf16":
                 bound = bound + 2.0 ** -8 * np.abs(want) * 1.01
@@ -236,7 +237,7 @@ def test_tree_long(q, out, past, new, H, G):
         zmax = float(z[torch.isfinite(z)].abs().max())
         # sums of N weights over blocks: no lane adds more than N / 16 in a row
         e = 2 * (130 * 2.0 ** -24 * big + 2.0 ** -22 * (1 + zmax)) + (L / 16 + 256) * 2.0 ** -23
-        w = 2.0 ** -16 if out == "bf16" else 2.0 ** -22
+        w = 2.0 ** -8 if out == "bf16" else 2.0 ** -22
         heads = slice(h * G, (h + 1) * G)
         bound = (e + w) * float(V.abs().max()) + (2.0 ** -8 * 1.01 * want.abs() if out == "bf16" else 0)
         assert bool(((o[rows, heads].cuda().double() - want).abs() <= bound).all())
