@@ -36,6 +36,40 @@ __device__ __forceinline__ bool draft_sees(const DraftArgs& a, int row, int i, i
   return j < 32 * a.words && (a.mask[(long)row * a.words + (j >> 5)] >> (j & 31) & 1);
 }
 
+// Exclusive prefix sum of one value a thread over a 256-thread block; total in `sum`.
+__device__ __forceinline__ long scan256(long v, long* lds, long& sum) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  long x = v;
+  for (int o = 1; o < 64; o <<= 1) {
+    const long y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) lds[wave] = x;
+  __syncthreads();
+  long before = 0;
+  sum = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += lds[w];
+    sum += lds[w];
+  }
+  return before + x - v;
+}
+
+// Position of a 16-byte piece within a token's row in LDS: an exclusive or with this.  Any 8
+// tokens in a row differ in the lower three bits (row reads), any 4 in bits 1 and 2 (transposed
+// reads of two pieces each).
+__device__ __forceinline__ int piece_xor(int tok) { return ((tok & 3) << 1) | ((tok >> 2) & 1) | (tok & 8); }
+
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
 size_t tree_scratch_bytes(const locks_cfg_t& c, int n_tokens);
 hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& a, const void* k_cache,
                               const void* v_cache, void* out, bool out_bf16, float* out_lse,

@@ -25,16 +25,8 @@
 namespace locks {
 namespace {
 
-typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
-typedef short s4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef float f16v __attribute__((ext_vector_type(16)));
-
 constexpr int kTiles = 512;        // row tiles of a launch whose items are cut into shares
 constexpr int kTreeBlocks = 512;   // two per compute unit
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 
 struct TreeArgs {
   DraftArgs d;
@@ -57,32 +49,6 @@ __device__ __forceinline__ float swap_sum(float v) {
   return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 __device__ __forceinline__ bool finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-
-// Exclusive prefix sum of one value a thread over a 256-thread block; total in `sum`.
-__device__ __forceinline__ long scan256(long v, long* lds, long& sum) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  long x = v;
-  for (int o = 1; o < 64; o <<= 1) {
-    const long y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) lds[wave] = x;
-  __syncthreads();
-  long before = 0;
-  sum = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < wave) before += lds[w];
-    sum += lds[w];
-  }
-  return before + x - v;
-}
-
-// Position of a 16-byte piece within a token's row in LDS: an exclusive or with this.  Any 8
-// tokens in a row differ in the lower three bits (key reads), any 4 in bits 1 and 2 (the
-// transposed reads of two pieces each).
-__device__ __forceinline__ int piece_xor(int tok) { return ((tok & 3) << 1) | ((tok >> 2) & 1) | (tok & 8); }
 
 // kF32: products in fp32 (32x32x2 MFMA), else bf16 (32x32x16), the weights in NT terms.
 template <bool kF32, typename TQ, typename TK, int NT, int RW, int TW, int NB>
