@@ -1,15 +1,25 @@
 // The tokens of a list (sequence, KV head) to keep: the first n_sink, the last n_recent and
 // the others of largest mass, in order.
 //
-// With the masses as unsigned keys of the same order, the key of the last token kept is found
-// digit by digit (radix select, 8 bits a pass, histograms in LDS), then the tokens above it and
-// the first ones equal to it are written at their ranks.  One block per list.
+// With the masses as unsigned keys of the same order, the key T of the last token kept is found
+// in three digits (11, 11 and 10 bits): a histogram of the digit over the tokens whose higher
+// digits are T's, and the bin where the count from above passes the number to keep.  Then the
+// tokens above T, and the first ones equal to it, are written at their ranks.  A block holds up
+// to 32 K tokens of a list in registers, a wave 64 kKeys of them in a row, so that ranks within
+// a wave are counts of ballots.  Lists of up to that many tokens take one launch; longer ones
+// are cut into chunks of 32 K, each with a block that writes its chunk's histogram, and four
+// launches: a launch's blocks each sum the chunks' histograms of the digit before (which also
+// tells how many tokens kept lie before their chunk).
 #include "tokens_internal.h"
 
 namespace locks {
 namespace {
 
-constexpr int kPickBlock = 1024;
+constexpr int kPickBlock = 1024, kWaves = kPickBlock / 64;
+constexpr int kBins = 2048;
+constexpr int kOneLaunch = 32768;  // tokens of a list that one block takes
+constexpr int kPickChunk = 32768;
+constexpr uint32_t kZeroKey = 0x80000000u;
 
 // Unsigned key of a mass: order as the values', -0 as 0, NaN below everything.
 __device__ __forceinline__ uint32_t mass_key(float x) {
@@ -17,7 +27,17 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
   return f32_order_key(x + 0.0f);
 }
 
-// Exclusive prefix sum of a value per thread over the block; total in `sum`.
+struct PickArgs {
+  const float* mass;
+  const int32_t* seq_lens;
+  int32_t* out;
+  uint16_t* hist;   // [3][lists][chunks][kBins]
+  int32_t* state;   // [lists][chunks][4]: T's digits, left to keep from the bin, kept before the chunk
+  int H, width, n_keep, n_sink, n_recent, chunks;
+  long lists;
+};
+
+// Exclusive prefix sum of one value a thread over the block; total in `sum`.
 __device__ __forceinline__ int block_scan(int v, int* lds, int& sum) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int x = v;
@@ -30,79 +50,196 @@ __device__ __forceinline__ int block_scan(int v, int* lds, int& sum) {
   __syncthreads();
   int before = 0;
   sum = 0;
-  for (int w = 0; w < kPickBlock / 64; ++w) {
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
     if (w < wave) before += lds[w];
     sum += lds[w];
   }
   return before + x - v;
 }
 
-__global__ __launch_bounds__(kPickBlock) void pick_kernel(const float* __restrict__ mass,
-                                                          const int32_t* __restrict__ seq_lens, int H,
-                                                          int width, int n_keep, int n_sink,
-                                                          int n_recent, int32_t* __restrict__ out_ids) {
-  __shared__ int hist[256], waves[kPickBlock / 64], s_bin, s_left;
-  const long list = blockIdx.x;
-  const int L = min(max(seq_lens[list / H], 0), width), tid = threadIdx.x;
-  const float* x = mass + list * width;
-  int32_t* out = out_ids + list * n_keep;
-  if (L <= n_keep) {
-    for (int i = tid; i < n_keep; i += kPickBlock) out[i] = i < L ? i : -1;
+// kPhase -1: the whole of it.  0, 1, 2: the histogram of that digit; 3: the output.
+template <int kKeys, int kPhase>
+__global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
+  __shared__ int s_hist[kBins], s_wave[kWaves], s_bin, s_left;
+  const long list = blockIdx.x / a.chunks;
+  const int chunk = blockIdx.x % a.chunks, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int L = min(max(a.seq_lens[list / a.H], 0), a.width);
+  int32_t* out = a.out + list * a.n_keep;
+  if (L <= a.n_keep) {
+    if ((kPhase == -1 || kPhase == 3) && chunk == 0)
+      for (int i = tid; i < a.n_keep; i += kPickBlock) out[i] = i < L ? i : -1;
     return;
   }
-  const int lo = n_sink, hi = L - n_recent;  // the candidates (lo < hi as L > n_keep)
-  int left = n_keep - n_sink - n_recent;     // of which so many are kept
-  uint32_t prefix = 0;
-  if (left > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int b = tid; b < 256; b += kPickBlock) hist[b] = 0;
-      __syncthreads();
-      for (int i = lo + tid; i < hi; i += kPickBlock) {
-        const uint32_t k = mass_key(x[i]);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[k >> shift & 255], 1);
+  constexpr int kChunk = kPickBlock * kKeys;
+  const int i0 = chunk * kChunk + wave * 64 * kKeys + lane;  // this thread's tokens: i0 + 64 e
+  if (chunk * kChunk >= L && kPhase != -1) {
+    if (kPhase < 3) {  // an empty chunk's histogram
+      uint16_t* to = a.hist + ((kPhase * a.lists + list) * a.chunks + chunk) * kBins;
+      reinterpret_cast<uint32_t*>(to)[tid] = 0;
+    }
+    return;
+  }
+  const int lo = a.n_sink, hi = L - a.n_recent;  // the candidates (lo < hi as L > n_keep)
+  const float* x = a.mass + list * a.width;
+  uint32_t key[kKeys];
+#pragma unroll
+  for (int e = 0; e < kKeys; ++e) {
+    const int i = i0 + 64 * e;
+    key[e] = i >= lo && i < hi ? __float_as_uint(x[i]) : 0;
+  }
+  auto open = [&](int e) { return i0 + 64 * e >= lo && i0 + 64 * e < hi; };
+
+  uint32_t prefix = 0;                              // T's digits so far
+  int left = a.n_keep - a.n_sink - a.n_recent;      // to keep of the tokens that have them
+  int above = 0;                                    // of earlier chunks, tokens above T's digits
+  if (kPhase > 0) {
+    const int32_t* st = a.state + (list * a.chunks + chunk) * 4;
+    if (kPhase > 1) prefix = (uint32_t)st[0], left = st[1], above = st[2];
+  }
+  const bool none = a.n_keep == a.n_sink + a.n_recent;
+#pragma unroll
+  for (int e = 0; e < kKeys; ++e) key[e] = mass_key(__uint_as_float(key[e]));
+
+  auto shift_of = [](int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; };
+  // counts digit d of the tokens whose higher digits are T's
+  auto count = [&](int d) {
+    s_hist[tid] = 0;
+    s_hist[tid + kPickBlock] = 0;
+    __syncthreads();
+    const int shift = shift_of(d), mask = d == 2 ? 1023 : 2047;
+#pragma unroll
+    for (int e = 0; e < kKeys; ++e) {
+      const bool in = open(e) && (d == 0 || key[e] >> (d == 1 ? 21 : 10) == prefix >> (d == 1 ? 21 : 10));
+      const int bin = key[e] >> shift & mask;
+      // zeros, and what the first lane has, in one addition each: equal masses would queue
+      const unsigned long long zero = __ballot(in && key[e] == kZeroKey);
+      const bool rest = in && key[e] != kZeroKey;
+      const unsigned long long live = __ballot(rest);
+      if (zero && lane == 0) atomicAdd(&s_hist[kZeroKey >> shift & mask], (int)__popcll(zero));
+      if (live) {
+        const int lead = __ffsll(live) - 1, lead_bin = __builtin_amdgcn_readlane(bin, lead);
+        const unsigned long long same = __ballot(rest && bin == lead_bin);
+        if (lane == lead) atomicAdd(&s_hist[lead_bin], (int)__popcll(same));
+        else if (rest && bin != lead_bin) atomicAdd(&s_hist[bin], 1);
       }
-      __syncthreads();
-      if (tid == 0) {
-        int b = 255, above = 0;
-        while (above + hist[b] < left) above += hist[b--];
-        s_bin = b;
-        s_left = left - above;
-      }
-      __syncthreads();
-      prefix |= (uint32_t)s_bin << shift;
-      left = s_left;
+    }
+    __syncthreads();
+  };
+  // the bin of digit d in which the count from above passes `left`; h: this thread's two bins,
+  // kBins - 1 - 2 tid and the one below, over all chunks; p: over the earlier ones
+  auto choose = [&](int d, int h0, int h1, int p0, int p1) {
+    int sum;
+    const int from = block_scan(h0 + h1, s_wave, sum);
+    const int b = kBins - 1 - 2 * tid;
+    if (from < left && from + h0 >= left) s_bin = b, s_left = left - from;
+    else if (from + h0 < left && from + h0 + h1 >= left) s_bin = b - 1, s_left = left - from - h0;
+    __syncthreads();
+    const int bin = s_bin;
+    prefix |= (uint32_t)bin << shift_of(d);
+    left = s_left;
+    if (kPhase != -1) {
+      block_scan((b > bin ? p0 : 0) + (b - 1 > bin ? p1 : 0), s_wave, sum);
+      above += sum;
+    }
+  };
+  int ties = 0;  // tokens equal to T in earlier chunks
+  if (kPhase == -1 && !none) {
+    for (int d = 0; d < 3; ++d) {
+      count(d);
+      choose(d, s_hist[kBins - 1 - 2 * tid], s_hist[kBins - 2 - 2 * tid], 0, 0);
       __syncthreads();
     }
   }
-  // ranks: a token is kept if forced, above the key, or among the first `left` equal to it
-  const bool none = n_keep == n_sink + n_recent;
-  int base = 0, ties = 0;
-  for (int i0 = 0; i0 < L; i0 += kPickBlock) {
-    const int i = i0 + tid;
-    const bool forced = i < L && (i < lo || i >= hi);
-    const uint32_t k = i < L ? mass_key(x[i]) : 0;
-    const bool open = i < L && !forced && !none;
-    const int tie = open && k == prefix;
-    int n_tie, n_new;
-    const int before = ties + block_scan(tie, waves, n_tie);
-    const int take = forced || (open && k > prefix) || (tie && before < left);
-    const int at = base + block_scan(take, waves, n_new);
-    if (take) out[at] = i;
-    base += n_new;
-    ties += n_tie;
+  if (kPhase > 0 && !none) {
+    const int d = kPhase - 1;
+    const uint16_t* hist = a.hist + (d * a.lists + list) * a.chunks * kBins;
+    int h0 = 0, h1 = 0, p0 = 0, p1 = 0;
+    for (int c = 0; c < a.chunks; ++c) {
+      const uint32_t v = reinterpret_cast<const uint32_t*>(hist + (long)c * kBins)[kPickBlock - 1 - tid];
+      h0 += v >> 16, h1 += v & 0xffffu;
+      if (c < chunk) p0 += v >> 16, p1 += v & 0xffffu;
+    }
+    choose(d, h0, h1, p0, p1);
+    if (kPhase == 3) {
+      int sum;
+      const int b = kBins - 1 - 2 * tid, bin = s_bin;
+      block_scan((b == bin ? p0 : 0) + (b - 1 == bin ? p1 : 0), s_wave, sum);
+      ties = sum;
+    } else if (tid == 0) {
+      int32_t* st = a.state + (list * a.chunks + chunk) * 4;
+      st[0] = (int32_t)prefix, st[1] = left, st[2] = above;
+    }
   }
+  if (kPhase >= 0 && kPhase < 3) {
+    if (none) return;
+    count(kPhase);
+    uint16_t* to = a.hist + ((kPhase * a.lists + list) * a.chunks + chunk) * kBins;
+    reinterpret_cast<uint32_t*>(to)[tid] = (uint32_t)s_hist[2 * tid] | (uint32_t)s_hist[2 * tid + 1] << 16;
+    return;
+  }
+
+  // ---- ranks: forced tokens, those above T, the first `left` equal to it
+  int counts = 0;  // above, and 2^16 times equal (a wave has at most 2,048 tokens)
+#pragma unroll
+  for (int e = 0; e < kKeys; ++e)
+    counts += !none && open(e) ? (key[e] > prefix ? 1 : key[e] == prefix ? 1 << 16 : 0) : 0;
+  for (int o = 32; o > 0; o >>= 1) counts += __shfl_xor(counts, o, 64);
+  __syncthreads();
+  if (lane == 0) s_wave[wave] = counts & 0xffff, s_hist[wave] = counts >> 16;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) above += s_wave[w], ties += s_hist[w];
+  const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+  for (int e = 0; e < kKeys; ++e) {
+    const int i = i0 + 64 * e, first = i - lane;
+    const bool forced = i < L && (i < lo || i >= hi), cand = !none && open(e);
+    const unsigned long long tie = __ballot(cand && key[e] == prefix), over = __ballot(cand && key[e] > prefix);
+    const int rank = ties + (int)__popcll(tie & below);
+    const bool take = forced || (over >> lane & 1) || ((tie >> lane & 1) && rank < left);
+    // forced ones before token i: the first n_sink and what lies behind hi
+    const int sure = min(i, lo) + max(0, i - hi);
+    if (take) out[sure + above + (int)__popcll(over & below) + min(rank, left)] = i;
+    above += (int)__popcll(over);
+    ties += (int)__popcll(tie);
+    if (first + 64 >= L) break;
+  }
+}
+
+int pick_chunks(const locks_cfg_t& c) {
+  const long width = (long)c.max_pages_per_seq * c.page_size;
+  return width <= kOneLaunch ? 1 : (int)((width + kPickChunk - 1) / kPickChunk);
 }
 
 }  // namespace
 
-size_t pick_scratch_bytes(const locks_cfg_t&) { return 256; }
+size_t pick_scratch_bytes(const locks_cfg_t& c) {
+  const size_t chunks = pick_chunks(c), lists = (size_t)c.num_seqs * c.num_kv_heads;
+  return 256 + (chunks > 1 ? lists * chunks * (3 * kBins * sizeof(uint16_t) + 4 * sizeof(int32_t)) : 0);
+}
 
 hipError_t launch_pick_tokens(const locks_cfg_t& c, const float* mass, const int32_t* seq_lens,
-                              int n_keep, int n_sink, int n_recent, int32_t* out_ids, void*,
+                              int n_keep, int n_sink, int n_recent, int32_t* out_ids, void* scratch,
                               hipStream_t st) {
-  hipLaunchKernelGGL(pick_kernel, dim3((unsigned)(c.num_seqs * c.num_kv_heads)), dim3(kPickBlock), 0, st, mass,
-                     seq_lens, c.num_kv_heads, c.max_pages_per_seq * c.page_size, n_keep, n_sink, n_recent,
-                     out_ids);
+  const long lists = (long)c.num_seqs * c.num_kv_heads;
+  const int width = c.max_pages_per_seq * c.page_size, chunks = pick_chunks(c);
+  uint16_t* hist = static_cast<uint16_t*>(scratch);
+  const PickArgs a{mass,   seq_lens, out_ids, hist,     reinterpret_cast<int32_t*>(hist + 3 * lists * chunks * kBins),
+                   c.num_kv_heads, width, n_keep, n_sink, n_recent, chunks, lists};
+  const dim3 grid((unsigned)(lists * chunks)), block(kPickBlock);
+#define PICK(KEYS, PHASE) hipLaunchKernelGGL((pick_kernel<KEYS, PHASE>), grid, block, 0, st, a)
+  if (chunks == 1) {
+    if (width <= 4 * kPickBlock) PICK(4, -1);
+    else if (width <= 8 * kPickBlock) PICK(8, -1);
+    else if (width <= 16 * kPickBlock) PICK(16, -1);
+    else PICK(32, -1);
+  } else {
+    PICK(32, 0);
+    PICK(32, 1);
+    PICK(32, 2);
+    PICK(32, 3);
+  }
+#undef PICK
   return hipGetLastError();
 }
 
