@@ -32,7 +32,8 @@ struct PickArgs {
   const int32_t* seq_lens;
   int32_t* out;
   uint16_t* hist;   // [3][lists][chunks][kBins]
-  int32_t* state;   // [lists][chunks][4]: T's digits, left to keep from the bin, kept before the chunk
+  int32_t* state;   // [lists][chunks][4]: T's digits, left to keep from the bin, kept before the
+                    // chunk, whether the whole bin is kept
   int H, width, n_keep, n_sink, n_recent, chunks;
   long lists;
 };
@@ -61,7 +62,7 @@ __device__ __forceinline__ int block_scan(int v, int* lds, int& sum) {
 // kPhase -1: the whole of it.  0, 1, 2: the histogram of that digit; 3: the output.
 template <int kKeys, int kPhase>
 __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
-  __shared__ int s_hist[kBins], s_wave[kWaves], s_bin, s_left;
+  __shared__ int s_hist[kBins], s_wave[kWaves], s_bin, s_left, s_all;
   const long list = blockIdx.x / a.chunks;
   const int chunk = blockIdx.x % a.chunks, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int L = min(max(a.seq_lens[list / a.H], 0), a.width);
@@ -84,18 +85,16 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   const float* x = a.mass + list * a.width;
   uint32_t key[kKeys];
 #pragma unroll
-  for (int e = 0; e < kKeys; ++e) {
-    const int i = i0 + 64 * e;
-    key[e] = i >= lo && i < hi ? __float_as_uint(x[i]) : 0;
-  }
+  for (int e = 0; e < kKeys; ++e) key[e] = __float_as_uint(x[min(i0 + 64 * e, L - 1)]);
   auto open = [&](int e) { return i0 + 64 * e >= lo && i0 + 64 * e < hi; };
 
   uint32_t prefix = 0;                              // T's digits so far
   int left = a.n_keep - a.n_sink - a.n_recent;      // to keep of the tokens that have them
   int above = 0;                                    // of earlier chunks, tokens above T's digits
+  bool all = false;                                 // every token that has them is kept
   if (kPhase > 0) {
     const int32_t* st = a.state + (list * a.chunks + chunk) * 4;
-    if (kPhase > 1) prefix = (uint32_t)st[0], left = st[1], above = st[2];
+    if (kPhase > 1) prefix = (uint32_t)st[0], left = st[1], above = st[2], all = st[3] != 0;
   }
   const bool none = a.n_keep == a.n_sink + a.n_recent;
 #pragma unroll
@@ -108,22 +107,15 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
     s_hist[tid + kPickBlock] = 0;
     __syncthreads();
     const int shift = shift_of(d), mask = d == 2 ? 1023 : 2047;
+    int zeros = 0;  // counted by ballots: as one bin's additions they would queue
 #pragma unroll
     for (int e = 0; e < kKeys; ++e) {
       const bool in = open(e) && (d == 0 || key[e] >> (d == 1 ? 21 : 10) == prefix >> (d == 1 ? 21 : 10));
-      const int bin = key[e] >> shift & mask;
-      // zeros, and what the first lane has, in one addition each: equal masses would queue
-      const unsigned long long zero = __ballot(in && key[e] == kZeroKey);
-      const bool rest = in && key[e] != kZeroKey;
-      const unsigned long long live = __ballot(rest);
-      if (zero && lane == 0) atomicAdd(&s_hist[kZeroKey >> shift & mask], (int)__popcll(zero));
-      if (live) {
-        const int lead = __ffsll(live) - 1, lead_bin = __builtin_amdgcn_readlane(bin, lead);
-        const unsigned long long same = __ballot(rest && bin == lead_bin);
-        if (lane == lead) atomicAdd(&s_hist[lead_bin], (int)__popcll(same));
-        else if (rest && bin != lead_bin) atomicAdd(&s_hist[bin], 1);
-      }
+      const bool zero = key[e] == kZeroKey;
+      zeros += (int)__popcll(__ballot(in && zero));
+      if (in && !zero) atomicAdd(&s_hist[key[e] >> shift & mask], 1);
     }
+    if (lane == 0 && zeros) atomicAdd(&s_hist[kZeroKey >> shift & mask], zeros);
     __syncthreads();
   };
   // the bin of digit d in which the count from above passes `left`; h: this thread's two bins,
@@ -132,29 +124,33 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
     int sum;
     const int from = block_scan(h0 + h1, s_wave, sum);
     const int b = kBins - 1 - 2 * tid;
-    if (from < left && from + h0 >= left) s_bin = b, s_left = left - from;
-    else if (from + h0 < left && from + h0 + h1 >= left) s_bin = b - 1, s_left = left - from - h0;
+    if (from < left && from + h0 >= left) s_bin = b, s_left = left - from, s_all = from + h0 == left;
+    else if (from + h0 < left && from + h0 + h1 >= left)
+      s_bin = b - 1, s_left = left - from - h0, s_all = from + h0 + h1 == left;
     __syncthreads();
     const int bin = s_bin;
     prefix |= (uint32_t)bin << shift_of(d);
     left = s_left;
+    all = s_all != 0;
     if (kPhase != -1) {
-      block_scan((b > bin ? p0 : 0) + (b - 1 > bin ? p1 : 0), s_wave, sum);
+      const int from_bin = all ? bin : bin + 1;  // (those of a bin kept whole count as above)
+      block_scan((b >= from_bin ? p0 : 0) + (b - 1 >= from_bin ? p1 : 0), s_wave, sum);
       above += sum;
     }
   };
   int ties = 0;  // tokens equal to T in earlier chunks
   if (kPhase == -1 && !none) {
-    for (int d = 0; d < 3; ++d) {
+    for (int d = 0; d < 3 && !all; ++d) {
       count(d);
       choose(d, s_hist[kBins - 1 - 2 * tid], s_hist[kBins - 2 - 2 * tid], 0, 0);
       __syncthreads();
     }
   }
-  if (kPhase > 0 && !none) {
+  if (kPhase > 0 && !none && !all) {
     const int d = kPhase - 1;
     const uint16_t* hist = a.hist + (d * a.lists + list) * a.chunks * kBins;
     int h0 = 0, h1 = 0, p0 = 0, p1 = 0;
+#pragma unroll 16
     for (int c = 0; c < a.chunks; ++c) {
       const uint32_t v = reinterpret_cast<const uint32_t*>(hist + (long)c * kBins)[kPickBlock - 1 - tid];
       h0 += v >> 16, h1 += v & 0xffffu;
@@ -165,44 +161,56 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
       int sum;
       const int b = kBins - 1 - 2 * tid, bin = s_bin;
       block_scan((b == bin ? p0 : 0) + (b - 1 == bin ? p1 : 0), s_wave, sum);
-      ties = sum;
+      ties = all ? 0 : sum;
     } else if (tid == 0) {
       int32_t* st = a.state + (list * a.chunks + chunk) * 4;
-      st[0] = (int32_t)prefix, st[1] = left, st[2] = above;
+      st[0] = (int32_t)prefix, st[1] = left, st[2] = above, st[3] = all;
     }
   }
   if (kPhase >= 0 && kPhase < 3) {
-    if (none) return;
+    if (none || all) return;
     count(kPhase);
     uint16_t* to = a.hist + ((kPhase * a.lists + list) * a.chunks + chunk) * kBins;
     reinterpret_cast<uint32_t*>(to)[tid] = (uint32_t)s_hist[2 * tid] | (uint32_t)s_hist[2 * tid + 1] << 16;
     return;
   }
 
-  // ---- ranks: forced tokens, those above T, the first `left` equal to it
-  int counts = 0;  // above, and 2^16 times equal (a wave has at most 2,048 tokens)
-#pragma unroll
-  for (int e = 0; e < kKeys; ++e)
-    counts += !none && open(e) ? (key[e] > prefix ? 1 : key[e] == prefix ? 1 << 16 : 0) : 0;
-  for (int o = 32; o > 0; o >>= 1) counts += __shfl_xor(counts, o, 64);
-  __syncthreads();
-  if (lane == 0) s_wave[wave] = counts & 0xffff, s_hist[wave] = counts >> 16;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) above += s_wave[w], ties += s_hist[w];
-  const unsigned long long below = (1ull << lane) - 1;
+  // ---- the first n_sink and the last n_recent
+  if (chunk == 0) {
+    for (int i = tid; i < lo; i += kPickBlock) out[i] = i;
+    for (int i = tid; i < a.n_recent; i += kPickBlock) out[a.n_keep - a.n_recent + i] = hi + i;
+  }
+  // ---- ranks.  Lane g takes the 64 tokens of the wave's group g: which are above T, and which
+  // equal to it.
+  unsigned long long over = 0, tie = 0;
 #pragma unroll
   for (int e = 0; e < kKeys; ++e) {
-    const int i = i0 + 64 * e, first = i - lane;
-    const bool forced = i < L && (i < lo || i >= hi), cand = !none && open(e);
-    const unsigned long long tie = __ballot(cand && key[e] == prefix), over = __ballot(cand && key[e] > prefix);
-    const int rank = ties + (int)__popcll(tie & below);
-    const bool take = forced || (over >> lane & 1) || ((tie >> lane & 1) && rank < left);
-    // forced ones before token i: the first n_sink and what lies behind hi
-    const int sure = min(i, lo) + max(0, i - hi);
-    if (take) out[sure + above + (int)__popcll(over & below) + min(rank, left)] = i;
-    above += (int)__popcll(over);
-    ties += (int)__popcll(tie);
-    if (first + 64 >= L) break;
+    const bool cand = !none && open(e);
+    const unsigned long long o = __ballot(cand && (key[e] > prefix || (all && key[e] == prefix)));
+    const unsigned long long t = __ballot(cand && !all && key[e] == prefix);
+    over = lane == e ? o : over;
+    tie = lane == e ? t : tie;
+  }
+  int n_over = (int)__popcll(over), n_tie = (int)__popcll(tie);
+  for (int o = 1; o < 64; o <<= 1) {  // inclusive over the lanes
+    const int p = __shfl_up(n_over, o, 64), q = __shfl_up(n_tie, o, 64);
+    if (lane >= o) n_over += p, n_tie += q;
+  }
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = n_over, s_hist[wave] = n_tie;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) above += s_wave[w], ties += s_hist[w];
+  above += n_over - (int)__popcll(over);
+  ties += n_tie - (int)__popcll(tie);
+  const int g0 = chunk * kChunk + wave * 64 * kKeys + 64 * lane;  // the group's first token
+  if (lane < kKeys && g0 < L) {
+    unsigned long long take = over;
+    int at = lo + above + min(ties, left);
+    for (int room = left - ties; tie && room > 0; --room) {  // the first ones equal to T
+      take |= tie & -tie;
+      tie &= tie - 1;
+    }
+    for (; take; take &= take - 1) out[at++] = g0 + __ffsll(take) - 1;
   }
 }
 
