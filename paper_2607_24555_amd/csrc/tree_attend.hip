@@ -163,28 +163,31 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         blk[b] = table[t >> lgP];
       }
     };
-    long base[2 * NB];  // (the same in every lane)
+    const uint32_t page_bytes = (uint32_t)d.pgsz * kDim * sizeof(TK), blk_bytes = page_bytes * d.H;
+    const char* const k_head = static_cast<const char*>(a.k) + (size_t)h * page_bytes;
+    const char* const v_head = static_cast<const char*>(a.v) + (size_t)h * page_bytes;
+    size_t base[2 * NB];  // (the same in every lane)
     auto load = [&](int u) {
 #pragma unroll
       for (int b = 0; b < 2 * NB; ++b) {
-        const int x = __builtin_amdgcn_readfirstlane(blk[b]);
-        base[b] = ((long)((unsigned)x < (unsigned)d.num_blocks ? x : 0) * d.H + h) * d.pgsz * kDim;
+        const uint32_t x = (uint32_t)__builtin_amdgcn_readfirstlane(blk[b]);
+        base[b] = (size_t)(x < (uint32_t)d.num_blocks ? x : 0u) * blk_bytes;
       }
 #pragma unroll
       for (int j = 0; j < C::kLoads; ++j) {
         constexpr int kElems = kF32 ? 4 : 8;
         const int t = min(u * C::kUnit + wt * C::kGroup + j * C::kTokStep + tok_in, L - 1);
-        const unsigned at = (t & (d.pgsz - 1)) * kDim + kElems * piece;
-        if constexpr (!C::kDirect)
-          kr[j] = *reinterpret_cast<const Raw*>(static_cast<const TK*>(a.k) + base[j * C::kTokStep / 16] + at);
-        vr[j] = *reinterpret_cast<const Raw*>(static_cast<const TK*>(a.v) + base[j * C::kTokStep / 16] + at);
+        const uint32_t at = ((t & (d.pgsz - 1)) * kDim + kElems * piece) * sizeof(TK);
+        if constexpr (!C::kDirect) kr[j] = *reinterpret_cast<const Raw*>(k_head + base[j * C::kTokStep / 16] + at);
+        vr[j] = *reinterpret_cast<const Raw*>(v_head + base[j * C::kTokStep / 16] + at);
       }
     };
     // (direct) this lane's half of its token's key, of the unit whose values were loaded last
     auto load_keys = [&](int u) {
       if constexpr (C::kDirect) {
         const int t = min(u * C::kUnit + wt * C::kGroup + col, L - 1);
-        const TK* p = static_cast<const TK*>(a.k) + (col < 16 ? base[0] : base[1]) + (t & (d.pgsz - 1)) * kDim + 8 * half;
+        const TK* p = reinterpret_cast<const TK*>(k_head + (col < 16 ? base[0] : base[1])) +
+                      (t & (d.pgsz - 1)) * kDim + 8 * half;
 #pragma unroll
         for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const Raw*>(p + 16 * j);
       }
@@ -283,36 +286,42 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         // ---- logits
         f16v z[NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int e = 0; e < 16; ++e) z[b][e] = 0.0f;
-          const unsigned char* kp = kt + (32 * b + col) * C::kKRow;
-          if constexpr (kF32) {
+        const unsigned char* kp = kt + col * C::kKRow;
+        if constexpr (kF32) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int u8 = 0; u8 < 16; ++u8) {
-              const float4 x = *reinterpret_cast<const float4*>(kp + 32 * u8 + 16 * half);
+              const float4 x = *reinterpret_cast<const float4*>(kp + 32 * b * C::kKRow + 32 * u8 + 16 * half);
               z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, qf[4 * u8], z[b], 0, 0, 0);
               z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, qf[4 * u8 + 1], z[b], 0, 0, 0);
               z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, qf[4 * u8 + 2], z[b], 0, 0, 0);
               z[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, qf[4 * u8 + 3], z[b], 0, 0, 0);
             }
-          } else if constexpr (C::kDirect) {
+        } else if constexpr (C::kDirect) {
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
-              const u4 y = *reinterpret_cast<const u4*>(q_lds + col * 256 + 16 * (piece_xor(col) ^ half ^ (2 * ks)));
-              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, kr[ks]), __builtin_bit_cast(bf8, y),
-                                                             z[b], 0, 0, 0);
-            }
-            if (u + 1 < g.u0 + g.count) load_keys(u + 1);
-          } else {
-            const int px = piece_xor(col) ^ half;
-            u4 x[8];
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) x[ks] = *reinterpret_cast<const u4*>(kp + 16 * (px ^ (2 * ks)));
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
-              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, x[ks]), qb[ks], z[b], 0, 0, 0);
+          for (int ks = 0; ks < 8; ++ks) {
+            const u4 y = *reinterpret_cast<const u4*>(q_lds + col * 256 + 16 * (piece_xor(col) ^ half ^ (2 * ks)));
+            z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, kr[ks]), __builtin_bit_cast(bf8, y),
+                                                           z[0], 0, 0, 0);
           }
+          if (u + 1 < g.u0 + g.count) load_keys(u + 1);
+        } else {
+          const int px = piece_xor(col) ^ half;
+          u4 x[8][NB];
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              x[ks][b] = *reinterpret_cast<const u4*>(kp + 32 * b * C::kKRow + 16 * (px ^ (2 * ks)));
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+              z[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, x[ks][b]), qb[ks], z[b], 0, 0, 0);
         }
         if constexpr (!kF32 && !C::kDirect) {
           // four key pieces ahead of the products
@@ -462,9 +471,9 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
           for (int c = 0; c < 2 * NB; ++c) {
             if (c + 1 < 2 * NB) fetch(c + 1);
 #pragma unroll
-            for (int dt = 0; dt < 4; ++dt)
+            for (int k = 0; k < NT; ++k)
 #pragma unroll
-              for (int k = 0; k < NT; ++k)
+              for (int dt = 0; dt < 4; ++dt)
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c & 1][dt], p[c & 1][k], o[dt], 0, 0, 0);
             if (c + 1 < 2 * NB) {
               form(c + 1);
