@@ -24,6 +24,17 @@ __device__ __forceinline__ int2 draft_rows(const DraftArgs& a, int s) {
   const int b = min(max(a.cu[s], 0), a.n_tokens), e = min(max(a.cu[s + 1], 0), a.n_tokens);
   return make_int2(b, max(b, e));
 }
+// (the loads together, so that one wait covers them)
+struct DraftSeq {
+  int row0, n, L;
+};
+__device__ __forceinline__ DraftSeq draft_seq(const DraftArgs& a, int s) {
+  int b = s, e = s + 1;
+  const int len = a.seq_lens[s];
+  if (a.cu) b = a.cu[s], e = a.cu[s + 1];
+  b = min(max(b, 0), a.n_tokens), e = min(max(e, 0), a.n_tokens);
+  return DraftSeq{b, max(e - b, 0), min(max(len, 0), a.max_pages * a.pgsz)};
+}
 __device__ __forceinline__ int draft_len(const DraftArgs& a, int s) {
   return min(max(a.seq_lens[s], 0), a.max_pages * a.pgsz);
 }
@@ -37,17 +48,18 @@ __device__ __forceinline__ bool draft_sees(const DraftArgs& a, int row, int i, i
 }
 
 // Exclusive prefix sum of one value a thread over a 256-thread block; total in `sum`.
-__device__ __forceinline__ long scan256(long v, long* lds, long& sum) {
+template <typename T>
+__device__ __forceinline__ T scan256(T v, T* lds, T& sum) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  long x = v;
+  T x = v;
   for (int o = 1; o < 64; o <<= 1) {
-    const long y = __shfl_up(x, o, 64);
+    const T y = __shfl_up(x, o, 64);
     if (lane >= o) x += y;
   }
   __syncthreads();
   if (lane == 63) lds[wave] = x;
   __syncthreads();
-  long before = 0;
+  T before = 0;
   sum = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {

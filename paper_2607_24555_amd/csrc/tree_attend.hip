@@ -73,6 +73,7 @@ struct Tree {
 struct Segment {
   int s, h, tile;
   int u0, count, units;
+  int row0, n, L;
 };
 
 template <bool kF32, typename TQ, typename TK, int NT, int RW, int TW, int NB, int kWaves>
@@ -80,8 +81,8 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
   using C = Tree<kF32, TQ, TK, NT, RW, TW, NB>;
   static_assert(RW * TW == 4, "four waves");
   __shared__ __align__(16) unsigned char lds[C::kLds];
-  __shared__ long s_units[kTiles + 1], s_sum[4];
-  __shared__ int s_first[kTiles + 1];
+  __shared__ int s_units[kTiles + 1], s_first[kTiles + 1], s_sum[4];
+  __shared__ int s_row0[kTiles], s_rows[kTiles], s_len[kTiles];
   __shared__ float s_m[TW][C::kRows], s_l[TW][C::kRows];
   const DraftArgs& d = a.d;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -105,15 +106,13 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
   auto units_of = [&](int n, int L, int tile) { return max(1, (reach(n, L, tile) + C::kUnit - 1) / C::kUnit); };
 
   // ---- one segment: units [u0, u0 + count) of an item
-  auto process = [&](const Segment& g, long lb, long share) {
-    const int s = g.s, h = g.h;
-    const int2 rows = draft_rows(d, s);
-    const int n = rows.y - rows.x, L = draft_len(d, s), first = L - n;
+  auto process = [&](const Segment& g, int lb, int share) {
+    const int s = g.s, h = g.h, row0 = g.row0, n = g.n, L = g.L, first = L - n;
     const int tr = tile_rows(n), r0 = g.tile * tr, count_rows = min(n * d.G - r0, tr);
     const int r = r0 + wr * 32 + col;
     const bool live = wr * 32 + col < count_rows, busy = wr * 32 < count_rows;
     const int i = live ? r / d.G : 0, hg = h * d.G + (live ? r % d.G : 0);
-    const long row = rows.x + i;
+    const long row = row0 + i;
     const uint32_t* mask = d.mask ? d.mask + row * d.words : nullptr;
 
     // this lane's query: dimensions 16 ks + 8 half + 0 .. 7, or 8 u + 4 half + 0 .. 3
@@ -125,7 +124,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
       const int rr = tid >> 3, rg = r0 + rr;  // 32 rows, two pieces a thread
       const bool there = rr < count_rows;
       const TQ* q = static_cast<const TQ*>(d.q) +
-                    (long)(rows.x + (there ? rg / d.G : 0)) * d.q_stride + (h * d.G + (there ? rg % d.G : 0)) * kDim;
+                    (long)(row0 + (there ? rg / d.G : 0)) * d.q_stride + (h * d.G + (there ? rg % d.G : 0)) * kDim;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int pc = (tid & 7) + 8 * e;
@@ -464,18 +463,25 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
                 rest[e] -= (float)p[c & 1][k][e];
               }
           };
-          fetch(0);
-          form(0);
-          __builtin_amdgcn_sched_barrier(0);
+          constexpr bool kAhead = !C::kDirect;  // (there is no room for it beside the loads)
+          if constexpr (kAhead) {
+            fetch(0);
+            form(0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
 #pragma unroll
           for (int c = 0; c < 2 * NB; ++c) {
-            if (c + 1 < 2 * NB) fetch(c + 1);
+            if constexpr (!kAhead) {
+              fetch(c);
+              form(c);
+            }
+            if (kAhead && c + 1 < 2 * NB) fetch(c + 1);
 #pragma unroll
             for (int k = 0; k < NT; ++k)
 #pragma unroll
               for (int dt = 0; dt < 4; ++dt)
                 o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[c & 1][dt], p[c & 1][k], o[dt], 0, 0, 0);
-            if (c + 1 < 2 * NB) {
+            if (kAhead && c + 1 < 2 * NB) {
               form(c + 1);
               __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
 #pragma unroll
@@ -484,7 +490,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
                 __builtin_amdgcn_sched_group_barrier(0x402, 6, 1);
               }
             }
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kAhead) __builtin_amdgcn_sched_barrier(0);
           }
         }
       };
@@ -497,13 +503,13 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     // ---- the item's output, or a partial
     l = swap_sum(l);
     const bool whole = g.count == g.units;
-    const long slot = g.u0 > 0 ? 2 * lb : 2 * lb + 1;
+    const long slot = g.u0 > 0 ? 2L * lb : 2L * lb + 1;
     auto emit = [&](int rr, int dim, float x0, float x1, float x2, float x3, float mm, float ll, bool stats) {
       // four dimensions of row rr of the tile
       const int rg = r0 + rr;
       if (rr >= count_rows) return;
       if (whole) {
-        const long to = (long)(rows.x + rg / d.G) * Hq + h * d.G + rg % d.G;
+        const long to = (long)(row0 + rg / d.G) * Hq + h * d.G + rg % d.G;
         const float inv = ll > 0.0f || ll != ll ? 1.0f / ll : 0.0f;
         if (a.out_bf16) {
           typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
@@ -564,15 +570,16 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     if (!whole && g.u0 == 0 && tid == 0) {
       int32_t* rec = a.rec + 8 * lb;
       rec[0] = count_rows;
-      rec[1] = 1 + (int)((g.units - g.count + share - 1) / share);
-      rec[2] = rows.x;
+      rec[1] = 1 + (g.units - g.count + share - 1) / share;
+      rec[2] = row0;
       rec[3] = r0;
       rec[4] = h;
     }
   };
 
   // ---- what this block computes
-  long x = 0, end = 1, lb = 0, share = 1;
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  int x = 0, end = 1, lb = 0, share = 1;
   Segment g{};
   if (!a.split) {
     // an item a block: tile slots, s + cu[s] G / rows on for sequence s, some of them empty
@@ -586,33 +593,34 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
       lo += k * step;
       hi = min(hi, lo + step);
     }
-    const int2 rows = draft_rows(d, lo);
-    const int n = rows.y - rows.x, tile = slot - base(lo);
-    if (tile < 0 || tile >= tiles_of(n)) return;
-    const int units = units_of(n, draft_len(d, lo), tile);
-    g = Segment{lo, h, tile, 0, units, units};
+    const DraftSeq q = draft_seq(d, lo);
+    const int tile = slot - base(lo);
+    if (tile < 0 || tile >= tiles_of(q.n)) return;
+    const int units = units_of(q.n, q.L, tile);
+    g = Segment{uniform(lo), h, uniform(tile), 0, uniform(units), uniform(units), uniform(q.row0), uniform(q.n), uniform(q.L)};
   } else {
     // the cut: tiles before each sequence, units before each tile
     constexpr int kPer = kTiles / 256;
-    long before[kPer], sum = 0, v = 0, total;
+    int before[kPer], sum = 0, v = 0, total;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
       const int s = tid * kPer + e;
       before[e] = v;
       if (s < d.S) {
-        const int2 rows = draft_rows(d, s);
-        v += tiles_of(rows.y - rows.x);
+        const DraftSeq q = draft_seq(d, s);
+        s_row0[s] = q.row0, s_rows[s] = q.n, s_len[s] = q.L;
+        v += tiles_of(q.n);
       }
     }
-    const long at = scan256(v, s_sum, total);
+    const int at = scan256(v, s_sum, total);
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
       const int s = tid * kPer + e;
-      if (s < d.S) s_first[s] = (int)(at + before[e]);
+      if (s < d.S) s_first[s] = at + before[e];
     }
-    if (tid == 0) s_first[d.S] = (int)total;
+    if (tid == 0) s_first[d.S] = total;
     __syncthreads();
-    const int T = min((int)total, kTiles);
+    const int T = min(total, kTiles);
     v = 0;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
@@ -625,19 +633,18 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
           if (s_first[mid] <= t) lo = mid;
           else hi = mid;
         }
-        const int2 rows = draft_rows(d, lo);
-        v += units_of(rows.y - rows.x, draft_len(d, lo), t - s_first[lo]);
+        v += units_of(s_rows[lo], s_len[lo], t - s_first[lo]);
       }
     }
-    const long ut = scan256(v, s_sum, sum);
+    const int ut = scan256(v, s_sum, sum);
 #pragma unroll
     for (int e = 0; e < kPer; ++e) s_units[tid * kPer + e] = ut + before[e];
     if (tid == 0) s_units[kTiles] = sum;
     __syncthreads();
-    const long all = s_units[kTiles] * d.H;
-    share = (all + gridDim.x - 1) / gridDim.x;
+    const int all = s_units[kTiles] * d.H;  // (below 2^31: see tree_plan)
+    share = (all + (int)gridDim.x - 1) / (int)gridDim.x;
     // (blocks that share an item or its keys run on one XCD)
-    lb = (gridDim.x & 7) ? blockIdx.x : (long)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    lb = (gridDim.x & 7) ? blockIdx.x : (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     x = lb * share;
     end = min(all, x + share);
     if (tid == 0) a.rec[8 * lb] = 0;
@@ -650,23 +657,20 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         if (s_units[s_first[mid]] * d.H <= x) lo = mid;
         else hi = mid;
       }
+      lo = uniform(lo);
       const int t0 = s_first[lo], t1 = s_first[lo + 1];
-      const long first = s_units[t0], per = s_units[t1] - first, in = x - first * d.H;
-      const int h = (int)(in / per);
-      const long rest = in % per + first;
+      const int first = s_units[t0], per = s_units[t1] - first, in = x - first * d.H;
+      const int h = (int)((unsigned)in / (unsigned)per), rest = in - h * per + first;
       int tl = t0, th = t1;
       while (th - tl > 1) {
         const int mid = (tl + th) / 2;
         if (s_units[mid] <= rest) tl = mid;
         else th = mid;
       }
-      const int units = (int)(s_units[tl + 1] - s_units[tl]), u0 = (int)(rest - s_units[tl]);
-      const int count = (int)min(end - x, (long)(units - u0));
-      g = Segment{lo, h, tl - t0, u0, count, units};
+      const int units = s_units[tl + 1] - s_units[tl], u0 = rest - s_units[tl];
+      g = Segment{lo, uniform(h), uniform(tl - t0), uniform(u0), uniform(min(end - x, units - u0)), uniform(units),
+                  uniform(s_row0[lo]), uniform(s_rows[lo]), uniform(s_len[lo])};
     }
-    g = Segment{__builtin_amdgcn_readfirstlane(g.s), __builtin_amdgcn_readfirstlane(g.h),
-                __builtin_amdgcn_readfirstlane(g.tile), __builtin_amdgcn_readfirstlane(g.u0),
-                __builtin_amdgcn_readfirstlane(g.count), __builtin_amdgcn_readfirstlane(g.units)};
     process(g, lb, share);
     x += g.count;
     if (!a.split) break;
@@ -685,11 +689,18 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(const int32_t* __restri
                                                          const float* __restrict__ pml, int tile_rows, int G,
                                                          int Hq, void* __restrict__ out, int out_bf16,
                                                          float* __restrict__ out_lse) {
-  __shared__ int s_end[kTreeBlocks], s_wave[8];
-  __shared__ float s_o[16][132], s_l[16];
+  __shared__ int s_end[kTreeBlocks], s_rec[kTreeBlocks][4], s_wave[8];
+  __shared__ __align__(16) float s_o[16][132];
+  __shared__ float s_m[16], s_l[16];
   const int tid = threadIdx.x, lane = tid & 63, l32 = tid & 31, grp = tid >> 5;
   // rows up to each block's item
-  int v = tid < blocks ? recs[8 * tid] : 0;
+  int4 r = make_int4(0, 0, 0, 0);
+  if (tid < blocks) {
+    r = *reinterpret_cast<const int4*>(recs + 8 * tid);
+    s_rec[tid][3] = recs[8 * tid + 4];
+  }
+  s_rec[tid][0] = r.y, s_rec[tid][1] = r.z, s_rec[tid][2] = r.w;
+  int v = r.x;
   for (int o = 1; o < 64; o <<= 1) {
     const int y = __shfl_up(v, o, 64);
     if (lane >= o) v += y;
@@ -720,54 +731,54 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(const int32_t* __restri
         if (s_end[mid] > row) hi = mid;
         else lo = mid + 1;
       }
-      const int32_t* rec = recs + 8 * lo;
-      const int rows = rec[0], parts = rec[1], rr = row - (s_end[lo] - rows), rg = rec[3] + rr;
-      to = (long)(rec[2] + rg / G) * Hq + rec[4] * G + rg % G;
+      const int parts = s_rec[lo][0], rr = row - (lo ? s_end[lo - 1] : 0), rg = s_rec[lo][2] + rr;
+      to = (long)(s_rec[lo][1] + rg / G) * Hq + s_rec[lo][3] * G + rg % G;
       auto slot = [&](int p) { return p ? 2L * (lo + p) : 2L * lo + 1; };
-      for (int p0 = 0; p0 < parts; p0 += 32)
-        if (p0 + l32 < parts) mx = fmaxf(mx, pml[(slot(p0 + l32) * tile_rows + rr) * 2]);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
       const int mine = (parts - part0 + groups - 1) / groups;  // parts part0, part0 + groups, ..
-      for (int k0 = 0; k0 < mine; k0 += 32) {
-        float w = 0.0f;
-        if (k0 + l32 < mine) {
-          const float2 st =
-              *reinterpret_cast<const float2*>(pml + (slot(part0 + (k0 + l32) * groups) * tile_rows + rr) * 2);
-          w = st.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.x - mx);
-          l += w * st.y;
+      for (int k = 0; k < mine; k += 8) {
+        float4 x[8];
+        float2 st[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const long at = slot(part0 + min(k + e, mine - 1) * groups) * tile_rows + rr;
+          st[e] = *reinterpret_cast<const float2*>(pml + at * 2);
+          x[e] = *reinterpret_cast<const float4*>(po + at * kDim + 4 * l32);
         }
-        const int nk = min(32, mine - k0);
-        for (int k = 0; k < nk; k += 8) {
-          float4 x[8];
+        float mn = mx;
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            x[e] = *reinterpret_cast<const float4*>(
-                po + (slot(part0 + (k0 + min(k + e, nk - 1)) * groups) * tile_rows + rr) * kDim + 4 * l32);
+        for (int e = 0; e < 8; ++e) mn = fmaxf(mn, st[e].x);
+        const float f = mx == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx - mn);
+        mx = mn;
+        l *= f;
+        acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float f = __shfl(w, min(k + e, 31), 32);
-            if (k + e < nk) {
-              acc.x = fmaf(f, x[e].x, acc.x);
-              acc.y = fmaf(f, x[e].y, acc.y);
-              acc.z = fmaf(f, x[e].z, acc.z);
-              acc.w = fmaf(f, x[e].w, acc.w);
-            }
-          }
+        for (int e = 0; e < 8; ++e) {
+          if (k + e >= mine) break;
+          const float w = st[e].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st[e].x - mn);
+          l = fmaf(w, st[e].y, l);
+          acc.x = fmaf(w, x[e].x, acc.x);
+          acc.y = fmaf(w, x[e].y, acc.y);
+          acc.z = fmaf(w, x[e].z, acc.z);
+          acc.w = fmaf(w, x[e].w, acc.w);
         }
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
     }
     if (groups > 1) {
       *reinterpret_cast<float4*>(&s_o[grp][4 * l32]) = acc;
-      if (l32 == 0) s_l[grp] = l;
+      if (l32 == 0) s_l[grp] = l, s_m[grp] = mx;
       __syncthreads();
       if (part0 == 0) {
-        for (int g = 1; g < groups; ++g) {
+        for (int g = 1; g < groups; ++g) mx = fmaxf(mx, s_m[grp + g]);
+        acc = make_float4(0, 0, 0, 0);
+        l = 0.0f;
+        for (int g = 0; g < groups; ++g) {
           const float4 x = *reinterpret_cast<const float4*>(&s_o[grp + g][4 * l32]);
-          acc.x += x.x, acc.y += x.y, acc.z += x.z, acc.w += x.w;
-          l += s_l[grp + g];
+          const float w = s_m[grp + g] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(s_m[grp + g] - mx);
+          l = fmaf(w, s_l[grp + g], l);
+          acc.x = fmaf(w, x.x, acc.x);
+          acc.y = fmaf(w, x.y, acc.y);
+          acc.z = fmaf(w, x.z, acc.z);
+          acc.w = fmaf(w, x.w, acc.w);
         }
       }
     }
@@ -802,10 +813,10 @@ Plan tree_plan(const locks_cfg_t& c, int n_tokens) {
   p.rows = rows <= 32 ? 32 : rows <= 64 && !f32 ? 64 : 128;
   p.unit = p.rows == 32 ? 128 : f32 ? 32 : 64;
   p.tiles = S + (long)n_tokens * G / p.rows;
-  p.split = p.tiles <= kTiles;
+  const long units = ((long)c.max_pages_per_seq * c.page_size + p.unit - 1) / p.unit;
+  const long most = p.tiles * units * c.num_kv_heads;  // (tokens x KV heads are below 2^31)
+  p.split = p.tiles <= kTiles && most <= 0x7fffffffL - kTreeBlocks;
   if (p.split) {
-    const long units = ((long)c.max_pages_per_seq * c.page_size + p.unit - 1) / p.unit;
-    const long most = p.tiles * units * c.num_kv_heads;
     p.blocks = (int)(most < kTreeBlocks ? (most + 7) / 8 * 8 : kTreeBlocks);
     p.po = (size_t)2 * p.blocks * p.rows * kDim * sizeof(float);
     p.pml = (size_t)2 * p.blocks * p.rows * 2 * sizeof(float);
