@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256, kF32 ? 1 : 2) void mass_kernel(DraftArgs a, co
         v += rows.y > rows.x ? (L + kUnit - 1) / kUnit : 0;
       }
     }
-    const long at = scan256(v, s_sum, total);
+    const long at = scan_block<4>(v, s_sum, total);
 #pragma unroll
     for (int e = 0; e < kPer; ++e) s_units[tid * kPer + e] = at + before[e];
     if (tid == 0) s_units[kSeqs] = total;

@@ -47,9 +47,9 @@ __device__ __forceinline__ bool draft_sees(const DraftArgs& a, int row, int i, i
   return j < 32 * a.words && (a.mask[(long)row * a.words + (j >> 5)] >> (j & 31) & 1);
 }
 
-// Exclusive prefix sum of one value a thread over a 256-thread block; total in `sum`.
-template <typename T>
-__device__ __forceinline__ T scan256(T v, T* lds, T& sum) {
+// Exclusive prefix sum of one value a thread over a block of kWaves waves; total in `sum`.
+template <int kWaves, typename T>
+__device__ __forceinline__ T scan_block(T v, T* lds, T& sum) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   T x = v;
   for (int o = 1; o < 64; o <<= 1) {
@@ -62,7 +62,7 @@ __device__ __forceinline__ T scan256(T v, T* lds, T& sum) {
   T before = 0;
   sum = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     if (w < wave) before += lds[w];
     sum += lds[w];
   }

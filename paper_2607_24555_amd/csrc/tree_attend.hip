@@ -77,11 +77,11 @@ struct Segment {
 };
 
 template <bool kF32, typename TQ, typename TK, int NT, int RW, int TW, int NB, int kWaves>
-__global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
+__global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) {
   using C = Tree<kF32, TQ, TK, NT, RW, TW, NB>;
-  static_assert(RW * TW == 4, "four waves");
+  constexpr int kBlock = 64 * RW * TW;
   __shared__ __align__(16) unsigned char lds[C::kLds];
-  __shared__ int s_units[kTiles + 1], s_first[kTiles + 1], s_sum[4];
+  __shared__ int s_units[kTiles + 1], s_first[kTiles + 1], s_sum[RW * TW];
   __shared__ int s_row0[kTiles], s_rows[kTiles], s_len[kTiles];
   __shared__ float s_m[TW][C::kRows], s_l[TW][C::kRows];
   const DraftArgs& d = a.d;
@@ -177,8 +177,11 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         constexpr int kElems = kF32 ? 4 : 8;
         const int t = min(u * C::kUnit + wt * C::kGroup + j * C::kTokStep + tok_in, L - 1);
         const uint32_t at = ((t & (d.pgsz - 1)) * kDim + kElems * piece) * sizeof(TK);
-        if constexpr (!C::kDirect) kr[j] = *reinterpret_cast<const Raw*>(k_head + base[j * C::kTokStep / 16] + at);
-        vr[j] = *reinterpret_cast<const Raw*>(v_head + base[j * C::kTokStep / 16] + at);
+        // (the same 16 tokens for a wave: of a step of 32, the second 16 for the upper four waves)
+        static_assert(C::kTokStep <= 32, "");
+        const size_t page = C::kTokStep == 32 && wr >= 4 ? base[(j * C::kTokStep / 16 + 1) % (2 * NB)] : base[j * C::kTokStep / 16];
+        if constexpr (!C::kDirect) kr[j] = *reinterpret_cast<const Raw*>(k_head + page + at);
+        vr[j] = *reinterpret_cast<const Raw*>(v_head + page + at);
       }
     };
     // (direct) this lane's half of its token's key, of the unit whose values were loaded last
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const Raw*>(p + 16 * j);
       }
     };
-    auto tile_at = [&](int u) { return lds + (wt * C::kBufs + (C::kBufs > 1 ? u & 1 : 0)) * C::kTile; };
+    auto tile_at = [&](int u) { return lds + (wt * C::kBufs + (u & (C::kBufs - 1))) * C::kTile; };
     // writes the loaded unit; returns whether this thread's values are all finite (where asked)
     auto store = [&](int u, bool check) -> bool {
       unsigned char* kt = tile_at(u);
@@ -255,6 +258,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
       for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
 
     if (L > 0) {
+      const int u_end = g.u0 + g.count;
       look_up(g.u0);
       load(g.u0);
       load_keys(g.u0);
@@ -268,16 +272,13 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         bool bad = !store(u, tail);
         if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (u + 1 < g.u0 + g.count) {
+        if (u + 1 < u_end) {
           load(u + 1);
-          if (u + 2 < g.u0 + g.count) look_up(u + 2);
+          if (u + 2 < u_end) look_up(u + 2);
         }
-        if constexpr (RW > 1) {
-          if constexpr (tail) bad = __syncthreads_or(bad);
-          else __syncthreads();
-        } else {
-          bad = tail && __any(bad);
-        }
+        if constexpr (RW == 1) bad = tail && __any(bad);
+        else if constexpr (tail) bad = __syncthreads_or(bad);
+        else __syncthreads();
         if (!busy && !(tail && bad)) return;  // (no rows: the wave only loads)
         unsigned char* kt = tile_at(u);
         unsigned char* vt = kt + C::kKeys;
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
             z[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, kr[ks]), __builtin_bit_cast(bf8, y),
                                                            z[0], 0, 0, 0);
           }
-          if (u + 1 < g.u0 + g.count) load_keys(u + 1);
+          if (u + 1 < u_end) load_keys(u + 1);
         } else {
           const int px = piece_xor(col) ^ half;
           u4 x[8][NB];
@@ -385,7 +386,8 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         auto row_bad = [&](int tok) { return __any(!finite(value(tok, 2 * lane)) || !finite(value(tok, 2 * lane + 1))); };
         if (tail && bad) {
           if constexpr (RW > 1) __syncthreads();  // (the keys' last readers)
-          float* w = reinterpret_cast<float*>(kt) + wr * 1024;
+          // (4 KB a wave: four in this tile's keys, four in those of the unit before)
+          float* w = reinterpret_cast<float*>(wr < 4 ? kt : tile_at(u + 1)) + (wr & 3) * 1024;
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -495,7 +497,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         }
       };
       // units in front of the new tokens, then the others
-      const int u_end = g.u0 + g.count, u_tail = min(u_end, max(g.u0, first > 0 ? first / C::kUnit : 0));
+      const int u_tail = min(u_end, max(g.u0, first > 0 ? first / C::kUnit : 0));
       for (int u = g.u0; u < u_tail; ++u) step(u, std::false_type{});
       for (int u = u_tail; u < u_end; ++u) step(u, std::true_type{});
     }
@@ -550,7 +552,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
           *reinterpret_cast<float4*>(to + 32 * dt + 2 * e + 4 * half) =
               make_float4(o[dt][e] * f, o[dt][e + 1] * f, o[dt][e + 2] * f, o[dt][e + 3] * f);
       __syncthreads();
-      for (int e = tid; e < C::kRows * 32; e += 256) {
+      for (int e = tid; e < C::kRows * 32; e += kBlock) {
         const int rr = e >> 5, dim = 4 * (e & 31);
         float M = -INFINITY, ll = 0.0f;
         float4 x = make_float4(0, 0, 0, 0);
@@ -600,7 +602,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
     g = Segment{uniform(lo), h, uniform(tile), 0, uniform(units), uniform(units), uniform(q.row0), uniform(q.n), uniform(q.L)};
   } else {
     // the cut: tiles before each sequence, units before each tile
-    constexpr int kPer = kTiles / 256;
+    constexpr int kPer = kTiles / kBlock;
     int before[kPer], sum = 0, v = 0, total;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
@@ -612,7 +614,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         v += tiles_of(q.n);
       }
     }
-    const int at = scan256(v, s_sum, total);
+    const int at = scan_block<RW * TW>(v, s_sum, total);
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
       const int s = tid * kPer + e;
@@ -636,7 +638,7 @@ __global__ __launch_bounds__(256, kWaves) void tree_kernel(TreeArgs a) {
         v += units_of(s_rows[lo], s_len[lo], t - s_first[lo]);
       }
     }
-    const int ut = scan256(v, s_sum, sum);
+    const int ut = scan_block<RW * TW>(v, s_sum, sum);
 #pragma unroll
     for (int e = 0; e < kPer; ++e) s_units[tid * kPer + e] = ut + before[e];
     if (tid == 0) s_units[kTiles] = sum;
@@ -810,14 +812,15 @@ Plan tree_plan(const locks_cfg_t& c, int n_tokens) {
   const bool f32 = c.q_dtype != LOCKS_BF16 || c.kv_dtype != LOCKS_BF16;
   const long rows = ((long)n_tokens * G + S - 1) / S;
   Plan p{};
-  p.rows = rows <= 32 ? 32 : rows <= 64 && !f32 ? 64 : 128;
+  p.rows = rows <= 32 ? 32 : f32 ? 128 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   p.unit = p.rows == 32 ? 128 : f32 ? 32 : 64;
   p.tiles = S + (long)n_tokens * G / p.rows;
   const long units = ((long)c.max_pages_per_seq * c.page_size + p.unit - 1) / p.unit;
   const long most = p.tiles * units * c.num_kv_heads;  // (tokens x KV heads are below 2^31)
   p.split = p.tiles <= kTiles && most <= 0x7fffffffL - kTreeBlocks;
   if (p.split) {
-    p.blocks = (int)(most < kTreeBlocks ? (most + 7) / 8 * 8 : kTreeBlocks);
+    const long fill = p.rows == 256 ? kTreeBlocks / 2 : kTreeBlocks;
+    p.blocks = (int)(most < fill ? (most + 7) / 8 * 8 : fill);
     p.po = (size_t)2 * p.blocks * p.rows * kDim * sizeof(float);
     p.pml = (size_t)2 * p.blocks * p.rows * 2 * sizeof(float);
   }
@@ -827,7 +830,7 @@ Plan tree_plan(const locks_cfg_t& c, int n_tokens) {
 template <bool kF32, typename TQ, typename TK, int NT, int RW, int TW, int NB, int kWaves>
 void launch_one(const TreeArgs& a, const Plan& p, hipStream_t st) {
   const unsigned grid = p.split ? (unsigned)p.blocks : (unsigned)(p.tiles * a.d.H);
-  hipLaunchKernelGGL((tree_kernel<kF32, TQ, TK, NT, RW, TW, NB, kWaves>), dim3(grid), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((tree_kernel<kF32, TQ, TK, NT, RW, TW, NB, kWaves>), dim3(grid), dim3(64 * RW * TW), 0, st, a);
 }
 
 template <typename TQ, typename TK>
@@ -844,9 +847,12 @@ void launch_bf16(const TreeArgs& a, const Plan& p, hipStream_t st) {
   } else if (p.rows == 64) {
     if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 1, 2, 2, 1, 2>(a, p, st);
     else launch_one<false, uint16_t, uint16_t, 3, 2, 2, 1, 2>(a, p, st);
-  } else {
+  } else if (p.rows == 128) {
     if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 1, 4, 1, 2, 2>(a, p, st);
     else launch_one<false, uint16_t, uint16_t, 3, 4, 1, 2, 2>(a, p, st);
+  } else {
+    if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 1, 8, 1, 2, 2>(a, p, st);
+    else launch_one<false, uint16_t, uint16_t, 3, 8, 1, 2, 2>(a, p, st);
   }
 }
 
@@ -854,7 +860,8 @@ void launch_bf16(const TreeArgs& a, const Plan& p, hipStream_t st) {
 
 // (what no smaller number of tokens needs more than: a workspace serves up to n_tokens)
 size_t tree_scratch_bytes(const locks_cfg_t& c, int n_tokens) {
-  return (size_t)kTreeBlocks * (2 * tree_plan(c, n_tokens).rows * (kDim + 2) * sizeof(float) + 8 * sizeof(int32_t));
+  const size_t rows = tree_plan(c, n_tokens).rows < 128 ? tree_plan(c, n_tokens).rows : 128;  // (256: half the blocks)
+  return (size_t)kTreeBlocks * (2 * rows * (kDim + 2) * sizeof(float) + 8 * sizeof(int32_t));
 }
 
 hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& d, const void* k_cache,
