@@ -63,12 +63,33 @@ struct Tree {
   static constexpr bool kDirect = !kF32 && RW == 1;
   static constexpr int kKeys = kDirect ? 4096 : kGroup * kKRow;  // (4 KB of scratch at least)
   static constexpr int kTile = kKeys + kGroup * kVRow;     // of one group's unit
-  static constexpr int kBufs = RW > 1 ? 2 : 1;
+  // bf16 rows that waves share go to LDS without passing registers: three units ahead where a
+  // block has the compute unit for itself, else one
+  static constexpr bool kDma = !kF32 && RW > 1;
+  static constexpr int kBufs = RW == 8 ? 4 : RW > 1 ? 2 : 1;
+  static constexpr int kLead = kBufs - 1;
+  static constexpr int kDmaLoads = kDma ? kGroup / 4 / RW : 0;  // of a wave and tensor: 4 rows each
   static constexpr int kJoin = TW > 1 ? TW * kRows * 132 * 4 : 0;
   // (direct) the rows' queries lie behind the tiles, to leave the registers to the loads
   static constexpr int kUsed = kTile * TW * kBufs + (kDirect ? 32 * 256 : 0);
   static constexpr int kLds = kUsed > kJoin ? kUsed : kJoin;
 };
+
+// 16 bytes a lane from memory to LDS: lane l's to lds + 16 l.  Counted by vmcnt only; whoever
+// reads them waits (wait_vm) and passes a barrier.
+__device__ __forceinline__ void copy_to_lds(const char* base, uint32_t offset, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(offset), "s"(base), "s"(lds)
+      : "memory", "m0");
+}
+template <int kLeft>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLeft) : "memory");
+}
 
 struct Segment {
   int s, h, tile;
@@ -194,6 +215,29 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
         for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const Raw*>(p + 16 * j);
       }
     };
+    // (kDma) this wave's rows of unit u: they lie in one page, whose block was looked up before
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+    const __attribute__((address_space(4))) int32_t* const const_table =
+        (const __attribute__((address_space(4))) int32_t*)table;
+    constexpr int kMine = 4 * C::kDmaLoads;  // rows of a wave
+    static_assert(!C::kDma || 16 % kMine == 0, "rows of one page");
+    auto block_of = [&](int u) {
+      const int t = min(u * C::kUnit + wt * C::kGroup + wr * kMine, L - 1);
+      return const_table[t >> lgP];
+    };
+    auto issue = [&](int u, int blk) {
+      const uint32_t x = (uint32_t)blk;
+      const size_t page = (size_t)(x < (uint32_t)d.num_blocks ? x : 0u) * blk_bytes;
+      const uint32_t to = lds_at + (wt * C::kBufs + (u & (C::kBufs - 1))) * C::kTile + wr * kMine * 256;
+#pragma unroll
+      for (int j = 0; j < C::kDmaLoads; ++j) {
+        const int in = wr * kMine + 4 * j + (lane >> 4);  // the tile's token
+        const int t = min(u * C::kUnit + wt * C::kGroup + in, L - 1);
+        const uint32_t at = ((t & (d.pgsz - 1)) * kDim + 8 * ((lane & 15) ^ piece_xor(in))) * 2;
+        copy_to_lds(k_head + page, at, to + 1024 * j);
+        copy_to_lds(v_head + page, at, to + C::kKeys + 1024 * j);
+      }
+    };
     auto tile_at = [&](int u) { return lds + (wt * C::kBufs + (u & (C::kBufs - 1))) * C::kTile; };
     // writes the loaded unit; returns whether this thread's values are all finite (where asked)
     auto store = [&](int u, bool check) -> bool {
@@ -259,26 +303,61 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
 
     if (L > 0) {
       const int u_end = g.u0 + g.count;
-      look_up(g.u0);
-      load(g.u0);
-      load_keys(g.u0);
-      __syncthreads();  // (the tiles' last readers: the segment before)
-      if (g.count > 1) look_up(g.u0 + 1);
+      int next_blk = 0;  // (kDma) of the unit kLead after the one at hand
+      if constexpr (C::kDma) {
+        __syncthreads();  // (the tiles' last readers: the segment before)
+#pragma unroll
+        for (int e = 0; e < C::kLead; ++e)
+          if (e < g.count) issue(g.u0 + e, block_of(g.u0 + e));
+        if (C::kLead < g.count) next_blk = block_of(g.u0 + C::kLead);
+      } else {
+        look_up(g.u0);
+        load(g.u0);
+        load_keys(g.u0);
+        __syncthreads();
+        if (g.count > 1) look_up(g.u0 + 1);
+      }
       auto step = [&](int u, auto tail_unit) {
         constexpr bool tail = decltype(tail_unit)::value;
         const int t0 = u * C::kUnit + wt * C::kGroup;
-        // (a wave that owns its tile needs no barrier, its LDS accesses being in order; the
-        // fences keep the compiler's order)
-        if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        bool bad = !store(u, tail);
-        if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (u + 1 < u_end) {
-          load(u + 1);
-          if (u + 2 < u_end) look_up(u + 2);
+        bool bad;
+        if constexpr (C::kDma) {
+          // this unit's copies are here; those of the units behind it may be on their way
+          constexpr int kUnitLoads = 2 * C::kDmaLoads;
+          if (C::kLead > 2 && u + 2 < u_end) wait_vm<2 * kUnitLoads>();
+          else if (C::kLead > 1 && u + 1 < u_end) wait_vm<kUnitLoads>();
+          else wait_vm<0>();
+          __syncthreads();
+          if (u + C::kLead < u_end) {
+            issue(u + C::kLead, next_blk);
+            if (u + C::kLead + 1 < u_end) next_blk = block_of(u + C::kLead + 1);
+          }
+          bad = false;
+          if constexpr (tail) {
+            const unsigned char* v = tile_at(u) + C::kKeys;
+#pragma unroll
+            for (int j = 0; j < C::kGroup * 16 / C::kThreads; ++j) {
+              const u4 x = *reinterpret_cast<const u4*>(v + 16 * (gt + j * C::kThreads));
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                bad = bad || (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+            }
+            bad = __syncthreads_or(bad);
+          }
+        } else {
+          // (a wave that owns its tile needs no barrier, its LDS accesses being in order; the
+          // fences keep the compiler's order)
+          if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          bad = !store(u, tail);
+          if constexpr (RW == 1) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          if (u + 1 < u_end) {
+            load(u + 1);
+            if (u + 2 < u_end) look_up(u + 2);
+          }
+          if constexpr (RW == 1) bad = tail && __any(bad);
+          else if constexpr (tail) bad = __syncthreads_or(bad);
+          else __syncthreads();
         }
-        if constexpr (RW == 1) bad = tail && __any(bad);
-        else if constexpr (tail) bad = __syncthreads_or(bad);
-        else __syncthreads();
         if (!busy && !(tail && bad)) return;  // (no rows: the wave only loads)
         unsigned char* kt = tile_at(u);
         unsigned char* vt = kt + C::kKeys;
@@ -386,21 +465,21 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
         auto row_bad = [&](int tok) { return __any(!finite(value(tok, 2 * lane)) || !finite(value(tok, 2 * lane + 1))); };
         if (tail && bad) {
           if constexpr (RW > 1) __syncthreads();  // (the keys' last readers)
-          // (4 KB a wave: four in this tile's keys, four in those of the unit before)
-          float* w = reinterpret_cast<float*>(wr < 4 ? kt : tile_at(u + 1)) + (wr & 3) * 1024;
+          // the weights of 16 tokens at a time, 2 KB a wave in the keys' place
+          float* w = reinterpret_cast<float*>(kt) + wr * 512;
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
+          for (int c = 0; c < 2 * NB; ++c) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[(8 * (e / 4) + 4 * half + e % 4) * 32 + col] = z[b][e];
+            for (int e = 0; e < 8; ++e) w[(8 * (e / 4) + 4 * half + e % 4) * 32 + col] = z[c / 2][8 * (c & 1) + e];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            for (int t = 0; t < 32; ++t) {
-              if (!row_bad(32 * b + t)) continue;
+            for (int t = 0; t < 16; ++t) {
+              if (!row_bad(16 * c + t)) continue;
               const float p = w[t * 32 + col];
 #pragma unroll
               for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                  const float x = value(32 * b + t, 32 * dt + 8 * (e / 4) + 4 * half + e % 4);
+                  const float x = value(16 * c + t, 32 * dt + 8 * (e / 4) + 4 * half + e % 4);
                   o[dt][e] += p != 0.0f ? p * x : 0.0f;
                 }
             }
