@@ -28,6 +28,8 @@ namespace {
 constexpr int kTiles = 512;        // row tiles of a launch whose items are cut into shares
 constexpr int kTreeBlocks = 512;   // two per compute unit
 
+constexpr int kMaskWords = 8;      // of a row's mask that lie in LDS (trees of up to 256 tokens)
+
 struct TreeArgs {
   DraftArgs d;
   const void *k, *v;
@@ -105,6 +107,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
   __shared__ int s_units[kTiles + 1], s_first[kTiles + 1], s_sum[RW * TW];
   __shared__ int s_row0[kTiles], s_rows[kTiles], s_len[kTiles];
   __shared__ float s_m[TW][C::kRows], s_l[TW][C::kRows];
+  __shared__ uint32_t s_mask[C::kRows][kMaskWords + 1];
   const DraftArgs& d = a.d;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % RW, wt = wave / RW;
@@ -284,8 +287,14 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
       uint32_t seen = j0 < 0 ? (1u << -j0) - 1u : 0u;
       if (mask) {
         const int w = j0 >> 5, sh = j0 & 31;
-        const uint32_t lo = (unsigned)w < (unsigned)d.words ? mask[w] : 0u;
-        const uint32_t hi = (unsigned)(w + 1) < (unsigned)d.words ? mask[w + 1] : 0u;
+        uint32_t lo = 0u, hi = 0u;
+        if (d.words <= kMaskWords) {
+          if ((unsigned)w < (unsigned)d.words) lo = s_mask[wr * 32 + col][w];
+          if ((unsigned)(w + 1) < (unsigned)d.words) hi = s_mask[wr * 32 + col][w + 1];
+        } else {
+          if ((unsigned)w < (unsigned)d.words) lo = mask[w];
+          if ((unsigned)(w + 1) < (unsigned)d.words) hi = mask[w + 1];
+        }
         seen |= sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
       } else {
         const int c = i - j0;
@@ -302,10 +311,20 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
       for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
 
     if (L > 0) {
-      const int u_end = g.u0 + g.count;
+      const int u_end = g.u0 + g.count, u_tail = min(u_end, max(g.u0, first > 0 ? first / C::kUnit : 0));
+      // the rows' masks, for units that hold new tokens: read from memory there, they would wait for
+      // the rows on their way too
+      auto fill_masks = [&] {
+        if (!mask || d.words > kMaskWords || u_tail == u_end) return;
+        for (int e = tid; e < count_rows * d.words; e += kBlock) {
+          const int rr = e / d.words, w = e % d.words;
+          s_mask[rr][w] = d.mask[(long)(row0 + (r0 + rr) / d.G) * d.words + w];
+        }
+      };
       int next_blk = 0;  // (kDma) of the unit kLead after the one at hand
       if constexpr (C::kDma) {
         __syncthreads();  // (the tiles' last readers: the segment before)
+        fill_masks();
 #pragma unroll
         for (int e = 0; e < C::kLead; ++e)
           if (e < g.count) issue(g.u0 + e, block_of(g.u0 + e));
@@ -315,6 +334,8 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
         load(g.u0);
         load_keys(g.u0);
         __syncthreads();
+        fill_masks();
+        if constexpr (RW == 1) __syncthreads();
         if (g.count > 1) look_up(g.u0 + 1);
       }
       auto step = [&](int u, auto tail_unit) {
@@ -576,7 +597,6 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
         }
       };
       // units in front of the new tokens, then the others
-      const int u_tail = min(u_end, max(g.u0, first > 0 ? first / C::kUnit : 0));
       for (int u = g.u0; u < u_tail; ++u) step(u, std::false_type{});
       for (int u = u_tail; u < u_end; ++u) step(u, std::true_type{});
     }
@@ -816,33 +836,38 @@ __global__ __launch_bounds__(512) void tree_merge_kernel(const int32_t* __restri
       to = (long)(s_rec[lo][1] + rg / G) * Hq + s_rec[lo][3] * G + rg % G;
       auto slot = [&](int p) { return p ? 2L * (lo + p) : 2L * lo + 1; };
       const int mine = (parts - part0 + groups - 1) / groups;  // parts part0, part0 + groups, ..
-      for (int k = 0; k < mine; k += 8) {
-        float4 x[8];
-        float2 st[8];
+      auto add = [&](auto batch) {
+        constexpr int kBatch = decltype(batch)::value;
+        for (int k = 0; k < mine; k += kBatch) {
+          float4 x[kBatch];
+          float2 st[kBatch];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const long at = slot(part0 + min(k + e, mine - 1) * groups) * tile_rows + rr;
-          st[e] = *reinterpret_cast<const float2*>(pml + at * 2);
-          x[e] = *reinterpret_cast<const float4*>(po + at * kDim + 4 * l32);
+          for (int e = 0; e < kBatch; ++e) {
+            const long at = slot(part0 + min(k + e, mine - 1) * groups) * tile_rows + rr;
+            st[e] = *reinterpret_cast<const float2*>(pml + at * 2);
+            x[e] = *reinterpret_cast<const float4*>(po + at * kDim + 4 * l32);
+          }
+          float mn = mx;
+#pragma unroll
+          for (int e = 0; e < kBatch; ++e) mn = fmaxf(mn, st[e].x);
+          const float f = mx == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx - mn);
+          mx = mn;
+          l *= f;
+          acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
+#pragma unroll
+          for (int e = 0; e < kBatch; ++e) {
+            if (k + e >= mine) break;
+            const float w = st[e].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st[e].x - mn);
+            l = fmaf(w, st[e].y, l);
+            acc.x = fmaf(w, x[e].x, acc.x);
+            acc.y = fmaf(w, x[e].y, acc.y);
+            acc.z = fmaf(w, x[e].z, acc.z);
+            acc.w = fmaf(w, x[e].w, acc.w);
+          }
         }
-        float mn = mx;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mn = fmaxf(mn, st[e].x);
-        const float f = mx == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mx - mn);
-        mx = mn;
-        l *= f;
-        acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (k + e >= mine) break;
-          const float w = st[e].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st[e].x - mn);
-          l = fmaf(w, st[e].y, l);
-          acc.x = fmaf(w, x[e].x, acc.x);
-          acc.y = fmaf(w, x[e].y, acc.y);
-          acc.z = fmaf(w, x[e].z, acc.z);
-          acc.w = fmaf(w, x[e].w, acc.w);
-        }
-      }
+      };
+      if (mine <= 2) add(std::integral_constant<int, 2>{});
+      else add(std::integral_constant<int, 8>{});
     }
     if (groups > 1) {
       *reinterpret_cast<float4*>(&s_o[grp][4 * l32]) = acc;
