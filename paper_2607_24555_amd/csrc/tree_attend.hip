@@ -13,7 +13,7 @@
 //
 // All (sequence, KV head, tile) items' units, in order, are cut into equal shares, one a
 // block (every block derives the cut from the lengths), so ragged batches and long lists
-// fill the chip; an item within a share writes its output, others leave partials (o, max,
+// fill the chip; a unit counts by the 32s of rows that its tile has (see weight_of); an item within a share writes its output, others leave partials (o, max,
 // sum), which merge_kernel combines in order.
 //
 // What a row does not see is masked by one 32-bit window per row and 32 tokens, the
@@ -129,8 +129,18 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
   };
   auto units_of = [&](int n, int L, int tile) { return max(1, (reach(n, L, tile) + C::kUnit - 1) / C::kUnit); };
 
-  // ---- one segment: units [u0, u0 + count) of an item
-  auto process = [&](const Segment& g, int lb, int share) {
+  // What a unit of a tile costs.  In the 256-row tile the products of more rows show a little
+  // (ragged trees of 140 to 248 rows: 232 us for tiles of 160 rows, 271 for 256, counted the same);
+  // in the others two blocks of a compute unit hide that.
+  constexpr int kMostWeight = RW == 8 ? 20 : 1;
+  auto weight_of = [&](int n, int tile) {
+    if (RW < 8) return 1;
+    const int tr = tile_rows(n), rows = (int)min((long)n * d.G - (long)tile * tr, (long)tr);
+    return 12 + (rows + 31) / 32;
+  };
+
+  // ---- one segment: units [u0, u0 + count) of an item, whose units lie in `parts` blocks
+  auto process = [&](const Segment& g, int lb, int parts) {
     const int s = g.s, h = g.h, row0 = g.row0, n = g.n, L = g.L, first = L - n;
     const int tr = tile_rows(n), r0 = g.tile * tr, count_rows = min(n * d.G - r0, tr);
     const int r = r0 + wr * 32 + col;
@@ -311,8 +321,11 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
       for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
 
     if (L > 0) {
-      const int u_end = g.u0 + g.count, u_tail = min(u_end, max(g.u0, first > 0 ? first / C::kUnit : 0));
-      // the rows' masks, for units that hold new tokens: read from memory there, they would wait for
+      // units that every row of the tile sees whole (of a run, up to its first row's token), then
+      // the others
+      const int all_see = d.mask ? first : first + r0 / d.G + 1;
+      const int u_end = g.u0 + g.count, u_tail = min(u_end, max(g.u0, all_see > 0 ? all_see / C::kUnit : 0));
+      // the rows' masks, for those others: read from memory there, they would wait for
       // the rows on their way too
       auto fill_masks = [&] {
         if (!mask || d.words > kMaskWords || u_tail == u_end) return;
@@ -453,7 +466,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
           for (int e = 0; e < 16; ++e) big = fmaxf(big, z[b][e]);
         big = swap_max(big) * zs;
         if (__any(big > m + 8.0f)) {
-          const float mn = fmaxf(m, big);
+          const float mn = big > m + 8.0f ? big : m;  // (by the row: no row's bits depend on another's)
           const float sc = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mn);
           m = mn;
           l *= sc;
@@ -596,7 +609,6 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
           }
         }
       };
-      // units in front of the new tokens, then the others
       for (int u = g.u0; u < u_tail; ++u) step(u, std::false_type{});
       for (int u = u_tail; u < u_end; ++u) step(u, std::true_type{});
     }
@@ -671,7 +683,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
     if (!whole && g.u0 == 0 && tid == 0) {
       int32_t* rec = a.rec + 8 * lb;
       rec[0] = count_rows;
-      rec[1] = 1 + (g.units - g.count + share - 1) / share;
+      rec[1] = parts;
       rec[2] = row0;
       rec[3] = r0;
       rec[4] = h;
@@ -680,7 +692,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
 
   // ---- what this block computes
   auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-  int x = 0, end = 1, lb = 0, share = 1;
+  int x = 0, end = 1, lb = 0, share = 1, parts = 1;
   Segment g{};
   if (!a.split) {
     // an item a block: tile slots, s + cu[s] G / rows on for sequence s, some of them empty
@@ -734,7 +746,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
           if (s_first[mid] <= t) lo = mid;
           else hi = mid;
         }
-        v += units_of(s_rows[lo], s_len[lo], t - s_first[lo]);
+        v += units_of(s_rows[lo], s_len[lo], t - s_first[lo]) * weight_of(s_rows[lo], t - s_first[lo]);
       }
     }
     const int ut = scan_block<RW * TW>(v, s_sum, sum);
@@ -743,7 +755,8 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
     if (tid == 0) s_units[kTiles] = sum;
     __syncthreads();
     const int all = s_units[kTiles] * d.H;  // (below 2^31: see tree_plan)
-    share = (all + (int)gridDim.x - 1) / (int)gridDim.x;
+    // (at least a unit, so that a block between an item's first and last has some of it)
+    share = max((all + (int)gridDim.x - 1) / (int)gridDim.x, kMostWeight);
     // (blocks that share an item or its keys run on one XCD)
     lb = (gridDim.x & 7) ? blockIdx.x : (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     x = lb * share;
@@ -768,12 +781,17 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
         if (s_units[mid] <= rest) tl = mid;
         else th = mid;
       }
-      const int units = s_units[tl + 1] - s_units[tl], u0 = rest - s_units[tl];
-      g = Segment{lo, uniform(h), uniform(tl - t0), uniform(u0), uniform(min(end - x, units - u0)), uniform(units),
-                  uniform(s_row0[lo]), uniform(s_rows[lo]), uniform(s_len[lo])};
+      // the item's units that begin in [x, end)
+      const int n = s_rows[lo], w = weight_of(n, tl - t0), at = x - (rest - s_units[tl]);
+      const int units = (s_units[tl + 1] - s_units[tl]) / w;
+      const int u0 = (x - at + w - 1) / w, u1 = min(units, (end - at + w - 1) / w);
+      parts = (at + (units - 1) * w) / share - lb + 1;
+      x = min(end, at + units * w);
+      if (u0 >= u1) continue;
+      g = Segment{lo, uniform(h), uniform(tl - t0), uniform(u0), uniform(u1 - u0), uniform(units),
+                  uniform(s_row0[lo]), uniform(n), uniform(s_len[lo])};
     }
-    process(g, lb, share);
-    x += g.count;
+    process(g, lb, parts);
     if (!a.split) break;
   }
 }
@@ -920,8 +938,8 @@ Plan tree_plan(const locks_cfg_t& c, int n_tokens) {
   p.unit = p.rows == 32 ? 128 : f32 ? 32 : 64;
   p.tiles = S + (long)n_tokens * G / p.rows;
   const long units = ((long)c.max_pages_per_seq * c.page_size + p.unit - 1) / p.unit;
-  const long most = p.tiles * units * c.num_kv_heads;  // (tokens x KV heads are below 2^31)
-  p.split = p.tiles <= kTiles && most <= 0x7fffffffL - kTreeBlocks;
+  const long most = p.tiles * units * c.num_kv_heads;
+  p.split = p.tiles <= kTiles && most <= 0x7fffffffL / 32;  // (a unit weighs up to 20)
   if (p.split) {
     const long fill = p.rows == 256 ? kTreeBlocks / 2 : kTreeBlocks;
     p.blocks = (int)(most < fill ? (most + 7) / 8 * 8 : fill);
