@@ -161,6 +161,39 @@ def test_tree_many_sequences(rows, q):
         assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
 
 
+@pytest.mark.parametrize("new,G,q", [(6, 8, "bf16"), (10, 8, "bf16"), (17, 8, "bf16"), (10, 8, "fp32"), (1, 16, "fp32")])
+def test_tree_more_tiles_than_are_cut_into_shares(new, G, q):
+    """520 sequences: every tile size with a block for each item."""
+    print(f"[tree] 520 x {new} tokens, G={G} {q}", flush=True)
+    b = Batch([(29 * s) % 50 for s in range(520)], [new - s % 2 if new > 1 else 1 for s in range(520)], H=1, G=G, P=16,
+              q=q, kv=q, seed=new, pad=1)
+    b.check("bf16" if new == 17 else "fp32")
+
+
+@pytest.mark.parametrize("new,G", [(300, 1), (300, 7), (520, 2)])
+@pytest.mark.parametrize("bad", [None, float("nan")])
+def test_tree_masks_wider_than_the_block_holds(new, G, bad):
+    """Trees of more than 256 tokens, whose masks are read from memory, over several tiles."""
+    b = Batch([77], [new], H=1, G=G, P=64, seed=G)
+    o0, l0 = b.check("bf16")
+    if bad is not None:
+        j = new - 40
+        b.v[int(b.table[0, (77 + j) // 64]), :, (77 + j) % 64, 5] = bad
+        o1, l1 = b.run("bf16")
+        sees = np.array([bool(int(b.mask[i, j // 32]) >> (j % 32) & 1) for i in range(new)])
+        assert sees.any() and torch.equal(o0[~sees], o1[~sees]) and bool(o1[sees][..., 5].isnan().all())
+
+
+def test_tree_rows_do_not_depend_on_others():
+    """A row's bits are the same whatever the other rows of its tile are."""
+    b = Batch([600, 90], [40, 9], seed=8)
+    o0, l0 = b.run()
+    b.q[::2] *= 30
+    o1, l1 = b.run()
+    assert torch.equal(o0[1::2], o1[1::2]) and torch.equal(l0[1::2], l1[1::2])
+    assert not torch.equal(o0[::2], o1[::2])
+
+
 def test_tree_equals_dense_attention_for_single_tokens():
     b = Batch([900, 64, 4000], [1, 1, 1], G=8, mask=None, ragged=False)
     o, lse = b.check()
@@ -314,6 +347,21 @@ def test_token_mass_decay_and_many_sequences(decay):
     print(f"[mass] decay={decay}", flush=True)
     _mass_case([(37 * s) % 90 for s in range(300)], [1] * 300, "bf16", "bf16", None, 2, 16, H=1, decay=decay, pad=0)
     _mass_case([0, 3, 1200], [4, 0, 2], "bf16", "bf16", "tree", 4, 32, decay=decay)
+
+
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+def test_token_mass_of_more_sequences_than_are_counted(q):
+    """Beyond 512 sequences a block takes whole lists."""
+    print(f"[mass] 600 sequences {q}", flush=True)
+    _mass_case([(53 * s) % 300 for s in range(600)], [s % 3 for s in range(600)], q, q, "tree", 2, 16, H=1, pad=1)
+
+
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+@pytest.mark.parametrize("mask", ["tree", None])
+def test_token_mass_of_many_rows(q, mask):
+    """More rows than LDS holds at once; trees wider than a word."""
+    print(f"[mass] many rows {q} {mask}", flush=True)
+    _mass_case([30, 0, 513], [150, 90, 33], q, q, mask, 4, 64, decay=0.25)
 
 
 def test_token_mass_of_rows_that_see_nothing_and_of_bad_keys():
@@ -625,6 +673,35 @@ def test_two_streams_at_once():
         torch.cuda.synchronize()
         for g, w in zip(got, want):
             assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])
+
+
+def test_a_workspace_serves_fewer_tokens():
+    """One workspace for the largest step, used for smaller ones, other contents left in it."""
+    big = Batch([100, 300], [64, 64], seed=1)
+    ws = T.alloc_tree_workspace(big.cfg, 20000)
+    ws.fill_(255)
+    for new in ([64, 64], [1, 1], [9, 2], [20, 15]):
+        b = Batch([100, 300], new, seed=sum(new))
+        d = b.dev()
+        assert T.tree_workspace_bytes(b.cfg, b.n) <= ws.numel()
+        got = T.tree_attend(b.cfg, d["q"], d["k"], d["v"], d["pt"], d["sl"], ws, cu_tokens=d["cu"], mask=d["mask"])
+        b.check(got=(got[0].cpu(), got[1].cpu()))
+
+
+def test_a_bad_page_is_read_as_block_zero_or_left_out():
+    """Without table checks: a block outside the cache is never read."""
+    b = Batch([100], [5], seed=3)
+    d = b.dev()
+    k0 = b.table.clone()
+    d["pt"][0, 2] = 1 << 30
+    out, lse = T.tree_attend(b.cfg, d["q"], d["k"], d["v"], d["pt"], d["sl"], d["ws"], cu_tokens=d["cu"], mask=d["mask"])
+    b.table[0, 2] = 0
+    b.check(got=(out.cpu(), lse.cpu()))
+    b.table = k0
+    mass = T.alloc_mass(b.cfg)
+    mass.fill_(2.0)
+    T.token_mass(b.cfg, d["q"], lse, d["k"], d["pt"], d["sl"], mass, cu_tokens=d["cu"], mask=d["mask"])
+    assert bool((mass[0, :, 32:48] == 2.0).all()) and bool((mass[0, :, :32] != 2.0).all())
 
 
 def test_the_same_inputs_twice_give_the_same_bits():
