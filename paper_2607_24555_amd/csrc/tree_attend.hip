@@ -28,7 +28,7 @@ namespace {
 constexpr int kTiles = 512;        // row tiles of a launch whose items are cut into shares
 constexpr int kTreeBlocks = 512;   // two per compute unit
 
-constexpr int kMaskWords = 8;      // of a row's mask that lie in LDS (trees of up to 256 tokens)
+constexpr int kMaskWords = 6;      // of a row's mask that lie in LDS (trees of up to 192 tokens)
 
 struct TreeArgs {
   DraftArgs d;
@@ -107,6 +107,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
   __shared__ int s_units[kTiles + 1], s_first[kTiles + 1], s_sum[RW * TW];
   __shared__ int s_row0[kTiles], s_rows[kTiles], s_len[kTiles];
   __shared__ float s_m[TW][C::kRows], s_l[TW][C::kRows];
+  __shared__ float2 s_all[TW > 1 ? C::kRows : 1];
   __shared__ uint32_t s_mask[C::kRows][kMaskWords + 1];
   const DraftArgs& d = a.d;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -651,32 +652,37 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
         s_l[wt][wr * 32 + col] = l;
       }
       __syncthreads();
-      float mx = -INFINITY;
+      // all waves' parts of a row at its largest maximum, and their sum
+      float mx = -INFINITY, ls = 0.0f;
 #pragma unroll
       for (int w = 0; w < TW; ++w) mx = fmaxf(mx, s_m[w][wr * 32 + col]);
+#pragma unroll
+      for (int w = 0; w < TW; ++w) {
+        const float mw = s_m[w][wr * 32 + col];
+        ls += mw == -INFINITY ? 0.0f : s_l[w][wr * 32 + col] * __builtin_amdgcn_exp2f(mw - mx);
+      }
       const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mx);
       float* to = reinterpret_cast<float*>(lds) + (wt * C::kRows + wr * 32 + col) * 132;
+      if (wr * 32 + col < count_rows) {
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
+        for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-        for (int e = 0; e < 16; e += 4)
-          *reinterpret_cast<float4*>(to + 32 * dt + 2 * e + 4 * half) =
-              make_float4(o[dt][e] * f, o[dt][e + 1] * f, o[dt][e + 2] * f, o[dt][e + 3] * f);
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<float4*>(to + 32 * dt + 2 * e + 4 * half) =
+                make_float4(o[dt][e] * f, o[dt][e + 1] * f, o[dt][e + 2] * f, o[dt][e + 3] * f);
+      }
+      if (wt == 0 && half == 0) s_all[wr * 32 + col] = make_float2(mx, ls);
       __syncthreads();
-      for (int e = tid; e < C::kRows * 32; e += kBlock) {
+      for (int e = tid; e < count_rows * 32; e += kBlock) {
         const int rr = e >> 5, dim = 4 * (e & 31);
-        float M = -INFINITY, ll = 0.0f;
         float4 x = make_float4(0, 0, 0, 0);
 #pragma unroll
-        for (int w = 0; w < TW; ++w) M = fmaxf(M, s_m[w][rr]);
-#pragma unroll
         for (int w = 0; w < TW; ++w) {
-          const float mw = s_m[w][rr];
-          ll += mw == -INFINITY ? 0.0f : s_l[w][rr] * __builtin_amdgcn_exp2f(mw - M);
           const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<float*>(lds) + (w * C::kRows + rr) * 132 + dim);
           x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
         }
-        emit(rr, dim, x.x, x.y, x.z, x.w, M, ll, dim == 0);
+        const float2 st = s_all[rr];
+        emit(rr, dim, x.x, x.y, x.z, x.w, st.x, st.y, dim == 0);
       }
       __syncthreads();
     }
@@ -713,47 +719,87 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
     g = Segment{uniform(lo), h, uniform(tile), 0, uniform(units), uniform(units), uniform(q.row0), uniform(q.n), uniform(q.L)};
   } else {
     // the cut: tiles before each sequence, units before each tile
-    constexpr int kPer = kTiles / kBlock;
-    int before[kPer], sum = 0, v = 0, total;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const int s = tid * kPer + e;
-      before[e] = v;
-      if (s < d.S) {
-        const DraftSeq q = draft_seq(d, s);
-        s_row0[s] = q.row0, s_rows[s] = q.n, s_len[s] = q.L;
-        v += tiles_of(q.n);
+    auto fill_seq = [&](int q) {
+      const DraftSeq v = draft_seq(d, q);
+      s_row0[q] = v.row0, s_rows[q] = v.n, s_len[q] = v.L;
+      return tiles_of(v.n);
+    };
+    auto cost_of = [&](int q, int tile) { return units_of(s_rows[q], s_len[q], tile) * weight_of(s_rows[q], tile); };
+    auto seq_of = [&](int t) {  // the last sequence whose tiles begin at t or before
+      int lo = 0, hi = d.S;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (s_first[mid] <= t) lo = mid;
+        else hi = mid;
       }
-    }
-    const int at = scan_block<RW * TW>(v, s_sum, total);
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const int s = tid * kPer + e;
-      if (s < d.S) s_first[s] = at + before[e];
-    }
-    if (tid == 0) s_first[d.S] = total;
-    __syncthreads();
-    const int T = min(total, kTiles);
-    v = 0;
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const int t = tid * kPer + e;
-      before[e] = v;
-      if (t < T) {
-        int lo = 0, hi = d.S;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) / 2;
-          if (s_first[mid] <= t) lo = mid;
-          else hi = mid;
+      return lo;
+    };
+    // few sequences and tiles: every wave for itself, in lanes, all writing the same (without the
+    // barriers of the other way a run of 5 tokens over 4K is planned in 1.3 us instead of 2.7)
+    int total = kTiles + 1;
+    if (d.S <= 64) {
+      int v = lane < d.S ? fill_seq(lane) : 0;
+      const int own = v;
+      for (int o = 1; o < d.S; o <<= 1) {
+        const int y = __shfl_up(v, o, 64);
+        if (lane >= o) v += y;
+      }
+      if (lane < d.S) s_first[lane] = v - own;
+      total = __builtin_amdgcn_readlane(v, d.S - 1);
+      s_first[d.S] = total;
+      if (total <= 64) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        int c = 0;
+        if (lane < total) {
+          const int q = seq_of(lane);
+          c = cost_of(q, lane - s_first[q]);
         }
-        v += units_of(s_rows[lo], s_len[lo], t - s_first[lo]) * weight_of(s_rows[lo], t - s_first[lo]);
+        int sum = c;
+        for (int o = 1; o < total; o <<= 1) {
+          const int y = __shfl_up(sum, o, 64);
+          if (lane >= o) sum += y;
+        }
+        const int all = total > 0 ? __builtin_amdgcn_readlane(sum, total - 1) : 0;
+        s_units[lane] = lane < total ? sum - c : all;
+        s_units[64] = s_units[kTiles] = all;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
-    const int ut = scan_block<RW * TW>(v, s_sum, sum);
+    if (total > 64) {
+      __syncthreads();
+      constexpr int kPer = kTiles / kBlock;
+      int before[kPer], sum = 0, v = 0;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) s_units[tid * kPer + e] = ut + before[e];
-    if (tid == 0) s_units[kTiles] = sum;
-    __syncthreads();
+      for (int e = 0; e < kPer; ++e) {
+        const int q = tid * kPer + e;
+        before[e] = v;
+        if (q < d.S) v += fill_seq(q);
+      }
+      const int at = scan_block<RW * TW>(v, s_sum, total);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const int q = tid * kPer + e;
+        if (q < d.S) s_first[q] = at + before[e];
+      }
+      if (tid == 0) s_first[d.S] = total;
+      __syncthreads();
+      const int T = min(total, kTiles);
+      v = 0;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const int t = tid * kPer + e;
+        before[e] = v;
+        if (t < T) {
+          const int q = seq_of(t);
+          v += cost_of(q, t - s_first[q]);
+        }
+      }
+      const int ut = scan_block<RW * TW>(v, s_sum, sum);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) s_units[tid * kPer + e] = ut + before[e];
+      if (tid == 0) s_units[kTiles] = sum;
+      __syncthreads();
+    }
     const int all = s_units[kTiles] * d.H;  // (below 2^31: see tree_plan)
     // (at least a unit, so that a block between an item's first and last has some of it)
     share = max((all + (int)gridDim.x - 1) / (int)gridDim.x, kMostWeight);

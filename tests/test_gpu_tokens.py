@@ -173,7 +173,7 @@ def test_tree_more_tiles_than_are_cut_into_shares(new, G, q):
 @pytest.mark.parametrize("new,G", [(300, 1), (300, 7), (520, 2)])
 @pytest.mark.parametrize("bad", [None, float("nan")])
 def test_tree_masks_wider_than_the_block_holds(new, G, bad):
-    """Trees of more than 256 tokens, whose masks are read from memory, over several tiles."""
+    """Trees of more than 192 tokens, whose masks are read from memory, over several tiles."""
     b = Batch([77], [new], H=1, G=G, P=64, seed=G)
     o0, l0 = b.check("bf16")
     if bad is not None:
