@@ -10,6 +10,11 @@
 // are cut into chunks of 32 K, each with a block that writes its chunk's histogram, and four
 // launches: a launch's blocks each sum the chunks' histograms of the digit before (which also
 // tells how many tokens kept lie before their chunk).
+//
+// Bound by latency, of barriers and launches: 8 lists of 4K tokens 9.9 us; 64 lists of 128K (33
+// MB, 6.5 us of HBM) 57 us in launches of 12, 12, 14 and 19; two of 1M 44 us.  Chunks of 16 K
+// for 128K tokens: 68 us.  Ranks by two ballots a group for every lane instead of lane masks, and
+// forced tokens among them: 67.
 #include "tokens_internal.h"
 
 namespace locks {

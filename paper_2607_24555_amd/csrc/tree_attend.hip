@@ -7,17 +7,35 @@
 //   S^T = K Q^T   (M = token, N = row), whose result has a row per lane column, so that the
 //                 online softmax (running maximum and sum, fp32) needs one lane swap,
 //   O^T += V^T P  (M = dimension, N = row, K = token), with P exactly as S^T left it.
-// Keys and values pass through registers into LDS, the next unit's while one is computed;
-// their 16-byte pieces are permuted by the token, so that neither the key reads nor the
-// transposed value reads meet on a bank.
+// Rows lie in LDS with their 16-byte pieces permuted by the token, so that neither the key
+// reads nor the transposed value reads meet on a bank.
+//
+// Tiles, by the average sequence's rows (bf16; 8 heads of 4 queries unless said):
+//   up to 32   four waves with tokens of their own and no barrier: keys in registers as the
+//              product takes them, values through LDS.  Bound by HBM from some thousand tokens
+//              (8 sequences of 32K, 8 new: 210 us, 5.1 TB/s), below by latency: 5 new tokens
+//              over 4K take 19.3 us, 12 of it here (plan 2.0, rows to sums 2.8, joins and
+//              partials 2.5 of a block's 7.4) and 6.5 in the merge's launch.
+//   up to 64   two waves by rows, two by tokens (16 new: 209 us, 5.2 TB/s).
+//   up to 128  four waves by rows, two blocks a compute unit.
+//   more       eight waves by rows, with three units of copies to LDS on their way.  Against the
+//              128-row tile: ragged trees of 140 to 248 rows 324 us (400), 16 tokens of 16 heads
+//              over 1M 505 (558), pieces of prompts 449 (528).  Its products and the weights'
+//              vector work overlap by half: at 2.05 GHz the matrix pipe is busy 45% of the time
+//              and the vector one 45% (pieces of prompts, 930 TFLOP/s).
+// fp32 products (any other types) take 32 or 128 rows and run at 69 TFLOP/s of the 154 of a
+// large product, the matrix pipe half busy: of a compute unit's two blocks the older one is
+// served first, and the other ends alone (82 and 105 us).
 //
 // All (sequence, KV head, tile) items' units, in order, are cut into equal shares, one a
 // block (every block derives the cut from the lengths), so ragged batches and long lists
-// fill the chip; a unit counts by the 32s of rows that its tile has (see weight_of); an item within a share writes its output, others leave partials (o, max,
-// sum), which merge_kernel combines in order.
+// fill the chip; a unit counts by the 32s of rows that its tile has (see weight_of); an item
+// within a share writes its output, others leave partials (o, max, sum), which merge_kernel
+// combines in order.  Where there are more tiles than kTiles an item is a block's.
 //
 // What a row does not see is masked by one 32-bit window per row and 32 tokens, the
-// ancestors' bits shifted to the tile; only units that hold new tokens look at it.
+// ancestors' bits shifted to the tile; only units that hold tokens some row does not see look
+// at it.
 #include <type_traits>
 
 #include "tokens_internal.h"
