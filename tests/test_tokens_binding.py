@@ -93,6 +93,14 @@ def test_null_arguments_and_empty_batches(lib):
     assert _mass(lib, c, draft(), decay=float("nan")) == _mass(lib, c, draft(), decay=float("inf")) == -1
 
 
+def test_blocks_of_four_gigabytes_are_refused(lib):
+    for dt, code in ((1, -2), (0, 0)):     # fp32: 2^32 bytes of a page over all heads; bf16: half
+        c = cfg(num_seqs=1, num_kv_heads=1 << 17, num_q_heads=1 << 17, page_size=64, max_pages_per_seq=1,
+                kv_dtype=dt, q_dtype=dt).c()
+        d = draft(n_tokens=0)
+        assert (_tree(lib, c, d), _mass(lib, c, d)) == (code, code)
+
+
 def test_workspaces(lib):
     c = cfg().c()
     need = lib.locks_tree_workspace_bytes(_ref(c), 5)
