@@ -14,10 +14,12 @@
  *
  * Pointers to rows, caches and outputs must be 16-byte aligned and row strides a multiple of
  * 16 bytes; LOCKS_E_INVAL otherwise.  Lengths are held to [0, B * max_pages_per_seq] and row
- * ranges to [0, n_tokens] by the kernels; a page whose block lies outside [0, num_blocks) is
- * read as block 0 by locks_tree_attend (with table checks on it is reported, see
- * locks_set_table_checks) and left out by locks_token_mass and locks_keep_tokens.  The calls
- * touch no summaries, so they take caches whose summary store would be too large too.
+ * ranges to [0, n_tokens] by the kernels (of cu_tokens that do not ascend rows may be wrong
+ * or not written, but nothing outside the buffers is accessed); a page whose block lies
+ * outside [0, num_blocks) is read as block 0 by locks_tree_attend (with table checks on it is
+ * reported, see locks_set_table_checks) and left out by locks_token_mass and
+ * locks_keep_tokens.  The calls touch no summaries, so they take caches whose summary store
+ * would be too large too.
  */
 #ifndef LOCKS_TOKENS_H
 #define LOCKS_TOKENS_H
@@ -63,9 +65,10 @@ size_t locks_tree_workspace_bytes(const locks_cfg_t* cfg, int32_t n_tokens);
  * the product with the values as bf16: for fp32 outputs in three terms (2^-24 of a weight), for
  * bf16 ones in one (2^-8, as their own rounding) or two; other types are computed in fp32
  * throughout.
- * Returns LOCKS_E_INVAL for a null or misaligned pointer, a bad stride or count, and
- * LOCKS_E_UNSUPPORTED for another out_dtype, or for n_tokens * H_q or a table's tokens over
- * all sequences and KV heads of 2^31 or more. */
+ * Returns LOCKS_E_INVAL for a null or misaligned pointer, a bad stride or count or out == q,
+ * and LOCKS_E_UNSUPPORTED for another out_dtype, for n_tokens * H_q or the tables' tokens
+ * over all sequences and KV heads of 2^31 or more, masks of more than 2^25 words a row, or a
+ * block of 4 GiB or more (all KV heads of a page). */
 int locks_tree_attend(const locks_cfg_t* cfg, const locks_draft_t* draft, const void* k_cache,
                       const void* v_cache, const int32_t* page_table, const int32_t* seq_lens,
                       void* out, int32_t out_dtype, float* out_lse, void* ws, size_t ws_bytes,

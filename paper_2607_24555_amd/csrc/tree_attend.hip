@@ -797,9 +797,9 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
         const int q = tid * kPer + e;
-        if (q < d.S) s_first[q] = at + before[e];
+        if (q < d.S) s_first[q] = min(at + before[e], kTiles);  // (more: cu that do not ascend)
       }
-      if (tid == 0) s_first[d.S] = total;
+      if (tid == 0) s_first[d.S] = min(total, kTiles);
       __syncthreads();
       const int T = min(total, kTiles);
       v = 0;

@@ -170,6 +170,25 @@ def test_tree_more_tiles_than_are_cut_into_shares(new, G, q):
     b.check("bf16" if new == 17 else "fp32")
 
 
+def test_tree_row_ranges_that_do_not_ascend():
+    # every second sequence claims all rows, over the same pages: 750 tiles where ascending ranges
+    # would have 305 at most
+    S, n = 300, 40
+    b = Batch([20], [n], seed=37)
+    want, lse = b.run()
+    d = dict(b.d)
+    b.cfg.num_seqs = S
+    pt, sl = d["pt"].expand(S, -1).contiguous(), d["sl"].expand(S).contiguous()
+    cu = torch.tensor([n * (s & 1) for s in range(S + 1)], dtype=torch.int32).cuda()
+    ws, out = T.alloc_tree_workspace(b.cfg, n), torch.full_like(want, 7.0).cuda()
+    _, l = T.tree_attend(b.cfg, d["q"], d["k"], d["v"], pt, sl, ws, cu_tokens=cu, mask=d["mask"], out=out)
+    m = T.token_mass(b.cfg, d["q"], l, d["k"], pt, sl, T.alloc_mass(b.cfg), cu_tokens=cu, mask=d["mask"])
+    torch.cuda.synchronize()
+    assert (m[1::2] == 0).all() and (m[::2] == m[0]).all()
+    b.cfg.num_seqs = 1
+    b.check(got=(out.cpu(), l.cpu()))
+
+
 @pytest.mark.parametrize("new,G", [(300, 1), (300, 7), (520, 2)])
 @pytest.mark.parametrize("bad", [None, float("nan")])
 def test_tree_masks_wider_than_the_block_holds(new, G, bad):
