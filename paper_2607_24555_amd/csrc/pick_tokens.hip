@@ -88,22 +88,38 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   }
   const int lo = a.n_sink, hi = L - a.n_recent;  // the candidates (lo < hi as L > n_keep)
   const float* x = a.mass + list * a.width;
-  uint32_t key[kKeys];
-#pragma unroll
-  for (int e = 0; e < kKeys; ++e) key[e] = __float_as_uint(x[min(i0 + 64 * e, L - 1)]);
   auto open = [&](int e) { return i0 + 64 * e >= lo && i0 + 64 * e < hi; };
 
   uint32_t prefix = 0;                              // T's digits so far
   int left = a.n_keep - a.n_sink - a.n_recent;      // to keep of the tokens that have them
   int above = 0;                                    // of earlier chunks, tokens above T's digits
   bool all = false;                                 // every token that has them is kept
-  if (kPhase > 0) {
+  if (kPhase > 1) {
     const int32_t* st = a.state + (list * a.chunks + chunk) * 4;
-    if (kPhase > 1) prefix = (uint32_t)st[0], left = st[1], above = st[2], all = st[3] != 0;
+    prefix = (uint32_t)st[0], left = st[1], above = st[2], all = st[3] != 0;
   }
   const bool none = a.n_keep == a.n_sink + a.n_recent;
+  // the chunks' histograms of the digit before (this thread's two bins over all chunks, and over
+  // the earlier ones), requested before the masses, so that the bin is found while those are on
+  // their way; where every token is kept already they hold anything, and are not used
+  int h0 = 0, h1 = 0, p0 = 0, p1 = 0;
+  if (kPhase > 0) {
+    const uint16_t* hist = a.hist + ((kPhase - 1) * a.lists + list) * a.chunks * kBins;
+#pragma unroll 16
+    for (int c = 0; c < a.chunks; ++c) {
+      const uint32_t v = reinterpret_cast<const uint32_t*>(hist + (long)c * kBins)[kPickBlock - 1 - tid];
+      h0 += v >> 16, h1 += v & 0xffffu;
+      if (c < chunk) p0 += v >> 16, p1 += v & 0xffffu;
+    }
+  }
+  uint32_t key[kKeys];
 #pragma unroll
-  for (int e = 0; e < kKeys; ++e) key[e] = mass_key(__uint_as_float(key[e]));
+  for (int e = 0; e < kKeys; ++e) key[e] = __float_as_uint(x[min(i0 + 64 * e, L - 1)]);
+  auto arrived = [&] {
+#pragma unroll
+    for (int e = 0; e < kKeys; ++e) key[e] = mass_key(__uint_as_float(key[e]));
+  };
+  if (kPhase <= 0) arrived();
 
   auto shift_of = [](int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; };
   // counts digit d of the tokens whose higher digits are T's
@@ -153,14 +169,6 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   }
   if (kPhase > 0 && !none && !all) {
     const int d = kPhase - 1;
-    const uint16_t* hist = a.hist + (d * a.lists + list) * a.chunks * kBins;
-    int h0 = 0, h1 = 0, p0 = 0, p1 = 0;
-#pragma unroll 16
-    for (int c = 0; c < a.chunks; ++c) {
-      const uint32_t v = reinterpret_cast<const uint32_t*>(hist + (long)c * kBins)[kPickBlock - 1 - tid];
-      h0 += v >> 16, h1 += v & 0xffffu;
-      if (c < chunk) p0 += v >> 16, p1 += v & 0xffffu;
-    }
     choose(d, h0, h1, p0, p1);
     if (kPhase == 3) {
       int sum;
@@ -172,6 +180,7 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
       st[0] = (int32_t)prefix, st[1] = left, st[2] = above, st[3] = all;
     }
   }
+  if (kPhase > 0) arrived();
   if (kPhase >= 0 && kPhase < 3) {
     if (none || all) return;
     count(kPhase);

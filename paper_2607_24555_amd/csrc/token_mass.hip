@@ -11,9 +11,9 @@
 // wide table of short sequences costs what its tokens cost; a run mostly stays with one KV
 // head, whose queries then stay in LDS.  Of more sequences a block takes whole lists.
 //
-// Bound by HBM: 64 sequences of 1.5K to 8K tokens, 8 heads, a new token each: 126 us, 4.9 TB/s
+// Bound by HBM: 64 sequences of 1.5K to 8K tokens, 8 heads, a new token each: 128 us, 4.9 TB/s
 // (a copy here 5.1).  Keys read in the product's order, 32 bytes of each of 32 rows a load, took
-// 154.  With 128 rows (the last 32 tokens of prompts of 20K to 32K) 118 us, 3.7 TB/s: 16 powers
+// 154.  With 128 rows (the last 32 tokens of prompts of 20K to 32K) 120 us, 3.7 TB/s: 16 powers
 // a lane and 32 x 32 logits take as long as their keys.
 #include <type_traits>
 
