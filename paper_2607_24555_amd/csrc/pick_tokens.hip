@@ -11,8 +11,8 @@
 // launches: a launch's blocks each sum the chunks' histograms of the digit before (which also
 // tells how many tokens kept lie before their chunk).
 //
-// Bound by latency, of barriers and launches: 8 lists of 4K tokens 9.9 us; 64 lists of 128K (33
-// MB, 6.5 us of HBM) 57 us in launches of 12, 12, 14 and 19; two of 1M 44 us.  Chunks of 16 K
+// Bound by latency, of barriers and launches: 8 lists of 4K tokens 10.4 us; 64 lists of 128K (33
+// MB, 6.5 us of HBM) 56 us in launches of 12, 12, 14 and 19; two of 1M 44 us.  Chunks of 16 K
 // for 128K tokens: 68 us.  Ranks by two ballots a group for every lane instead of lane masks, and
 // forced tokens among them: 67.
 #include "tokens_internal.h"
@@ -67,7 +67,10 @@ __device__ __forceinline__ int block_scan(int v, int* lds, int& sum) {
 // kPhase -1: the whole of it.  0, 1, 2: the histogram of that digit; 3: the output.
 template <int kKeys, int kPhase>
 __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
-  __shared__ int s_hist[kBins], s_wave[kWaves], s_bin, s_left, s_all;
+  // copies of the first digit's bins, by lane: masses of a list share few exponents, so that a
+  // wave's additions would meet (64 lists of 128K: 55.9 us instead of 57.4)
+  constexpr int kCopies = kPhase == 0 ? 8 : 1;
+  __shared__ int s_hist[kBins * kCopies], s_wave[kWaves], s_bin, s_left, s_all;
   const long list = blockIdx.x / a.chunks;
   const int chunk = blockIdx.x % a.chunks, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int L = min(max(a.seq_lens[list / a.H], 0), a.width);
@@ -88,7 +91,12 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   }
   const int lo = a.n_sink, hi = L - a.n_recent;  // the candidates (lo < hi as L > n_keep)
   const float* x = a.mass + list * a.width;
-  auto open = [&](int e) { return i0 + 64 * e >= lo && i0 + 64 * e < hi; };
+  // bit e: token i0 + 64 e is a candidate (a register a lane; as masks of lanes they spill)
+  uint32_t in_range = 0;
+#pragma unroll
+  for (int e = 0; e < kKeys; ++e) in_range |= i0 + 64 * e >= lo && i0 + 64 * e < hi ? 1u << e : 0u;
+  asm volatile("" : "+v"(in_range));
+  auto open = [&](int e) { return (in_range >> e & 1u) != 0; };
 
   uint32_t prefix = 0;                              // T's digits so far
   int left = a.n_keep - a.n_sink - a.n_recent;      // to keep of the tokens that have them
@@ -124,8 +132,8 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   auto shift_of = [](int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; };
   // counts digit d of the tokens whose higher digits are T's
   auto count = [&](int d) {
-    s_hist[tid] = 0;
-    s_hist[tid + kPickBlock] = 0;
+#pragma unroll
+    for (int e = 0; e < kCopies * kBins / kPickBlock; ++e) s_hist[tid + e * kPickBlock] = 0;
     __syncthreads();
     const int shift = shift_of(d), mask = d == 2 ? 1023 : 2047;
     int zeros = 0;  // counted by ballots: as one bin's additions they would queue
@@ -134,9 +142,9 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
       const bool in = open(e) && (d == 0 || key[e] >> (d == 1 ? 21 : 10) == prefix >> (d == 1 ? 21 : 10));
       const bool zero = key[e] == kZeroKey;
       zeros += (int)__popcll(__ballot(in && zero));
-      if (in && !zero) atomicAdd(&s_hist[key[e] >> shift & mask], 1);
+      if (in && !zero) atomicAdd(&s_hist[(key[e] >> shift & mask) * kCopies + lane % kCopies], 1);
     }
-    if (lane == 0 && zeros) atomicAdd(&s_hist[kZeroKey >> shift & mask], zeros);
+    if (lane == 0 && zeros) atomicAdd(&s_hist[(kZeroKey >> shift & mask) * kCopies], zeros);
     __syncthreads();
   };
   // the bin of digit d in which the count from above passes `left`; h: this thread's two bins,
@@ -185,7 +193,11 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
     if (none || all) return;
     count(kPhase);
     uint16_t* to = a.hist + ((kPhase * a.lists + list) * a.chunks + chunk) * kBins;
-    reinterpret_cast<uint32_t*>(to)[tid] = (uint32_t)s_hist[2 * tid] | (uint32_t)s_hist[2 * tid + 1] << 16;
+    uint32_t n0 = 0, n1 = 0;
+#pragma unroll
+    for (int e = 0; e < kCopies; ++e)
+      n0 += s_hist[2 * tid * kCopies + e], n1 += s_hist[(2 * tid + 1) * kCopies + e];
+    reinterpret_cast<uint32_t*>(to)[tid] = n0 | n1 << 16;
     return;
   }
 
