@@ -248,6 +248,14 @@ __global__ __launch_bounds__(256, kF32 ? 1 : 2) void mass_kernel(DraftArgs a, co
 #pragma unroll
         for (int e = 0; e < 16; ++e) z[e] = 0.0f;
         const unsigned char* qp = s_q + (32 * c + col) * kRow;
+        // among the new tokens: which of the wave's 32 tokens row 32 c + col sees
+        const int tb = w.u * kUnit + wave * 32;
+        const bool tail = tb + 31 >= first;
+        uint32_t seen = ~0u;
+        if (tail) {
+          const int i = s_i[32 * c + col];
+          seen = draft_window(a, w.row0 + i, i, tb - first, w.L - tb);
+        }
         if constexpr (kF32) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) {
@@ -281,12 +289,14 @@ __global__ __launch_bounds__(256, kF32 ? 1 : 2) void mass_kernel(DraftArgs a, co
         uint32_t on = 0;  // of this lane's 16 rows, those that count
 #pragma unroll
         for (int e = 0; e < 16; ++e) on |= nl[e] != -INFINITY ? 1u << e : 0u;
-        if (w.u * kUnit + wave * 32 + 31 >= first) {
+        if (tail) {  // a bit of each of this lane's rows, from the lane that has the row
 #pragma unroll 1
-          for (int e = 0; e < 16; ++e) {
-            const int i = s_i[32 * c + 8 * (e / 4) + 4 * half + e % 4];
-            if (on >> e & 1u && !(t < w.L && draft_sees(a, w.row0 + i, i, t, first))) on &= ~(1u << e);
-          }
+          for (int e0 = 0; e0 < 16; e0 += 4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t y = __shfl(seen, 2 * e0 + 4 * half + e, 64);
+              on &= ~((~y >> col & 1u) << (e0 + e));
+            }
         }
         if (__all(on == 0xffffu)) {
 #pragma unroll

@@ -38,13 +38,21 @@ __device__ __forceinline__ DraftSeq draft_seq(const DraftArgs& a, int s) {
 __device__ __forceinline__ int draft_len(const DraftArgs& a, int s) {
   return min(max(a.seq_lens[s], 0), a.max_pages * a.pgsz);
 }
-// Whether new token i (mask row `row`) sees token t, `first` being the first new token's
-// index (t < L is the caller's).
-__device__ __forceinline__ bool draft_sees(const DraftArgs& a, int row, int i, int t, int first) {
-  const int j = t - first;
-  if (j < 0) return true;
-  if (!a.mask) return j <= i;
-  return j < 32 * a.words && (a.mask[(long)row * a.words + (j >> 5)] >> (j & 31) & 1);
+// Which of the 32 tokens from new token j0 on (j0 > -32) new token i (mask row `row`) sees, `left`
+// of them up to the sequence's end.
+__device__ __forceinline__ uint32_t draft_window(const DraftArgs& a, int row, int i, int j0, int left) {
+  if (left <= 0) return 0u;
+  uint32_t seen = j0 < 0 ? (1u << -j0) - 1u : 0u;
+  if (a.mask) {
+    const uint32_t* mask = a.mask + (long)row * a.words;
+    const int w = j0 >> 5, sh = j0 & 31;
+    const uint32_t lo = (unsigned)w < (unsigned)a.words ? mask[w] : 0u;
+    const uint32_t hi = (unsigned)(w + 1) < (unsigned)a.words ? mask[w + 1] : 0u;
+    seen |= sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
+  } else if (i >= j0) {
+    seen |= i - j0 >= 31 ? ~0u : (2u << (i - j0)) - 1u;
+  }
+  return left >= 32 ? seen : seen & ((1u << left) - 1u);
 }
 
 // Exclusive prefix sum of one value a thread over a block of kWaves waves; total in `sum`.
