@@ -1001,9 +1001,14 @@ Plan tree_plan(const locks_cfg_t& c, int n_tokens) {
   p.rows = rows <= 32 ? 32 : f32 ? 128 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   p.unit = p.rows == 32 ? 128 : f32 ? 32 : 64;
   p.tiles = S + (long)n_tokens * G / p.rows;
-  const long units = ((long)c.max_pages_per_seq * c.page_size + p.unit - 1) / p.unit;
+  const long width = (long)c.max_pages_per_seq * c.page_size, units = (width + p.unit - 1) / p.unit;
   const long most = p.tiles * units * c.num_kv_heads;
-  p.split = p.tiles <= kTiles && most <= 0x7fffffffL / 32;  // (a unit weighs up to 20)
+  // short tables: a block goes through an item's tokens sooner than a second launch joins its
+  // parts (5 new tokens, 8 heads, tables of 512: 12.8 us, cut 14.2; of 1,024 17.6 and 14.5;
+  // 16 sequences 16.4 and 24.2; fp32 trees of 30, tables of 128: 30.1 and 30.6, of 256 46.9 and
+  // 43.0; where the sequences are short all of these are 3 to 8 us less without the cut)
+  const long alone = !f32 ? 512 : p.rows == 32 ? 256 : 128;
+  p.split = width > alone && p.tiles <= kTiles && most <= 0x7fffffffL / 32;  // (a unit weighs up to 20)
   if (p.split) {
     const long fill = p.rows == 256 ? kTreeBlocks / 2 : kTreeBlocks;
     p.blocks = (int)(most < fill ? (most + 7) / 8 * 8 : fill);

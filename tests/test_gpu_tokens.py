@@ -174,7 +174,7 @@ def test_tree_row_ranges_that_do_not_ascend():
     # every second sequence claims all rows, over the same pages: 750 tiles where ascending ranges
     # would have 305 at most
     S, n = 300, 40
-    b = Batch([20], [n], seed=37)
+    b = Batch([20], [n], seed=37, extra=40)   # (tables of more than 512 tokens)
     want, lse = b.run()
     d = dict(b.d)
     b.cfg.num_seqs = S
@@ -263,6 +263,60 @@ def test_tree_unseen_tokens_do_not_reach_a_row(q, new, bad):
     assert torch.equal(o0[~sees], o1[~sees]) and torch.equal(l0[~sees], l1[~sees])
     if not np.isfinite(bad):
         assert not bool(torch.isfinite(o1[sees]).all(-1).any())
+
+
+@pytest.fixture
+def wide(monkeypatch):
+    """Tables of 1,024 tokens more than the sequences have: short ones' items are blocks', these
+    are cut into shares."""
+    table_of = R.table_of
+    monkeypatch.setattr(R, "table_of", lambda lens, P, g, spare=3, extra=1: table_of(lens, P, g, spare, extra + 1024 // P))
+
+
+@pytest.mark.parametrize("mask", ["tree", None])
+@pytest.mark.parametrize("q,kv,out", [("bf16", "bf16", "fp32"), ("bf16", "bf16", "bf16"), ("fp32", "fp32", "fp32"),
+                                      ("bf16", "fp32", "fp32"), ("fp32", "bf16", "bf16")])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_tree_wide_tables(wide, shape, q, kv, out, mask):
+    test_tree_attend(shape, q, kv, out, mask)
+
+
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+def test_tree_wide_tables_of_many_sequences(wide, q):
+    for rows in ((40, 1), (150, 3), (700, 2)):
+        test_tree_many_sequences(rows, q)
+
+
+@pytest.mark.parametrize("G", [1, 5, 8, 13, 16])
+def test_tree_wide_tables_groups(wide, G):
+    test_tree_groups(G)
+
+
+@pytest.mark.parametrize("new,G", [(300, 1), (300, 7), (520, 2)])
+@pytest.mark.parametrize("bad", [None, float("nan")])
+def test_tree_wide_tables_and_masks(wide, new, G, bad):
+    test_tree_masks_wider_than_the_block_holds(new, G, bad)
+
+
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [7, 40, 200])
+def test_tree_wide_tables_unseen_tokens(wide, q, new):
+    for bad in (float("nan"), float("inf"), -float("inf"), 3e38):
+        test_tree_unseen_tokens_do_not_reach_a_row(q, new, bad)
+
+
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+def test_tree_wide_tables_rows_that_see_nothing(wide, q):
+    test_tree_rows_that_see_nothing(q)
+
+
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+@pytest.mark.parametrize("pages", [8, 9, 16, 17, 31, 32, 33])
+def test_tree_full_tables_around_the_cut(q, pages):
+    """Sequences that fill tables of 128 to 528 tokens."""
+    L = 16 * pages
+    for new in ([5, 5], [40, 33], [100, 77]):
+        Batch([L - new[0], L - 3 - new[1]], new, q=q, kv=q, seed=pages, extra=0).check("bf16" if pages % 2 else "fp32")
 
 
 @pytest.mark.parametrize("q,out", [("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "fp32")])
