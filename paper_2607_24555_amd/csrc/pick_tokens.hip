@@ -7,12 +7,12 @@
 // tokens above T, and the first ones equal to it, are written at their ranks.  A block holds up
 // to 32 K tokens of a list in registers, a wave 64 kKeys of them in a row, so that ranks within
 // a wave are counts of ballots.  Lists of up to that many tokens take one launch; longer ones
-// are cut into chunks of 32 K, each with a block that writes its chunk's histogram, and four
+// are cut into chunks of 8 K to 32 K, each with a block that writes its chunk's histogram, and four
 // launches: a launch's blocks each sum the chunks' histograms of the digit before (which also
 // tells how many tokens kept lie before their chunk).
 //
 // Bound by latency, of barriers and launches: 8 lists of 4K tokens 10.4 us; 64 lists of 128K (33
-// MB, 6.5 us of HBM) 56 us in launches of 12, 12, 14 and 19; two of 1M 44 us.  Chunks of 16 K
+// MB, 6.5 us of HBM) 56 us in launches of 12, 12, 14 and 19; two of 1M 38 us.  Chunks of 16 K
 // for 128K tokens: 68 us.  Ranks by two ballots a group for every lane instead of lane masks, and
 // forced tokens among them: 67.
 #include "tokens_internal.h"
@@ -240,9 +240,19 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   }
 }
 
+// Tokens of a chunk: as few as leave each block a compute unit, and at most 64 histograms to
+// sum where there is a choice (16 lists of 128K: 29 us, in chunks of 32 K 45; 2 of 1M 41 and 49;
+// 64 of 40K 32 and 45; 2 of 256K in chunks of 8 K 28, of 16 K 31).
+int pick_chunk(const locks_cfg_t& c) {
+  const long width = (long)c.max_pages_per_seq * c.page_size, lists = (long)c.num_seqs * c.num_kv_heads;
+  if (width <= kOneLaunch) return kOneLaunch;
+  int chunk = kPickBlock * 8;
+  while (chunk < kPickChunk && ((width + chunk - 1) / chunk > 64 || lists * ((width + chunk - 1) / chunk) > 256)) chunk *= 2;
+  return chunk;
+}
 int pick_chunks(const locks_cfg_t& c) {
-  const long width = (long)c.max_pages_per_seq * c.page_size;
-  return width <= kOneLaunch ? 1 : (int)((width + kPickChunk - 1) / kPickChunk);
+  const long width = (long)c.max_pages_per_seq * c.page_size, chunk = pick_chunk(c);
+  return (int)((width + chunk - 1) / chunk);
 }
 
 }  // namespace
@@ -268,10 +278,13 @@ hipError_t launch_pick_tokens(const locks_cfg_t& c, const float* mass, const int
     else if (width <= 16 * kPickBlock) PICK(16, -1);
     else PICK(32, -1);
   } else {
-    PICK(32, 0);
-    PICK(32, 1);
-    PICK(32, 2);
-    PICK(32, 3);
+#define PICK4(KEYS) PICK(KEYS, 0); PICK(KEYS, 1); PICK(KEYS, 2); PICK(KEYS, 3)
+    switch (pick_chunk(c) / kPickBlock) {
+      case 8: PICK4(8); break;
+      case 16: PICK4(16); break;
+      default: PICK4(32);
+    }
+#undef PICK4
   }
 #undef PICK
   return hipGetLastError();

@@ -530,6 +530,13 @@ def test_pick_tokens(lens, n_keep, sink, recent, kind):
             assert got[s, h].tolist() == want + [-1] * (n_keep - len(want)), (s, h)
 
 
+@pytest.mark.parametrize("kind", ["spread", "ties", "special"])
+@pytest.mark.parametrize("lens", [[40000, 32769, 8193, 100], [33000 - 900 * s for s in range(30)],
+                                  [33000 - 450 * s for s in range(60)], [600001, 16384]])
+def test_pick_chunks_of_every_size(lens, kind):
+    test_pick_tokens(lens, 700, 4, 65, kind)
+
+
 def test_pick_holds_lengths_to_the_table():
     cfg = B.Config(2, 8, 2, 8, 256, 3, 8)
     x = torch.rand(2, 2, 48).cuda()
