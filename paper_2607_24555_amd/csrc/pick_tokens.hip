@@ -13,7 +13,7 @@
 //
 // Bound by latency, of barriers and launches: 8 lists of 4K tokens 10.4 us; 64 lists of 128K (33
 // MB, 6.5 us of HBM) 56 us in launches of 12, 12, 14 and 19; two of 1M 38 us.  Chunks of 16 K
-// for 128K tokens: 68 us.  Ranks by two ballots a group for every lane instead of lane masks, and
+// for 64 lists of 128K: 64 us.  Ranks by two ballots a group for every lane instead of lane masks, and
 // forced tokens among them: 67.
 #include "tokens_internal.h"
 

@@ -13,8 +13,11 @@
 //
 // Bound by HBM: 64 sequences of 1.5K to 8K tokens, 8 heads, a new token each: 128 us, 4.9 TB/s
 // (a copy here 5.1).  Keys read in the product's order, 32 bytes of each of 32 rows a load, took
-// 154.  With 128 rows (the last 32 tokens of prompts of 20K to 32K) 120 us, 3.7 TB/s: 16 powers
-// a lane and 32 x 32 logits take as long as their keys.
+// 154.  With 128 rows (the last 32 tokens of prompts of 20K to 32K) 117 us, 3.7 TB/s: 16 powers
+// a lane and 32 x 32 logits take as long as their keys.  Among the new tokens a lane first has
+// what its row sees of the 32 tokens, one window of the mask, and the tokens' lanes take their bits
+// from it (15 trees of 34 to 104 tokens, eight heads a group, over up to 232: 44 us; with a mask
+// load for each row and token 116).
 #include <type_traits>
 
 #include "tokens_internal.h"

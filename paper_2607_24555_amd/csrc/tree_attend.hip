@@ -30,8 +30,9 @@
 // All (sequence, KV head, tile) items' units, in order, are cut into equal shares, one a
 // block (every block derives the cut from the lengths), so ragged batches and long lists
 // fill the chip; a unit counts by the 32s of rows that its tile has (see weight_of); an item
-// within a share writes its output, others leave partials (o, max, sum), which merge_kernel
-// combines in order.  Where there are more tiles than kTiles an item is a block's.
+// within a share writes its output, others leave partials (o, max, sum), which
+// tree_merge_kernel combines in order.  Where there are more tiles than kTiles, or the tables are
+// short, an item is a block's and there is nothing to merge.
 //
 // What a row does not see is masked by one 32-bit window per row and 32 tokens, the
 // ancestors' bits shifted to the tile; only units that hold tokens some row does not see look
