@@ -15,6 +15,8 @@
 // MB, 6.5 us of HBM) 56 us in launches of 12, 12, 14 and 19; two of 1M 38 us.  Chunks of 16 K
 // for 64 lists of 128K: 64 us.  Ranks by two ballots a group for every lane instead of lane masks, and
 // forced tokens among them: 67.
+#include <type_traits>
+
 #include "tokens_internal.h"
 
 namespace locks {
@@ -112,12 +114,30 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   // their way; where every token is kept already they hold anything, and are not used
   int h0 = 0, h1 = 0, p0 = 0, p1 = 0;
   if (kPhase > 0) {
-    const uint16_t* hist = a.hist + ((kPhase - 1) * a.lists + list) * a.chunks * kBins;
+    const uint32_t* hist = reinterpret_cast<const uint32_t*>(a.hist + ((kPhase - 1) * a.lists + list) * a.chunks * kBins) +
+                           (kPickBlock - 1 - tid);
+    auto few = [&](auto most) {  // all together (64 lists of 128K, four chunks: 51 us, in turn 54)
+      constexpr int kMost = decltype(most)::value;
+      uint32_t v[kMost];
+#pragma unroll
+      for (int e = 0; e < kMost; ++e) v[e] = hist[min(e, a.chunks - 1) * (kBins / 2)];
+#pragma unroll
+      for (int e = 0; e < kMost; ++e) {
+        if (e < a.chunks) h0 += v[e] >> 16, h1 += v[e] & 0xffffu;
+        if (e < chunk) p0 += v[e] >> 16, p1 += v[e] & 0xffffu;
+      }
+    };
+    if (a.chunks <= 4) {
+      few(std::integral_constant<int, 4>{});
+    } else if (a.chunks <= 8) {
+      few(std::integral_constant<int, 8>{});
+    } else {
 #pragma unroll 16
-    for (int c = 0; c < a.chunks; ++c) {
-      const uint32_t v = reinterpret_cast<const uint32_t*>(hist + (long)c * kBins)[kPickBlock - 1 - tid];
-      h0 += v >> 16, h1 += v & 0xffffu;
-      if (c < chunk) p0 += v >> 16, p1 += v & 0xffffu;
+      for (int c = 0; c < a.chunks; ++c) {
+        const uint32_t v = hist[(long)c * (kBins / 2)];
+        h0 += v >> 16, h1 += v & 0xffffu;
+        if (c < chunk) p0 += v >> 16, p1 += v & 0xffffu;
+      }
     }
   }
   uint32_t key[kKeys];
