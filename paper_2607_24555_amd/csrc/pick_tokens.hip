@@ -12,7 +12,7 @@
 // tells how many tokens kept lie before their chunk).
 //
 // Bound by latency, of barriers and launches: 8 lists of 4K tokens 10.4 us; 64 lists of 128K (33
-// MB, 6.5 us of HBM) 56 us in launches of 12, 12, 14 and 19; two of 1M 38 us.  Chunks of 16 K
+// MB, 6.5 us of HBM) 54 us in launches of 11, 13, 13 and 18; two of 1M 38 us.  Chunks of 16 K
 // for 64 lists of 128K: 64 us.  Ranks by two ballots a group for every lane instead of lane masks, and
 // forced tokens among them: 67.
 #include <type_traits>
