@@ -27,6 +27,7 @@ namespace {
 
 constexpr int kSeqs = 512;          // sequences whose units are counted on the device
 constexpr int kMassBlocks = 512;    // two per compute unit
+constexpr int kManyRows = 128;      // of a sequence and KV head
 
 // kF32: products in fp32 (32x32x2 MFMA), else bf16 (32x32x16).
 template <bool kF32, typename TQ, typename TK>
@@ -349,20 +350,112 @@ __global__ __launch_bounds__(256, kF32 ? 1 : 2) void mass_kernel(DraftArgs a, co
   }
 }
 
+// Many rows over few tokens: a block takes 32 tokens of a list and its eight waves every eighth
+// chunk of rows, whose queries they read as the product takes them; their sums are added in
+// order.  Above, a wave goes through all rows alone: 7 prompts of 159 to 477 tokens over up to
+// 577, 16 heads a group, fp32 147 us instead of 745; 15 trees of 34 to 104, eight heads a group,
+// bf16 12.6 instead of 43.6.
+constexpr int kRowWaves = 8;
+template <bool kF32, typename TQ, typename TK>
+__global__ __launch_bounds__(64 * kRowWaves) void mass_rows_kernel(DraftArgs a, const float* __restrict__ lse,
+                                                                   const TK* __restrict__ k_cache, float decay,
+                                                                   float* __restrict__ mass) {
+  __shared__ float s_sum[kRowWaves][32];
+  const int h = blockIdx.y, s = blockIdx.z, t0 = blockIdx.x * 32;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const float zs = kLog2e / sqrtf((float)kDim);
+  const DraftSeq w = draft_seq(a, s);
+  if (w.n == 0 || t0 >= w.L) return;
+  const int first = w.L - w.n, count = w.n * a.G, j0 = t0 - first, t = min(t0 + col, w.L - 1);
+  const bool tail = j0 > -32;
+  const int lgP = a.pgsz == 64 ? 6 : a.pgsz == 32 ? 5 : 4;
+  const int blk = a.page_table[(long)s * a.max_pages + (t >> lgP)];
+  const bool live = (unsigned)blk < (unsigned)a.num_blocks;
+
+  using RawK = typename std::conditional<kF32 && sizeof(TK) == 2, u2, u4>::type;
+  using RawQ = typename std::conditional<kF32 && sizeof(TQ) == 2, u2, u4>::type;
+  constexpr int kLoads = kF32 ? 16 : 8, kElems = kF32 ? 4 : 8;
+  RawK kr[kLoads];
+  const TK* k = k_cache + (((long)(live ? blk : 0) * a.H + h) * a.pgsz + (t & (a.pgsz - 1))) * kDim + kElems * half;
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) kr[j] = *reinterpret_cast<const RawK*>(k + 2 * kElems * j);
+
+  float sum = 0.0f;
+  const int r0 = a.mask ? 0 : max(0, j0) * a.G;  // (a run: earlier rows do not see these tokens)
+  for (int c = r0 / 32 + wave; 32 * c < count; c += kRowWaves) {
+    const int r = 32 * c + col, i = min(r, count - 1) / a.G, hq = h * a.G + min(r, count - 1) % a.G;
+    const TQ* qp = static_cast<const TQ*>(a.q) + (long)(w.row0 + i) * a.q_stride + (long)hq * kDim + kElems * half;
+    RawQ qr[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) qr[j] = *reinterpret_cast<const RawQ*>(qp + 2 * kElems * j);
+    const float l = lse[(long)(w.row0 + i) * a.H * a.G + hq];
+    const float nl = -l * kLog2e;
+    uint32_t seen = tail ? draft_window(a, w.row0 + i, i, j0, w.L - t0) : ~0u;
+    if (r >= count || fabsf(l) == INFINITY) seen = 0u;
+    f16v z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = 0.0f;
+    if constexpr (kF32) {
+      auto at = [](const auto& x, int e) {
+        if constexpr (sizeof(x) == 8) return __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+        else return __uint_as_float(x[e]);
+      };
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z = __builtin_amdgcn_mfma_f32_32x32x2f32(at(qr[j], e), at(kr[j], e), z, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, qr[j]), __builtin_bit_cast(bf8, kr[j]), z,
+                                                    0, 0, 0);
+    }
+    // element e: row 8 (e / 4) + 4 half + e % 4 of the chunk, whose lane has its sum and window
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int from = 8 * (e / 4) + 4 * half + e % 4;
+      const float y = __builtin_amdgcn_exp2f(fmaf(z[e], zs, __shfl(nl, from, 64)));
+      sum += __shfl(seen, from, 64) >> col & 1u ? y : 0.0f;
+    }
+  }
+  auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+  if (half == 0) s_sum[wave][col] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  __syncthreads();
+  if (tid < 32 && t0 + tid < w.L && live) {
+    float all = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kRowWaves; ++e) all += s_sum[e][tid];
+    float* const m = mass + ((long)s * a.H + h) * a.max_pages * a.pgsz + t0 + tid;
+    *m = (t0 + tid < first ? decay * *m : 0.0f) + all;
+  }
+}
+
 }  // namespace
 
 hipError_t launch_token_mass(const locks_cfg_t& c, const DraftArgs& a, const float* lse,
                              const void* k_cache, float decay, float* mass, hipStream_t st) {
   const bool f32 = c.q_dtype != LOCKS_BF16 || c.kv_dtype != LOCKS_BF16;
-  const long all = ((long)a.max_pages * a.pgsz + 127) / 128 * a.H * a.S;
-  const dim3 grid((unsigned)(all < kMassBlocks ? all : kMassBlocks)), block(256);
-#define MASS(F32, TQ, TK)                                                                  \
-  hipLaunchKernelGGL((mass_kernel<F32, TQ, TK>), grid, block, 0, st, a, lse,               \
-                     static_cast<const TK*>(k_cache), decay, mass)
-  if (!f32) MASS(false, uint16_t, uint16_t);
-  else if (c.q_dtype == LOCKS_BF16) MASS(true, uint16_t, float);
-  else if (c.kv_dtype == LOCKS_BF16) MASS(true, float, uint16_t);
-  else MASS(true, float, float);
+  const long width = (long)a.max_pages * a.pgsz, all = (width + 127) / 128 * a.H * a.S;
+  // by the average sequence's rows, and the most units there can be
+  const bool by_rows = (long)a.n_tokens * a.G / a.S >= kManyRows && all <= kMassBlocks;
+  const dim3 grid = by_rows ? dim3((unsigned)((width + 31) / 32), a.H, a.S) : dim3((unsigned)(all < kMassBlocks ? all : kMassBlocks));
+#define MASS(F32, TQ, TK)                                                                            \
+  if (by_rows)                                                                                       \
+    hipLaunchKernelGGL((mass_rows_kernel<F32, TQ, TK>), grid, dim3(64 * kRowWaves), 0, st, a, lse,   \
+                       static_cast<const TK*>(k_cache), decay, mass);                                \
+  else                                                                                               \
+    hipLaunchKernelGGL((mass_kernel<F32, TQ, TK>), grid, dim3(256), 0, st, a, lse,                   \
+                       static_cast<const TK*>(k_cache), decay, mass)
+  if (!f32) {
+    MASS(false, uint16_t, uint16_t);
+  } else if (c.q_dtype == LOCKS_BF16) {
+    MASS(true, uint16_t, float);
+  } else if (c.kv_dtype == LOCKS_BF16) {
+    MASS(true, float, uint16_t);
+  } else {
+    MASS(true, float, float);
+  }
 #undef MASS
   return hipGetLastError();
 }

@@ -437,6 +437,17 @@ def test_token_mass_of_many_rows(q, mask):
     _mass_case([30, 0, 513], [150, 90, 33], q, q, mask, 4, 64, decay=0.25)
 
 
+@pytest.mark.parametrize("q,kv", [("bf16", "bf16"), ("fp32", "fp32"), ("bf16", "fp32"), ("fp32", "bf16")])
+@pytest.mark.parametrize("mask", ["tree", None])
+@pytest.mark.parametrize("extra", [0, 40000])
+@pytest.mark.parametrize("past,new,G,P", [([0, 31, 100], [64, 33, 40], 8, 16), ([7], [300], 16, 64), ([500, 3], [97, 128], 4, 32)])
+def test_token_mass_of_many_rows_and_any_table(monkeypatch, past, new, G, P, extra, mask, q, kv):
+    """Rows shared by a block's waves (short tables), and not."""
+    table_of = R.table_of
+    monkeypatch.setattr(R, "table_of", lambda lens, P, g, spare=3, extra=1, more=extra: table_of(lens, P, g, spare, extra + more // P))
+    _mass_case(past, new, q, kv, mask, G, P)
+
+
 def test_token_mass_of_rows_that_see_nothing_and_of_bad_keys():
     """-inf rows add nothing; a key that is not finite makes only its own token's mass so; a
     NaN row makes what it sees NaN."""
