@@ -62,8 +62,8 @@ size_t locks_tree_workspace_bytes(const locks_cfg_t* cfg, int32_t n_tokens);
  * A token that sees nothing gets out = 0 and out_lse = -inf.  Tokens that a row does not see
  * do not reach it, whatever their keys and values hold; nor do rows past a sequence's end.
  * Logits, maxima and sums are fp32.  Over bf16 queries and caches the softmax weights enter
- * the product with the values as bf16: for fp32 outputs in three terms (2^-24 of a weight), for
- * bf16 ones in one (2^-8, as their own rounding) or two; other types are computed in fp32
+ * the product with the values as sums of bf16 terms: three for fp32 outputs (2^-24 of a
+ * weight), two for bf16 ones (2^-16), whatever the batch; other types are computed in fp32
  * throughout.
  * Returns LOCKS_E_INVAL for a null or misaligned pointer, a bad stride or count or out == q,
  * and LOCKS_E_UNSUPPORTED for another out_dtype, for n_tokens * H_q or the tables' tokens

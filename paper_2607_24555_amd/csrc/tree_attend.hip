@@ -19,8 +19,8 @@
 //   up to 64   two waves by rows, two by tokens (16 new: 209 us, 5.2 TB/s).
 //   up to 128  four waves by rows, two blocks a compute unit.
 //   more       eight waves by rows, with three units of copies to LDS on their way.  Against the
-//              128-row tile: ragged trees of 140 to 248 rows 324 us (400), 16 tokens of 16 heads
-//              over 1M 505 (558), pieces of prompts 449 (528).  Its products and the weights'
+//              128-row tile: ragged trees of 140 to 248 rows 394 us (449), 16 tokens of 16 heads
+//              over 1M 501 (536), pieces of prompts 594 (637).  Its products and the weights'
 //              vector work overlap by half: at 2.05 GHz the matrix pipe is busy 45% of the time
 //              and the vector one 45% (pieces of prompts, 930 TFLOP/s).
 // fp32 products (any other types) take 32 or 128 rows and run at 69 TFLOP/s of the 154 of a
@@ -1030,22 +1030,20 @@ void launch_f32(const TreeArgs& a, const Plan& p, hipStream_t st) {
   if (p.rows == 32) launch_one<true, TQ, TK, 1, 1, 4, 1, 1>(a, p, st);
   else launch_one<true, TQ, TK, 1, 4, 1, 1, 2>(a, p, st);
 }
-// Terms of a weight: three for fp32 outputs (2^-24); one for bf16 ones, whose own rounding is as
-// large (prompts 728 us in two terms, 580 in one), but two where the tile is bound by memory.
+template <int NT>
+void launch_terms(const TreeArgs& a, const Plan& p, hipStream_t st) {
+  if (p.rows == 32) launch_one<false, uint16_t, uint16_t, NT, 1, 4, 1, 2>(a, p, st);
+  else if (p.rows == 64) launch_one<false, uint16_t, uint16_t, NT, 2, 2, 1, 2>(a, p, st);
+  else if (p.rows == 128) launch_one<false, uint16_t, uint16_t, NT, 4, 1, 2, 2>(a, p, st);
+  else launch_one<false, uint16_t, uint16_t, NT, 8, 1, 2, 2>(a, p, st);
+}
+// Terms of a weight, by the output's type alone: three for fp32 (2^-24 of it), two for bf16 (2^-16, a
+// 256th of the output's own rounding).  In one term (2^-8) a bf16 output is as far off again as by its own
+// rounding, 2.3e-3 of it instead of 1.7e-3, and so much depends on the batch's tile where only some tiles have it
+// (ragged trees 304 us in one term, 400 in two, 492 in three; pieces of prompts 447, 605 and 751).
 void launch_bf16(const TreeArgs& a, const Plan& p, hipStream_t st) {
-  if (p.rows == 32) {
-    if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 2, 1, 4, 1, 2>(a, p, st);
-    else launch_one<false, uint16_t, uint16_t, 3, 1, 4, 1, 2>(a, p, st);
-  } else if (p.rows == 64) {
-    if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 1, 2, 2, 1, 2>(a, p, st);
-    else launch_one<false, uint16_t, uint16_t, 3, 2, 2, 1, 2>(a, p, st);
-  } else if (p.rows == 128) {
-    if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 1, 4, 1, 2, 2>(a, p, st);
-    else launch_one<false, uint16_t, uint16_t, 3, 4, 1, 2, 2>(a, p, st);
-  } else {
-    if (a.out_bf16) launch_one<false, uint16_t, uint16_t, 1, 8, 1, 2, 2>(a, p, st);
-    else launch_one<false, uint16_t, uint16_t, 3, 8, 1, 2, 2>(a, p, st);
-  }
+  if (a.out_bf16) launch_terms<2>(a, p, st);
+  else launch_terms<3>(a, p, st);
 }
 
 }  // namespace
