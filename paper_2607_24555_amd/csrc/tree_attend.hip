@@ -678,7 +678,8 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
 #pragma unroll
       for (int w = 0; w < TW; ++w) {
         const float mw = s_m[w][wr * 32 + col];
-        ls += mw == -INFINITY ? 0.0f : s_l[w][wr * 32 + col] * __builtin_amdgcn_exp2f(mw - mx);
+        // (a product where the wave has no maximum too: a sum of NaN logits, whose maximum stays -inf, stays NaN)
+        ls += s_l[w][wr * 32 + col] * (mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - mx));
       }
       const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mx);
       float* to = reinterpret_cast<float*>(lds) + (wt * C::kRows + wr * 32 + col) * 132;

@@ -1,5 +1,5 @@
 """GPU checks of the calls on single cached tokens (include/locks_tokens.h) where only a part of an
-answer can go wrong: the roundings of bf16 outputs."""
+answer can go wrong: the roundings of bf16 outputs, and the LSE of rows that a NaN reaches."""
 import numpy as np
 import pytest
 import torch
@@ -61,3 +61,60 @@ def test_bf16_rows_beside_others_are_as_exact_as_alone(rows):
         e = 2 * (130 * 2.0 ** -24 * big + 2.0 ** -22 * (1 + zmax)) + (b.lens[s] + 64) * 2.0 ** -23
         bound = 2.0 ** -8 * 1.01 * np.abs(want) + (e + 2.0 ** -16) * 1.01 * size[at, heads].double().numpy()
         assert (np.abs(both[at, heads].double().numpy() - want) <= bound).all()
+
+
+@pytest.mark.parametrize("extra", WIDE)
+@pytest.mark.parametrize("new", TILES)
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+def test_lse_of_rows_that_a_nan_reaches(q, new, extra):
+    """A NaN query head and a NaN key that is alone in its 32 tokens (the last one; a run, so that
+    only the last row sees it): their rows' outputs and LSEs are NaN, all others keep their bits."""
+    print(f"[nan] {q} new={new} extra={extra}", flush=True)
+    L = 97 if new == 70 else 33
+    b = Batch([L - new, 5], [new, new], P=16, q=q, kv=q, mask=None, seed=new, extra=extra)
+    d = b.dev()
+    o0, l0 = _attend(b)
+    assert bool(torch.isfinite(o0).all()) and bool(torch.isfinite(l0).all())
+
+    hit = torch.zeros(b.n, b.G * b.H, dtype=torch.bool)
+    hit[0, 3] = hit[new // 2, 5] = hit[b.n - 1, 0] = True
+    clean = d["q"].clone()
+    d["q"][hit.cuda()] = float("nan")
+    o1, l1 = _attend(b)
+    d["q"].copy_(clean)
+    assert bool(o1[hit].isnan().all()) and bool(l1[hit].isnan().all())
+    assert torch.equal(o1[~hit], o0[~hit]) and torch.equal(l1[~hit], l0[~hit])
+
+    d["k"][int(b.table[0, (L - 1) // 16]), :, (L - 1) % 16] = float("nan")
+    o1, l1 = _attend(b)
+    hit[:] = False
+    hit[new - 1] = True
+    assert bool(o1[hit].isnan().all()) and bool(l1[hit].isnan().all())
+    assert torch.equal(o1[~hit], o0[~hit]) and torch.equal(l1[~hit], l0[~hit])
+
+
+@pytest.mark.parametrize("extra", WIDE)
+@pytest.mark.parametrize("new", TILES)
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_lse_of_trees_with_bad_tokens(bad, q, new, extra):
+    """A drafted token with a bad key: the LSE of the rows that see it is NaN (NaN) or not finite
+    (infinity, whose products with a query are of both signs), of the others as before; a bad value
+    changes no LSE."""
+    b = Batch([40], [new], P=16, q=q, kv=q, seed=new, extra=extra)
+    d = b.dev()
+    o0, l0 = _attend(b)
+    j = new // 2
+    at = (int(b.table[0, (40 + j) // 16]), slice(None), (40 + j) % 16)
+    sees = torch.tensor([bool(int(b.mask[i, j // 32]) >> (j % 32) & 1) for i in range(new)])
+    assert bool(sees.any()) and not bool(sees.all())
+    old = d["v"][at].clone()
+    d["v"][at] = bad
+    o1, l1 = _attend(b)
+    d["v"][at] = old
+    assert torch.equal(l1, l0) and torch.equal(o1[~sees], o0[~sees]) and not bool(torch.isfinite(o1[sees]).any())
+    d["k"][at] = bad
+    o1, l1 = _attend(b)
+    assert torch.equal(o1[~sees], o0[~sees]) and torch.equal(l1[~sees], l0[~sees])
+    assert not bool(torch.isfinite(o1[sees]).any())
+    assert bool(l1[sees].isnan().all()) if bad != bad else not bool(torch.isfinite(l1[sees]).any())
