@@ -51,8 +51,9 @@ typedef struct locks_draft {
   int32_t mask_words;        /* >= 1 where there is a mask, else not read                  */
 } locks_draft_t;
 
-/* Bytes of workspace locks_tree_attend needs for cfg and n_tokens new tokens, at least
- * locks_workspace_bytes(cfg) (whose table-check word it holds too); 0 if one is invalid. */
+/* Bytes of workspace for locks_tree_attend with cfg and n_tokens new tokens, and with fewer
+ * of them or fewer sequences (num_seqs); at least locks_workspace_bytes(cfg) (whose
+ * table-check word it holds too).  0 if one is invalid. */
 size_t locks_tree_workspace_bytes(const locks_cfg_t* cfg, int32_t n_tokens);
 
 /* Attention of every new token's query heads over the tokens that it sees,
@@ -89,7 +90,8 @@ int locks_token_mass(const locks_cfg_t* cfg, const locks_draft_t* draft, const f
                      const void* k_cache, const int32_t* page_table, const int32_t* seq_lens,
                      float decay, float* mass, void* stream);
 
-/* Bytes of workspace locks_pick_tokens needs (0 if cfg is invalid). */
+/* Bytes of workspace for locks_pick_tokens with cfg, and with fewer sequences (0 if cfg is
+ * invalid). */
 size_t locks_pick_workspace_bytes(const locks_cfg_t* cfg);
 
 /* The n_keep tokens of every sequence and KV head to keep: the first n_sink, the last

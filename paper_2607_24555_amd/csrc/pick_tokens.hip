@@ -282,6 +282,18 @@ size_t pick_scratch_bytes(const locks_cfg_t& c) {
   return 256 + (chunks > 1 ? lists * chunks * (3 * kBins * sizeof(uint16_t) + 4 * sizeof(int32_t)) : 0);
 }
 
+// What no launch of as many sequences or fewer needs more than: fewer lists can be cut into more
+// chunks in all, where chunks are below the largest, so of up to 256 lists.
+size_t pick_scratch_most(const locks_cfg_t& c) {
+  size_t most = pick_scratch_bytes(c);
+  locks_cfg_t fewer = c;
+  for (fewer.num_seqs = 1; fewer.num_seqs < c.num_seqs && fewer.num_seqs <= 256; ++fewer.num_seqs) {
+    const size_t n = pick_scratch_bytes(fewer);
+    if (n > most) most = n;
+  }
+  return most;
+}
+
 hipError_t launch_pick_tokens(const locks_cfg_t& c, const float* mass, const int32_t* seq_lens,
                               int n_keep, int n_sink, int n_recent, int32_t* out_ids, void* scratch,
                               hipStream_t st) {

@@ -44,7 +44,14 @@ extern "C" {
 
 size_t locks_tree_workspace_bytes(const locks_cfg_t* cfg, int32_t n_tokens) {
   if (validate(cfg, false) || n_tokens < 0) return 0;
-  return align256(plan_workspace(*cfg).total) + tree_scratch_bytes(*cfg, n_tokens);
+  // the attention calls' part of fewer sequences can be larger too
+  locks_cfg_t fewer = *cfg;
+  size_t most = plan_workspace(*cfg).total;
+  for (fewer.num_seqs = 1; fewer.num_seqs < cfg->num_seqs; ++fewer.num_seqs) {
+    const size_t n = plan_workspace(fewer).total;
+    if (n > most) most = n;
+  }
+  return align256(most) + tree_scratch_most(*cfg, n_tokens);
 }
 
 int locks_tree_attend(const locks_cfg_t* cfg, const locks_draft_t* draft, const void* k_cache,
@@ -58,12 +65,13 @@ int locks_tree_attend(const locks_cfg_t* cfg, const locks_draft_t* draft, const 
   if (!k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache)) return LOCKS_E_INVAL;
   if (draft->n_tokens > 0 && (!out || !aligned16(out) || out == draft->q)) return LOCKS_E_INVAL;
   if ((rc = check_ws(cfg, ws, ws_bytes))) return rc;
-  if (ws_bytes < locks_tree_workspace_bytes(cfg, draft->n_tokens)) return LOCKS_E_WORKSPACE;
+  const size_t scratch = align256(plan_workspace(*cfg).total);
+  if (ws_bytes < scratch + tree_scratch_bytes(*cfg, draft->n_tokens)) return LOCKS_E_WORKSPACE;
   if (cfg->num_seqs == 0 || draft->n_tokens == 0) return LOCKS_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if ((rc = checked_tables(*cfg, ws, a.page_table, a.seq_lens, st))) return rc;
   return hip_status(launch_tree_attend(*cfg, a, k_cache, v_cache, out, out_dtype == LOCKS_BF16, out_lse,
-                                       static_cast<char*>(ws) + align256(plan_workspace(*cfg).total), st));
+                                       static_cast<char*>(ws) + scratch, st));
 }
 
 int locks_token_mass(const locks_cfg_t* cfg, const locks_draft_t* draft, const float* lse,
@@ -81,7 +89,7 @@ int locks_token_mass(const locks_cfg_t* cfg, const locks_draft_t* draft, const f
 
 size_t locks_pick_workspace_bytes(const locks_cfg_t* cfg) {
   if (validate(cfg, false)) return 0;
-  return pick_scratch_bytes(*cfg);
+  return pick_scratch_most(*cfg);
 }
 
 int locks_pick_tokens(const locks_cfg_t* cfg, const float* mass, const int32_t* seq_lens,

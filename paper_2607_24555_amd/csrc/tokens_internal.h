@@ -91,12 +91,14 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 size_t tree_scratch_bytes(const locks_cfg_t& c, int n_tokens);
+size_t tree_scratch_most(const locks_cfg_t& c, int n_tokens);
 hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& a, const void* k_cache,
                               const void* v_cache, void* out, bool out_bf16, float* out_lse,
                               void* scratch, hipStream_t st);
 hipError_t launch_token_mass(const locks_cfg_t& c, const DraftArgs& a, const float* lse,
                              const void* k_cache, float decay, float* mass, hipStream_t st);
 size_t pick_scratch_bytes(const locks_cfg_t& c);
+size_t pick_scratch_most(const locks_cfg_t& c);
 hipError_t launch_pick_tokens(const locks_cfg_t& c, const float* mass, const int32_t* seq_lens,
                               int n_keep, int n_sink, int n_recent, int32_t* out_ids, void* scratch,
                               hipStream_t st);

@@ -1047,12 +1047,21 @@ void launch_bf16(const TreeArgs& a, const Plan& p, hipStream_t st) {
   else launch_terms<3>(a, p, st);
 }
 
+// Of tiles of so many rows (256: half the blocks, so as much as 128).
+size_t scratch_of(int rows) {
+  return (size_t)kTreeBlocks * (2 * (size_t)(rows < 128 ? rows : 128) * (kDim + 2) * sizeof(float) + 8 * sizeof(int32_t));
+}
+
 }  // namespace
 
-// (what no smaller number of tokens needs more than: a workspace serves up to n_tokens)
-size_t tree_scratch_bytes(const locks_cfg_t& c, int n_tokens) {
-  const size_t rows = tree_plan(c, n_tokens).rows < 128 ? tree_plan(c, n_tokens).rows : 128;  // (256: half the blocks)
-  return (size_t)kTreeBlocks * (2 * rows * (kDim + 2) * sizeof(float) + 8 * sizeof(int32_t));
+size_t tree_scratch_bytes(const locks_cfg_t& c, int n_tokens) { return scratch_of(tree_plan(c, n_tokens).rows); }
+
+// What no launch of as many sequences and tokens or fewer needs more than: fewer sequences have
+// larger tiles, and one with all the tokens has the largest.
+size_t tree_scratch_most(const locks_cfg_t& c, int n_tokens) {
+  locks_cfg_t one = c;
+  if (one.num_seqs > 1) one.num_seqs = 1;
+  return tree_scratch_bytes(one, n_tokens);
 }
 
 hipError_t launch_tree_attend(const locks_cfg_t& c, const DraftArgs& d, const void* k_cache,

@@ -78,12 +78,12 @@ def tree_workspace_bytes(cfg: Config, n_tokens: int) -> int:
 
 
 def alloc_tree_workspace(cfg: Config, n_tokens: int, device="cuda") -> torch.Tensor:
-    """A workspace of tree_attend for up to n_tokens new tokens."""
+    """A workspace of tree_attend for up to n_tokens new tokens of up to cfg.num_seqs sequences."""
     return torch.empty(tree_workspace_bytes(cfg, n_tokens), dtype=torch.uint8, device=device)
 
 
 def alloc_pick_workspace(cfg: Config, device="cuda") -> torch.Tensor:
-    """A workspace of pick_tokens."""
+    """A workspace of pick_tokens for up to cfg.num_seqs sequences."""
     c = cfg.c()
     n = int(lib().locks_pick_workspace_bytes(ctypes.byref(c)))
     if n == 0:

@@ -1,5 +1,6 @@
 """GPU checks of the calls on single cached tokens (include/locks_tokens.h) where only a part of an
-answer can go wrong: the roundings of bf16 outputs, and the LSE of rows that a NaN reaches."""
+answer can go wrong: the roundings of bf16 outputs, and the LSE of rows that a NaN reaches; and of workspaces
+that serve smaller batches."""
 import numpy as np
 import pytest
 import torch
@@ -118,3 +119,34 @@ def test_lse_of_trees_with_bad_tokens(bad, q, new, extra):
     assert torch.equal(o1[~sees], o0[~sees]) and torch.equal(l1[~sees], l0[~sees])
     assert not bool(torch.isfinite(o1[sees]).any())
     assert bool(l1[sees].isnan().all()) if bad != bad else not bool(torch.isfinite(l1[sees]).any())
+
+
+@pytest.mark.parametrize("width,seqs", [(131072, [5, 4, 2, 1]), (40000, [7, 6, 3]), (300000, [3, 2, 1])])
+def test_a_pick_workspace_serves_fewer_sequences(width, seqs):
+    """Whose lists are cut into more chunks."""
+    from paper_2607_24555_amd import locks as B
+    cfg = B.Config(seqs[0], 32, 8, 8, 256, width // 16, 8, page_size=16)
+    ws = T.alloc_pick_workspace(cfg)
+    ws.fill_(255)
+    g = torch.Generator().manual_seed(width)
+    x = torch.rand(seqs[0], 8, width, generator=g)
+    lens = torch.tensor([width - 977 * s for s in range(seqs[0])], dtype=torch.int32)
+    for s in seqs:
+        print(f"[pick] {s} of {seqs[0]} x 8 lists of {width}", flush=True)
+        cfg.num_seqs = s
+        got = T.pick_tokens(cfg, x[:s].cuda(), lens[:s].cuda(), 500, 4, 64, ws).cpu()
+        for q in range(s):
+            assert got[q, 7].tolist() == R.pick(x[q, 7].numpy(), int(lens[q]), 500, 4, 64)
+
+
+def test_a_tree_workspace_serves_fewer_sequences():
+    """With the same tokens between them, so that their tiles are larger."""
+    b = Batch([60] * 16, [4] * 16, seed=3, extra=80)
+    ws = T.alloc_tree_workspace(b.cfg, b.n)
+    ws.fill_(255)
+    for seqs, new in ((16, 4), (8, 8), (4, 16), (1, 64)):
+        print(f"[tree] {seqs} x {new}", flush=True)
+        one = Batch([60] * seqs, [new] * seqs, seed=seqs, extra=80)
+        d = one.dev()
+        got = T.tree_attend(one.cfg, d["q"], d["k"], d["v"], d["pt"], d["sl"], ws, cu_tokens=d["cu"], mask=d["mask"])
+        one.check(got=(got[0].cpu(), got[1].cpu()))

@@ -111,6 +111,23 @@ def test_workspaces(lib):
     assert lib.locks_pick_workspace_bytes(_ref(c)) > 0 and lib.locks_pick_workspace_bytes(None) == 0
 
 
+@pytest.mark.parametrize("heads,group,pages,page,dt", [
+    (8, 4, 8192, 16, 1), (8, 4, 2500, 16, 1), (8, 7, 1000, 64, 1), (2, 16, 65536, 16, 1), (16, 7, 8192, 64, 0), (1, 1, 1, 16, 0)])
+def test_workspaces_of_larger_batches_are_no_smaller(lib, heads, group, pages, page, dt):
+    """What a workspace for the largest step is made for: fewer sequences need no more, nor do fewer
+    tokens (though they are cut into more chunks or larger tiles)."""
+    seqs, rows = [*range(0, 70), 128, 200, 256, 257, 300, 513, 1024], [0, 1, 5, 16, 64, 200, 4000]
+    pick, tree = 0, [0] * len(rows)
+    for s in seqs:
+        c = cfg(num_seqs=s, num_q_heads=heads * group, num_kv_heads=heads, max_pages_per_seq=pages, page_size=page,
+                kv_dtype=dt, q_dtype=dt).c()
+        pick, was = lib.locks_pick_workspace_bytes(_ref(c)), pick
+        assert pick >= was > 0 or s == 0, s
+        tree, was = [lib.locks_tree_workspace_bytes(_ref(c), n) for n in rows], tree
+        assert tree == sorted(tree) and all(a >= b for a, b in zip(tree, was)), s
+        assert tree[0] >= lib.locks_workspace_bytes(_ref(c))
+
+
 def test_pick_arguments(lib):
     c = cfg().c()
     need = lib.locks_pick_workspace_bytes(_ref(c))
