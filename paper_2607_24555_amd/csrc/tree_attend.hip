@@ -57,7 +57,7 @@ struct TreeArgs {
   float* po;       // [2 blocks][rows][128]
   float* pml;      // [2 blocks][rows][2]
   int32_t* rec;    // [blocks][8]: the item that begins in a block and ends in a later one
-  int tiles;       // most row tiles there can be
+  int tiles;       // most row tiles there can be, of row ranges that ascend
   int split, out_bf16;
 };
 
@@ -756,6 +756,9 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
     };
     // few sequences and tiles: every wave for itself, in lanes, all writing the same (without the
     // barriers of the other way a run of 5 tokens over 4K is planned in 1.3 us instead of 2.7)
+    // (tiles beyond a.tiles, of row ranges that do not ascend, are left out: all sums below are then
+    // within what tree_plan allows)
+    const int few = min(64, a.tiles);
     int total = kTiles + 1;
     if (d.S <= 64) {
       int v = lane < d.S ? fill_seq(lane) : 0;
@@ -767,7 +770,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
       if (lane < d.S) s_first[lane] = v - own;
       total = __builtin_amdgcn_readlane(v, d.S - 1);
       s_first[d.S] = total;
-      if (total <= 64) {
+      if (total <= few) {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         int c = 0;
         if (lane < total) {
@@ -785,7 +788,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
-    if (total > 64) {
+    if (total > few) {
       __syncthreads();
       constexpr int kPer = kTiles / kBlock;
       int before[kPer], sum = 0, v = 0;
@@ -799,11 +802,11 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {
         const int q = tid * kPer + e;
-        if (q < d.S) s_first[q] = min(at + before[e], kTiles);  // (more: cu that do not ascend)
+        if (q < d.S) s_first[q] = min(at + before[e], a.tiles);
       }
-      if (tid == 0) s_first[d.S] = min(total, kTiles);
+      if (tid == 0) s_first[d.S] = min(total, a.tiles);
       __syncthreads();
-      const int T = min(total, kTiles);
+      const int T = min(total, a.tiles);
       v = 0;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) {

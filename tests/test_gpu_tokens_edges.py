@@ -1,6 +1,6 @@
 """GPU checks of the calls on single cached tokens (include/locks_tokens.h) where only a part of an
-answer can go wrong: the roundings of bf16 outputs, and the LSE of rows that a NaN reaches; and of workspaces
-that serve smaller batches."""
+answer can go wrong: the roundings of bf16 outputs, and the LSE of rows that a NaN reaches; of workspaces that
+serve smaller batches, and of row ranges that do not ascend over very long tables."""
 import numpy as np
 import pytest
 import torch
@@ -150,3 +150,31 @@ def test_a_tree_workspace_serves_fewer_sequences():
         d = one.dev()
         got = T.tree_attend(one.cfg, d["q"], d["k"], d["v"], d["pt"], d["sl"], ws, cu_tokens=d["cu"], mask=d["mask"])
         one.check(got=(got[0].cpu(), got[1].cpu()))
+
+
+def test_tree_row_ranges_that_do_not_ascend_over_long_tables():
+    """Ten of 19 sequences claim all rows: ten times the 256-row tiles that ascending ranges have, over
+    14 M tokens each, whose weighted units in all KV heads pass 2^31.  The first ones are computed.
+    Every page is the same block; of zero keys and small whole values every sum is below 2^24
+    and exact, so that an output has a reciprocal's and a product's rounding, and an LSE below 32 at
+    most two steps of 2^-19 of a logarithm."""
+    from paper_2607_24555_amd import locks as B
+    S, H, P, pages, n = 19, 8, 64, 220000, 2560
+    L = pages * P
+    assert (S // 2 + 1) * (n // 256) * pages * H * 20 >= 1 << 31 and S * H * L < 1 << 31
+    cfg = B.Config(S, H, H, 8, 256, pages, 1, page_size=P)
+    g = torch.Generator().manual_seed(1)
+    k = torch.zeros(1, H, P, D, dtype=torch.bfloat16).cuda()
+    v = torch.randint(0, 2, (1, H, P, D), generator=g).bfloat16()
+    q = torch.randn(n, H, D, generator=g).bfloat16().cuda()
+    table = torch.zeros(S, pages, dtype=torch.int32).cuda()
+    lens = torch.full((S,), L, dtype=torch.int32).cuda()
+    cu = torch.tensor([n * (s & 1) for s in range(S + 1)], dtype=torch.int32).cuda()
+    print("[tree] row ranges that do not ascend, 14 M tokens", flush=True)
+    out, lse = T.tree_attend(cfg, q, k, v.cuda(), table, lens, T.alloc_tree_workspace(cfg, n), cu_tokens=cu)
+    torch.cuda.synchronize()
+    seen = L - n + 1 + torch.arange(n)                          # of row i, the first ones
+    count = (seen[:, None] // P + (torch.arange(P) < seen[:, None] % P)).double()
+    want = torch.stack([count @ v[0, h].double() for h in range(H)], 1) / seen[:, None, None]
+    assert bool(((out.cpu().double() - want).abs() <= 2.0 ** -22 * want).all())
+    assert bool(((lse.cpu().double() - torch.log(seen.double())[:, None]).abs() <= 2.0 ** -18).all())
