@@ -70,10 +70,12 @@ __global__ __launch_bounds__(256, kF32 ? 1 : 2) void mass_kernel(DraftArgs a, co
   const long lists = (long)a.S * a.H;
   auto next_list = [&](Unit& w) {  // not counted: the first list from `list` on that has units
     for (; list < lists; list += gridDim.x) {
-      w.s = (int)(list / a.H), w.h = (int)(list % a.H), w.u = 0;
-      list_of(w);
-      if (w.per) {
+      Unit y;
+      y.s = (int)(list / a.H), y.h = (int)(list % a.H), y.u = 0;
+      list_of(y);
+      if (y.per) {
         list += gridDim.x;
+        w = y;
         return true;
       }
     }

@@ -1,10 +1,12 @@
 """GPU checks of the calls on single cached tokens (include/locks_tokens.h) where only a part of an
 answer can go wrong: the roundings of bf16 outputs, and the LSE of rows that a NaN reaches; of workspaces that
-serve smaller batches, and of row ranges that do not ascend over very long tables."""
+serve smaller batches, of row ranges that do not ascend over very long tables, and of masses whose
+last sequences are empty."""
 import numpy as np
 import pytest
 import torch
 
+from paper_2607_24555_amd import locks as B
 from paper_2607_24555_amd import tokens as T
 from tests import _tokens_reference as R
 from tests.test_gpu_tokens import D, Batch
@@ -124,7 +126,6 @@ def test_lse_of_trees_with_bad_tokens(bad, q, new, extra):
 @pytest.mark.parametrize("width,seqs", [(131072, [5, 4, 2, 1]), (40000, [7, 6, 3]), (300000, [3, 2, 1])])
 def test_a_pick_workspace_serves_fewer_sequences(width, seqs):
     """Whose lists are cut into more chunks."""
-    from paper_2607_24555_amd import locks as B
     cfg = B.Config(seqs[0], 32, 8, 8, 256, width // 16, 8, page_size=16)
     ws = T.alloc_pick_workspace(cfg)
     ws.fill_(255)
@@ -158,7 +159,6 @@ def test_tree_row_ranges_that_do_not_ascend_over_long_tables():
     Every page is the same block; of zero keys and small whole values every sum is below 2^24
     and exact, so that an output has a reciprocal's and a product's rounding, and an LSE below 32 at
     most two steps of 2^-19 of a logarithm."""
-    from paper_2607_24555_amd import locks as B
     S, H, P, pages, n = 19, 8, 64, 220000, 2560
     L = pages * P
     assert (S // 2 + 1) * (n // 256) * pages * H * 20 >= 1 << 31 and S * H * L < 1 << 31
@@ -178,3 +178,31 @@ def test_tree_row_ranges_that_do_not_ascend_over_long_tables():
     want = torch.stack([count @ v[0, h].double() for h in range(H)], 1) / seen[:, None, None]
     assert bool(((out.cpu().double() - want).abs() <= 2.0 ** -22 * want).all())
     assert bool(((lse.cpu().double() - torch.log(seen.double())[:, None]).abs() <= 2.0 ** -18).all())
+
+
+@pytest.mark.parametrize("H", [1, 3])
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+def test_mass_of_many_sequences_whose_last_ones_are_empty(q, H):
+    """Beyond 512 sequences a block's lists may end with ones that have no tokens or no rows: what it
+    requests behind the last unit is that unit's again, not theirs."""
+    print(f"[mass] 1,700 sequences, {H} heads, {q}", flush=True)
+    lens = [40 + s % 90 if s < 600 else 0 if s % 2 else 5 for s in range(1700)]
+    new = [1 if s < 600 or (s % 2 and s % 3) else 0 for s in range(1700)]
+    b = Batch([max(0, L - n) for L, n in zip(lens, new)], [min(L, n) for L, n in zip(lens, new)], H=H, G=2, q=q, kv=q,
+              mask=None, seed=H)
+    d = b.dev()
+    cu = torch.tensor([0] + new, dtype=torch.int32).cumsum(0).int().cuda()  # (some empty sequences have a row)
+    n = int(cu[-1])
+    qs = torch.zeros(n, 2 * H, D, dtype=d["q"].dtype).cuda()
+    rows = torch.tensor([i for i, s in enumerate(s for s, k in enumerate(new) if k) if lens[s]])
+    qs[rows.cuda()] = d["q"][:len(rows)]
+    _, lse = T.tree_attend(b.cfg, qs, d["k"], d["v"], d["pt"], d["sl"], T.alloc_tree_workspace(b.cfg, n), cu_tokens=cu)
+    mass = T.token_mass(b.cfg, qs, lse, d["k"], d["pt"], d["sl"], T.alloc_mass(b.cfg), cu_tokens=cu)
+    one = T.alloc_mass(b.cfg)
+    for s0 in range(0, 600, 300):             # as few sequences at once as are counted
+        c = B.Config(300, 2 * H, H, 8, 256, b.cfg.max_pages_per_seq, b.cfg.num_blocks, b.cfg.kv_dtype, b.cfg.q_dtype)
+        T.token_mass(c, d["q"][s0:s0 + 300], lse[rows.cuda()][s0:s0 + 300].contiguous(), d["k"],
+                     d["pt"][s0:s0 + 300], d["sl"][s0:s0 + 300], one[s0:s0 + 300])
+    torch.cuda.synchronize()
+    assert bool((mass[600:] == 0).all()) and bool((mass[:600] != 0).any())
+    assert torch.equal(mass, one)
