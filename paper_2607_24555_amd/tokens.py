@@ -9,8 +9,9 @@ checks once for loops over fixed buffers.
 Speculative decoding over a paged cache:
 
     mask, depth = tree_mask(parents, cu_tokens)
+    # past [num_seqs]: tokens cached before; seq [n]: the sequence of each new token
     q = cache.rope_append_kv(cfg, k, v, k_cache, v_cache, page_table, seq_lens, rope,
-                             positions=past + depth, cu_tokens=cu, q=q)
+                             positions=past[seq] + depth, cu_tokens=cu, q=q)
     out, lse = tree_attend(cfg, q, k_cache, v_cache, page_table, seq_lens, ws, cu_tokens=cu, mask=mask)
     # ... the caller accepts a branch: its tokens' indices in `kept`, padded with -1
     keep_tokens(cfg, kept, k_cache, v_cache, page_table, start=past, out_lens=seq_lens)

@@ -208,3 +208,12 @@ def test_tree_mask():
     for cu in ([0, 1], [1, 2], [], [0, 2, 1, 2]):
         with pytest.raises(B.LocksError, match="cu_tokens"):
             T.tree_mask([-1, -1], cu, device="cpu")
+
+
+def test_the_documented_positions_are_one_a_token():
+    """The example's expression, for several sequences."""
+    words = re.search(r"positions=([^,]+),", T.__doc__).group(1)
+    _, depth = T.tree_mask([-1, 0, 0, -1, 0], [0, 3, 5], device="cpu")
+    past, seq = torch.tensor([70, 33], dtype=torch.int32), torch.tensor([0, 0, 0, 1, 1])
+    got = eval(words, {"past": past, "seq": seq, "depth": depth})
+    assert got.dtype == torch.int32 and got.tolist() == [70, 71, 71, 33, 34]
