@@ -27,7 +27,7 @@ A cache of bounded size:
 from __future__ import annotations
 
 import ctypes
-from typing import Optional, Sequence
+from typing import Sequence
 
 import torch
 
@@ -101,7 +101,10 @@ def alloc_mass(cfg: Config, device="cuda") -> torch.Tensor:
 def tree_mask(parents: Sequence[int], cu_tokens: Sequence[int], device="cuda"):
     """The mask [n][words] (int32) and depths [n] (int32) of drafted trees: parents[r] is the
     index, among its sequence's new tokens, of row r's parent, an earlier one, or -1 where it
-    follows the cached tokens themselves; cu_tokens as tree_attend takes it, on the host."""
+    follows the cached tokens themselves; cu_tokens as tree_attend takes it, on the host.  A loop
+    on the host and a copy that waits (8 trees of 48 tokens 0.6 to 1.2 ms, 64 of 64 17 to 30), for
+    trees that keep their shape over many steps; where they change with each one, its caller
+    builds the mask beside them."""
     parents, cu = [int(p) for p in parents], [int(c) for c in cu_tokens]
     if not cu or cu[0] != 0 or cu[-1] != len(parents) or any(a > b for a, b in zip(cu, cu[1:])):
         raise LocksError("cu_tokens: expected ascending row counts from 0 to the number of parents")
