@@ -231,9 +231,8 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
         constexpr int kElems = kF32 ? 4 : 8;
         const int t = min(u * C::kUnit + wt * C::kGroup + j * C::kTokStep + tok_in, L - 1);
         const uint32_t at = ((t & (d.pgsz - 1)) * kDim + kElems * piece) * sizeof(TK);
-        // (the same 16 tokens for a wave: of a step of 32, the second 16 for the upper four waves)
-        static_assert(C::kTokStep <= 32, "");
-        const size_t page = C::kTokStep == 32 && wr >= 4 ? base[(j * C::kTokStep / 16 + 1) % (2 * NB)] : base[j * C::kTokStep / 16];
+        static_assert(C::kDma || C::kTokStep <= 16, "a step's tokens lie in one page");
+        const size_t page = base[j * C::kTokStep / 16];
         if constexpr (!C::kDirect) kr[j] = *reinterpret_cast<const Raw*>(k_head + page + at);
         vr[j] = *reinterpret_cast<const Raw*>(v_head + page + at);
       }
@@ -301,8 +300,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
             for (int e = 0; e < 4; ++e)
               ok = ok && (vr[j][e] & 0x7f80u) != 0x7f80u && (vr[j][e] & 0x7f800000u) != 0x7f800000u;
           }
-          if constexpr (!C::kDirect) *reinterpret_cast<u4*>(kt + tok * C::kKRow + at) = kr[j];
-          *reinterpret_cast<u4*>(vt + tok * C::kVRow + at) = vr[j];
+          *reinterpret_cast<u4*>(vt + tok * C::kVRow + at) = vr[j];  // (keys stay in registers)
         }
       }
       return ok;
