@@ -45,27 +45,6 @@ struct PickArgs {
   long lists;
 };
 
-// Exclusive prefix sum of one value a thread over the block; total in `sum`.
-__device__ __forceinline__ int block_scan(int v, int* lds, int& sum) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) lds[wave] = x;
-  __syncthreads();
-  int before = 0;
-  sum = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += lds[w];
-    sum += lds[w];
-  }
-  return before + x - v;
-}
-
 // kPhase -1: the whole of it.  0, 1, 2: the histogram of that digit; 3: the output.
 template <int kKeys, int kPhase>
 __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
@@ -171,7 +150,7 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   // kBins - 1 - 2 tid and the one below, over all chunks; p: over the earlier ones
   auto choose = [&](int d, int h0, int h1, int p0, int p1) {
     int sum;
-    const int from = block_scan(h0 + h1, s_wave, sum);
+    const int from = scan_block<kWaves>(h0 + h1, s_wave, sum);
     const int b = kBins - 1 - 2 * tid;
     if (from < left && from + h0 >= left) s_bin = b, s_left = left - from, s_all = from + h0 == left;
     else if (from + h0 < left && from + h0 + h1 >= left)
@@ -183,7 +162,7 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
     all = s_all != 0;
     if (kPhase != -1) {
       const int from_bin = all ? bin : bin + 1;  // (those of a bin kept whole count as above)
-      block_scan((b >= from_bin ? p0 : 0) + (b - 1 >= from_bin ? p1 : 0), s_wave, sum);
+      scan_block<kWaves>((b >= from_bin ? p0 : 0) + (b - 1 >= from_bin ? p1 : 0), s_wave, sum);
       above += sum;
     }
   };
@@ -201,7 +180,7 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
     if (kPhase == 3) {
       int sum;
       const int b = kBins - 1 - 2 * tid, bin = s_bin;
-      block_scan((b == bin ? p0 : 0) + (b - 1 == bin ? p1 : 0), s_wave, sum);
+      scan_block<kWaves>((b == bin ? p0 : 0) + (b - 1 == bin ? p1 : 0), s_wave, sum);
       ties = all ? 0 : sum;
     } else if (tid == 0) {
       int32_t* st = a.state + (list * a.chunks + chunk) * 4;
