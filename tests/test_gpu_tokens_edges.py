@@ -1,7 +1,7 @@
 """GPU checks of the calls on single cached tokens (include/locks_tokens.h) where only a part of an
 answer can go wrong: the roundings of bf16 outputs, and the LSE of rows that a NaN reaches; of workspaces that
-serve smaller batches, of row ranges that do not ascend over very long tables, and of masses whose
-last sequences are empty."""
+serve smaller batches, of row ranges that do not ascend over very long tables, of masses whose
+last sequences are empty or whose LSE holds a NaN, and of kept tokens in front of a sequence's start."""
 import numpy as np
 import pytest
 import torch
@@ -206,3 +206,59 @@ def test_mass_of_many_sequences_whose_last_ones_are_empty(q, H):
     torch.cuda.synchronize()
     assert bool((mass[600:] == 0).all()) and bool((mass[:600] != 0).any())
     assert torch.equal(mass, one)
+
+
+@pytest.mark.parametrize("past,new,extra", [(40, 20, 1), (40, 20, 3000), (30, 70, 1), (30, 70, 3000)])
+@pytest.mark.parametrize("q", ["bf16", "fp32"])
+@pytest.mark.parametrize("mask", ["tree", None])
+def test_mass_of_nan_rows(mask, q, past, new, extra):
+    """One NaN in the LSE makes the masses of exactly what its row sees NaN, of its head's KV head
+    (rows shared by a block's waves: 70 new tokens in a short table; and not)."""
+    print(f"[mass nan] {past}+{new} extra={extra} {q} {mask}", flush=True)
+    b = Batch([past], [new], P=16, q=q, kv=q, mask=mask, seed=new, extra=extra)
+    d = b.dev()
+    _, lse = _attend(b)
+
+    def mass(l):
+        m = T.alloc_mass(b.cfg)
+        T.token_mass(b.cfg, d["q"], l.cuda(), d["k"], d["pt"], d["sl"], m, cu_tokens=d["cu"], mask=d["mask"])
+        return m.cpu()
+    want = mass(lse)
+    assert bool(torch.isfinite(want).all())
+    i, head = new - 3, 6                      # of KV head 1
+    lse[i, head] = float("nan")
+    got = mass(lse)
+    sees = torch.from_numpy(R.sees(new, past + new, None if b.mask is None else b.mask.numpy())[i])
+    nan = torch.zeros_like(want, dtype=torch.bool)
+    nan[0, 1, :past + new] = sees
+    assert torch.equal(got.isnan(), nan) and torch.equal(got[~nan], want[~nan])
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [6, 900])
+def test_keep_in_front_of_the_first_token(kv, n):
+    """A negative start: entries whose new place lies in front of the sequence are left out, the
+    others move, and the length counts all of them."""
+    print(f"[keep] start < 0, {n} entries {kv}", flush=True)
+    g = torch.Generator().manual_seed(n)
+    H, P, L, start = 2, 16, 2000, [-4, -1000]
+    table, nb = R.table_of([L, L], P, g)
+    dt, kind = (torch.bfloat16, B.LOCKS_BF16) if kv == "bf16" else (torch.float32, B.LOCKS_FP32)
+    cfg = B.Config(2, 4 * H, H, 8, 256, table.shape[1], nb, kind, kind, page_size=P)
+    k, v = (torch.randn(nb, H, P, D, generator=g).to(dt) for _ in range(2))
+    mass = torch.rand(2, H, table.shape[1] * P, generator=g)
+    kept = torch.stack([torch.stack([torch.randperm(L, generator=g)[:n].sort()[0] for _ in range(H)])
+                        for _ in range(2)]).int()
+    dk, dv, dm = k.cuda(), v.cuda(), mass.cuda()
+    got = T.keep_tokens(cfg, kept.cuda(), dk, dv, table.cuda(), start=torch.tensor(start, dtype=torch.int32).cuda(),
+                        mass=dm)
+    wk, wv, wm = k.clone(), v.clone(), mass.clone()
+    for s in range(2):
+        for h in range(H):
+            for i in range(max(0, -start[s]), n):
+                src, dst = int(kept[s, h, i]), start[s] + i
+                a, b = int(table[s, src // P]), int(table[s, dst // P])
+                wk[b, h, dst % P], wv[b, h, dst % P] = k[a, h, src % P], v[a, h, src % P]
+                wm[s, h, dst] = mass[s, h, src]
+    assert got.tolist() == [x + n for x in start]
+    assert torch.equal(dk.cpu(), wk) and torch.equal(dv.cpu(), wv) and torch.equal(dm.cpu(), wm)
