@@ -12,9 +12,9 @@
 // tells how many tokens kept lie before their chunk).
 //
 // Bound by latency, of barriers and launches: 8 lists of 4K tokens 10.4 us; 64 lists of 128K (33
-// MB, 6.5 us of HBM) 54 us in launches of 11, 13, 13 and 18; two of 1M 38 us.  Chunks of 16 K
-// for 64 lists of 128K: 64 us.  Ranks by two ballots a group for every lane instead of lane masks, and
-// forced tokens among them: 67.
+// MB, 6.5 us of HBM) with ties 54 us, without 51, in launches of 10, 12, 13 and 18; two of 1M
+// 38 us.  The number of launches goes by the tables' width: 64 lists of 4K in tables of 128K take
+// 43 us, in their own 12.
 #include <type_traits>
 
 #include "tokens_internal.h"
@@ -49,7 +49,8 @@ struct PickArgs {
 template <int kKeys, int kPhase>
 __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   // copies of the first digit's bins, by lane: masses of a list share few exponents, so that a
-  // wave's additions would meet (64 lists of 128K: 55.9 us instead of 57.4)
+  // wave's additions would meet (64 lists of 128K with ties 53.6 us instead of 55.2; without ties,
+  // where few meet, 51.4 instead of 50.3)
   constexpr int kCopies = kPhase == 0 ? 8 : 1;
   __shared__ int s_hist[kBins * kCopies], s_wave[kWaves], s_bin, s_left, s_all;
   const long list = blockIdx.x / a.chunks;
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   if (kPhase > 0) {
     const uint32_t* hist = reinterpret_cast<const uint32_t*>(a.hist + ((kPhase - 1) * a.lists + list) * a.chunks * kBins) +
                            (kPickBlock - 1 - tid);
-    auto few = [&](auto most) {  // all together (64 lists of 128K, four chunks: 51 us, in turn 54)
+    auto few = [&](auto most) {  // all together (64 lists of 128K, four chunks: 53.6 us, in turn 55.8)
       constexpr int kMost = decltype(most)::value;
       uint32_t v[kMost];
 #pragma unroll
@@ -240,8 +241,9 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
 }
 
 // Tokens of a chunk: as few as leave each block a compute unit, and at most 64 histograms to
-// sum where there is a choice (16 lists of 128K: 29 us, in chunks of 32 K 45; 2 of 1M 41 and 49;
-// 64 of 40K 32 and 45; 2 of 256K in chunks of 8 K 28, of 16 K 31).
+// sum where there is a choice (16 lists of 128K in chunks of 8 K: 28 us, of 32 K 44; 64 of 128K in
+// chunks of 32 K 51, of 16 K 57, of 8 K 64; 2 of 1M in chunks of 16 K 36, of 32 K 42, of 8 K 46; 64 of
+// 40K in chunks of 16 K 31.5, of 32 K 45; 2 of 256K in chunks of 8 K 24, of 16 K 27).
 int pick_chunk(const locks_cfg_t& c) {
   const long width = (long)c.max_pages_per_seq * c.page_size, lists = (long)c.num_seqs * c.num_kv_heads;
   if (width <= kOneLaunch) return kOneLaunch;

@@ -13,8 +13,9 @@
 //
 // Bound by HBM: 64 sequences of 1.5K to 8K tokens, 8 heads, a new token each: 128 us, 4.9 TB/s
 // (a copy here 5.1).  Keys read in the product's order, 32 bytes of each of 32 rows a load, took
-// 154.  With 128 rows (the last 32 tokens of prompts of 20K to 32K) 117 us, 3.7 TB/s: 16 powers
-// a lane and 32 x 32 logits take as long as their keys.  Among the new tokens a lane first has
+// 154.  With 128 rows (the last 32 tokens of prompts of 20K to 32K) 117 us, 3.7 TB/s: the vector
+// work (16 powers a lane and 32 x 32 logits) is half of that and the products a fifth, but a wave
+// does the three in turn, and two waves a SIMD do not hide all of it.  Among the new tokens a lane first has
 // what its row sees of the 32 tokens, one window of the mask, and the tokens' lanes take their bits
 // from it (15 trees of 34 to 104 tokens, eight heads a group, over up to 232: 44 us; with a mask
 // load for each row and token 116).
@@ -440,7 +441,9 @@ hipError_t launch_token_mass(const locks_cfg_t& c, const DraftArgs& a, const flo
   const bool f32 = c.q_dtype != LOCKS_BF16 || c.kv_dtype != LOCKS_BF16;
   const long width = (long)a.max_pages * a.pgsz, all = (width + 127) / 128 * a.H * a.S;
   // by the average sequence's rows, and the most units there can be (4 trees of up to 45 tokens over
-  // 3.7K, 8 heads of 5 queries, some thousand units: by rows 25 us, else 17.5)
+  // 3.7K, 8 heads of 5 queries, some thousand units: by rows 25 us, else 17.5).  The lengths are not
+  // known here, so short sequences in wide tables take the other way: 7 fp32 prompts as above in
+  // tables of 128K tokens 778 us instead of 157, 15 runs of 34 to 104 40 instead of 11.
   const bool by_rows = (long)a.n_tokens * a.G / a.S >= kManyRows && all <= kMassBlocks;
   const dim3 grid = by_rows ? dim3((unsigned)((width + 31) / 32), a.H, a.S) : dim3((unsigned)(all < kMassBlocks ? all : kMassBlocks));
 #define MASS(F32, TQ, TK)                                                                            \

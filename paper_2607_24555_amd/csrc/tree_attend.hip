@@ -16,13 +16,13 @@
 //              (8 sequences of 32K, 8 new: 210 us, 5.1 TB/s), below by latency: 5 new tokens
 //              over 4K take 19.3 us, 12 of it here (plan 2.0, rows to sums 2.8, joins and
 //              partials 2.5 of a block's 7.4) and 6.5 in the merge's launch.
-//   up to 64   two waves by rows, two by tokens (16 new: 209 us, 5.2 TB/s).
+//   up to 64   two waves by rows, two by tokens (16 new: 216 us, 5.0 TB/s).
 //   up to 128  four waves by rows, two blocks a compute unit.
 //   more       eight waves by rows, with three units of copies to LDS on their way.  Against the
 //              128-row tile: ragged trees of 140 to 248 rows 394 us (449), 16 tokens of 16 heads
 //              over 1M 501 (536), pieces of prompts 594 (637).  Its products and the weights'
-//              vector work overlap by half: at 2.05 GHz the matrix pipe is busy 45% of the time
-//              and the vector one 45% (pieces of prompts, 930 TFLOP/s).
+//              vector work overlap by half: the matrix pipe is busy 54% of the time and the
+//              vector one 53% (pieces of prompts, 700 TFLOP/s; 1,050 with the second term's).
 // fp32 products (any other types) take 32 or 128 rows and run at 69 TFLOP/s of the 154 of a
 // large product, the matrix pipe half busy: of a compute unit's two blocks the older one is
 // served first, and the other ends alone (82 and 105 us).
@@ -150,8 +150,8 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
   auto units_of = [&](int n, int L, int tile) { return max(1, (reach(n, L, tile) + C::kUnit - 1) / C::kUnit); };
 
   // What a unit of a tile costs.  In the 256-row tile the products of more rows show a little
-  // (ragged trees of 140 to 248 rows: 232 us for tiles of 160 rows, 271 for 256, counted the same);
-  // in the others two blocks of a compute unit hide that.
+  // (pieces of prompts 594 us; with 8 instead of 12: 596, 4: 625); in the others two blocks of a compute
+  // unit hide that.
   constexpr int kMostWeight = RW == 8 ? 20 : 1;
   auto weight_of = [&](int n, int tile) {
     if (RW < 8) return 1;
