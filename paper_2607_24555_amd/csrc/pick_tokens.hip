@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
   int32_t* out = a.out + list * a.n_keep;
   if (L <= a.n_keep) {
     if ((kPhase == -1 || kPhase == 3) && chunk == 0)
-      for (int i = tid; i < a.n_keep; i += kPickBlock) out[i] = i < L ? i : -1;
+      for (unsigned i = tid; i < (unsigned)a.n_keep; i += kPickBlock) out[i] = i < (unsigned)L ? (int)i : -1;
     return;
   }
   constexpr int kChunk = kPickBlock * kKeys;
@@ -203,8 +203,9 @@ __global__ __launch_bounds__(kPickBlock) void pick_kernel(PickArgs a) {
 
   // ---- the first n_sink and the last n_recent
   if (chunk == 0) {
-    for (int i = tid; i < lo; i += kPickBlock) out[i] = i;
-    for (int i = tid; i < a.n_recent; i += kPickBlock) out[a.n_keep - a.n_recent + i] = hi + i;
+    // (unsigned, as above: the last step may pass 2^31)
+    for (unsigned i = tid; i < (unsigned)lo; i += kPickBlock) out[i] = (int)i;
+    for (unsigned i = tid; i < (unsigned)a.n_recent; i += kPickBlock) out[a.n_keep - a.n_recent + i] = hi + (int)i;
   }
   // ---- ranks.  Lane g takes the 64 tokens of the wave's group g: which are above T, and which
   // equal to it.

@@ -1,7 +1,8 @@
 """GPU checks of the calls on single cached tokens (include/locks_tokens.h) where only a part of an
 answer can go wrong: the roundings of bf16 outputs, and the LSE of rows that a NaN reaches; of workspaces that
 serve smaller batches, of row ranges that do not ascend over very long tables, of masses whose
-last sequences are empty or whose LSE holds a NaN, and of kept tokens in front of a sequence's start."""
+last sequences are empty or whose LSE holds a NaN, and of kept tokens in front of a sequence's start, and
+of lists of nearly 2^31 entries."""
 import numpy as np
 import pytest
 import torch
@@ -262,3 +263,15 @@ def test_keep_in_front_of_the_first_token(kv, n):
                 wm[s, h, dst] = mass[s, h, src]
     assert got.tolist() == [x + n for x in start]
     assert torch.equal(dk.cpu(), wk) and torch.equal(dv.cpu(), wv) and torch.equal(dm.cpu(), wm)
+
+
+def test_pick_of_the_longest_list():
+    """n_keep at its limit: the fill's last step passes 2^31."""
+    n = (1 << 31) - 1
+    cfg = B.Config(1, 1, 1, 8, 256, 3, 8, page_size=16)
+    print("[pick] 2^31 - 1 kept", flush=True)
+    got = T.pick_tokens(cfg, torch.rand(1, 1, 48).cuda(), torch.tensor([37], dtype=torch.int32).cuda(), n, 0, 0,
+                        T.alloc_pick_workspace(cfg))[0, 0]
+    assert got[:37].tolist() == list(range(37))
+    for a in range(37, n, 1 << 28):
+        assert bool((got[a:a + (1 << 28)] == -1).all())
