@@ -37,25 +37,26 @@ __device__ __forceinline__ void move_rows(const KeepArgs& a, T* data, bool cache
     int src[kRows];                  // list entries
     int from[kRows], to[kRows];  // blocks of the row's old and new page; -1: nothing moves
   };
-  auto entries = [&](int i0, Round& r) {
+  // (rounds are counted in 64 bits: those requested ahead may begin past 2^31)
+  auto entries = [&](long i0, Round& r) {
 #pragma unroll
     for (int e = 0; e < kRows; ++e) {
-      const int i = i0 + e * kStep + me;
-      r.src[e] = i < a.n_keep && i >= 0 ? ids[i] : 0;
+      const long i = i0 + e * kStep + me;
+      r.src[e] = i < a.n_keep ? ids[i] : 0;
     }
   };
   // (once the entries are here) the list's end, and the pages
-  auto ends = [&](int i0, const Round& r) {
+  auto ends = [&](long i0, const Round& r) {
 #pragma unroll
     for (int e = 0; e < kRows; ++e) {
-      const int i = i0 + e * kStep + me;
-      if (r.src[e] < 0 && i < a.n_keep) atomicMin(&s_end, i);
+      const long i = i0 + e * kStep + me;
+      if (r.src[e] < 0 && i < a.n_keep) atomicMin(&s_end, (int)i);
     }
   };
-  auto pages = [&](int i0, Round& r) {
+  auto pages = [&](long i0, Round& r) {
 #pragma unroll
     for (int e = 0; e < kRows; ++e) {
-      const long i = (long)i0 + e * kStep + me, dst = a0 + i;
+      const long i = i0 + e * kStep + me, dst = a0 + i;
       r.from[e] = r.to[e] = -1;
       if (i < a.n_keep && r.src[e] > dst && dst >= 0 && r.src[e] >> lgP < a.max_pages) {
         r.from[e] = table[r.src[e] >> lgP];
@@ -64,10 +65,10 @@ __device__ __forceinline__ void move_rows(const KeepArgs& a, T* data, bool cache
     }
   };
   // (once those are here) the rows, and where they go
-  auto read = [&](int i0, const Round& r, int end, T (&x)[kRows], long (&to)[kRows]) {
+  auto read = [&](long i0, const Round& r, int end, T (&x)[kRows], long (&to)[kRows]) {
 #pragma unroll
     for (int e = 0; e < kRows; ++e) {
-      const long i = (long)i0 + e * kStep + me, dst = a0 + i;
+      const long i = i0 + e * kStep + me, dst = a0 + i;
       to[e] = -1;
       if (i < end && (unsigned)r.from[e] < (unsigned)a.num_blocks && (unsigned)r.to[e] < (unsigned)a.num_blocks) {
         auto at = [&](int blk, long t) {
@@ -92,7 +93,7 @@ __device__ __forceinline__ void move_rows(const KeepArgs& a, T* data, bool cache
   __syncthreads();
   int end = s_end;
   read(0, r1, end, x, to);
-  for (int i0 = 0; i0 < min(a.n_keep, end); i0 += kRound) {
+  for (long i0 = 0; i0 < min(a.n_keep, end); i0 += kRound) {
     arrived();
     ends(i0 + 2 * kRound, r3);
     __syncthreads();  // this round's rows are in registers, the list is known up to r3

@@ -275,3 +275,24 @@ def test_pick_of_the_longest_list():
     assert got[:37].tolist() == list(range(37))
     for a in range(37, n, 1 << 28):
         assert bool((got[a:a + (1 << 28)] == -1).all())
+
+
+@pytest.mark.parametrize("with_mass", [False, True])
+def test_keep_of_the_longest_list(with_mass):
+    """2^31 - 1 entries, none of which moves but one at the front: the rounds' ends pass 2^31."""
+    n = (1 << 31) - 1
+    cfg = B.Config(1, 1, 1, 8, 256, 4, 5, page_size=16)
+    k, v = (torch.randn(5, 1, 16, D).bfloat16() for _ in range(2))
+    mass = torch.rand(1, 1, 64) if with_mass else None
+    kept = torch.zeros(1, 1, n, dtype=torch.int32, device="cuda")
+    kept[0, 0, 3] = 50
+    table = torch.tensor([[2, 0, 4, 1]], dtype=torch.int32).cuda()
+    dk, dv, dm = k.cuda(), v.cuda(), mass.cuda() if with_mass else None
+    print("[keep] 2^31 - 1 entries", flush=True)
+    got = T.keep_tokens(cfg, kept, dk, dv, table, mass=dm)
+    assert got.tolist() == [n]
+    k[2, 0, 3], v[2, 0, 3] = k[1, 0, 2], v[1, 0, 2]
+    assert torch.equal(dk.cpu(), k) and torch.equal(dv.cpu(), v)
+    if with_mass:
+        mass[0, 0, 3] = mass[0, 0, 50]
+        assert torch.equal(dm.cpu(), mass)
