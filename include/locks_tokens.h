@@ -73,9 +73,9 @@ size_t locks_tree_workspace_bytes(const locks_cfg_t* cfg, int32_t n_tokens);
  * weight), two for bf16 ones (2^-16), whatever the batch; other types are computed in fp32
  * throughout.
  * Returns LOCKS_E_INVAL for a null or misaligned pointer, a bad stride or count or out == q,
- * and LOCKS_E_UNSUPPORTED for another out_dtype, for n_tokens * H_q or the tables' tokens
- * over all sequences and KV heads of 2^31 or more, masks of more than 2^25 words a row, or a
- * block of 4 GiB or more (all KV heads of a page). */
+ * and LOCKS_E_UNSUPPORTED for another out_dtype, for n_tokens * H_q of 2^31 or more, the
+ * tables' tokens over all sequences and KV heads of 2^31 - 4,096 or more, masks of more than
+ * 2^25 words a row, or a block of 4 GiB or more (all KV heads of a page). */
 int locks_tree_attend(const locks_cfg_t* cfg, const locks_draft_t* draft, const void* k_cache,
                       const void* v_cache, const int32_t* page_table, const int32_t* seq_lens,
                       void* out, int32_t out_dtype, float* out_lse, void* ws, size_t ws_bytes,

@@ -22,8 +22,10 @@ int draft_args(const locks_cfg_t* c, const locks_draft_t* d, const int32_t* page
       (!d->q || !aligned16(d->q) || d->q_stride < (int64_t)c->num_q_heads * kDim ||
        d->q_stride * qb % 16 != 0 || d->q_stride > (int64_t)1 << 40))
     return LOCKS_E_INVAL;
+  // (a sequence's tokens are rounded up to whole units in 32 bits)
   if ((int64_t)d->n_tokens * c->num_q_heads > 0x7fffffffL ||
-      (int64_t)c->max_pages_per_seq * c->page_size * c->num_kv_heads > 0x7fffffffL / (c->num_seqs ? c->num_seqs : 1) ||
+      (int64_t)c->max_pages_per_seq * c->page_size * c->num_kv_heads >
+          (0x7fffffffL - 4096) / (c->num_seqs ? c->num_seqs : 1) ||
       (int64_t)c->num_kv_heads * c->page_size * kDim * (c->kv_dtype == LOCKS_BF16 ? 2 : 4) > 0xffffffffL ||
       (d->mask && d->mask_words > 1 << 25))
     return LOCKS_E_UNSUPPORTED;

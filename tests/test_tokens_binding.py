@@ -111,6 +111,15 @@ def test_workspaces(lib):
     assert lib.locks_pick_workspace_bytes(_ref(c)) > 0 and lib.locks_pick_workspace_bytes(None) == 0
 
 
+@pytest.mark.parametrize("seqs,heads,pages,code", [
+    (1, 1, (1 << 27) - 1, -2), (1, 1, (1 << 27) - 256, -2), (1, 1, (1 << 27) - 257, 0),
+    (1, 8, (1 << 24) - 31, -2), (1, 8, (1 << 24) - 33, 0), (4, 2, (1 << 24) - 31, -2), (4, 2, (1 << 24) - 33, 0)])
+def test_tables_whose_tokens_round_up_past_31_bits_are_refused(lib, seqs, heads, pages, code):
+    c = cfg(num_seqs=seqs, num_kv_heads=heads, num_q_heads=heads, max_pages_per_seq=pages).c()
+    d = draft(n_tokens=0)
+    assert (_tree(lib, c, d), _mass(lib, c, d)) == (code, code)
+
+
 @pytest.mark.parametrize("heads,group,pages,page,dt", [
     (8, 4, 8192, 16, 1), (8, 4, 2500, 16, 1), (8, 7, 1000, 64, 1), (2, 16, 65536, 16, 1), (16, 7, 8192, 64, 0), (1, 1, 1, 16, 0)])
 def test_workspaces_of_larger_batches_are_no_smaller(lib, heads, group, pages, page, dt):
