@@ -296,3 +296,43 @@ def test_keep_of_the_longest_list(with_mass):
     if with_mass:
         mass[0, 0, 3] = mass[0, 0, 50]
         assert torch.equal(dm.cpu(), mass)
+
+
+@pytest.mark.parametrize("mask", ["tree", None])
+def test_steps_without_new_tokens(mask):
+    """Of some sequences, and of all: nothing is written."""
+    b = Batch([30, 0, 700], [0, 0, 3], mask=mask, seed=1)
+    b.check()
+    d = b.d
+    none = torch.zeros(4, dtype=torch.int32).cuda()
+    out, lse = T.tree_attend(b.cfg, d["q"][:0], d["k"], d["v"], d["pt"], d["sl"], d["ws"], cu_tokens=none,
+                             mask=None if mask is None else d["mask"][:0])
+    assert out.shape == (0, 8, D) and lse.shape == (0, 8)
+    mass = torch.full((3, 2, b.cfg.max_pages_per_seq * 16), 2.0).cuda()
+    T.token_mass(b.cfg, d["q"][:0], lse, d["k"], d["pt"], d["sl"], mass, cu_tokens=none, decay=0.5)
+    assert bool((mass == 2.0).all())
+    kept = torch.full((3, 1, 5), -1, dtype=torch.int32).cuda()
+    k, v = d["k"].clone(), d["v"].clone()
+    lens = T.keep_tokens(b.cfg, kept, d["k"], d["v"], d["pt"], start=d["sl"], mass=mass)
+    assert torch.equal(lens, d["sl"]) and torch.equal(d["k"], k) and torch.equal(d["v"], v) and bool((mass == 2.0).all())
+
+
+def test_calls_on_a_stream_that_is_not_the_current_one():
+    """The four calls in order on one side stream, their inputs made on it, equal the current
+    stream's."""
+    def step(b, d, stream):
+        mass, pws = T.alloc_mass(b.cfg), T.alloc_pick_workspace(b.cfg)
+        torch.cuda.synchronize()
+        out, lse = T.tree_attend(b.cfg, d["q"], d["k"], d["v"], d["pt"], d["sl"], d["ws"], cu_tokens=d["cu"],
+                                 mask=d["mask"], stream=stream)
+        T.token_mass(b.cfg, d["q"], lse, d["k"], d["pt"], d["sl"], mass, cu_tokens=d["cu"], mask=d["mask"],
+                     decay=0.5, stream=stream)
+        ids = T.pick_tokens(b.cfg, mass, d["sl"], 64, 4, 16, pws, stream=stream)
+        lens = T.keep_tokens(b.cfg, ids, d["k"], d["v"], d["pt"], mass=mass, stream=stream)
+        torch.cuda.synchronize()
+        return out, lse, mass, ids, lens, d["k"], d["v"]
+    got = []
+    for stream in (None, torch.cuda.Stream()):
+        b = Batch([9000, 300], [20, 9], seed=5)
+        got.append(step(b, b.dev(), stream))
+    assert all(torch.equal(x, y) for x, y in zip(*got))
