@@ -22,9 +22,9 @@
  * would be too large too.
  *
  * Lengths are known on the device only, so where kernels differ for short sequences they are
- * chosen by the tables' width, max_pages_per_seq.  Tables much wider than the sequences cost
- * time in attention up to 512 tokens, masses of many new tokens over few, and picks up to
- * 32,768 tokens, twice to five times as much.
+ * chosen by the tables' width, max_pages_per_seq.  In tables much wider than the sequences
+ * attention over up to 512 tokens takes 1.4 times as long, picks of up to 32,768 tokens two to
+ * four times, masses of many new tokens over few four to five times.
  */
 #ifndef LOCKS_TOKENS_H
 #define LOCKS_TOKENS_H
@@ -65,9 +65,9 @@ size_t locks_tree_workspace_bytes(const locks_cfg_t* cfg, int32_t n_tokens);
  *   o = sum_t softmax_t(q . k_t / sqrt(128)) v_t.
  *   out      [n_tokens][H_q][128] of out_dtype (LOCKS_BF16 or LOCKS_FP32)
  *   out_lse  nullable float [n_tokens][H_q], log of the softmax denominator
- * A token that sees nothing gets out = 0 and out_lse = -inf; a NaN in a query, or in a key that it
- * sees, makes its out and out_lse NaN.  Tokens that a row does not see
- * do not reach it, whatever their keys and values hold; nor do rows past a sequence's end.
+ * A token that sees nothing gets out = 0 and out_lse = -inf; a NaN in a query, or in a key
+ * that it sees, makes its out and out_lse NaN.  Tokens that a row does not see do not reach
+ * it, whatever their keys and values hold; nor do rows past a sequence's end.
  * Logits, maxima and sums are fp32.  Over bf16 queries and caches the softmax weights enter
  * the product with the values as sums of bf16 terms: three for fp32 outputs (2^-24 of a
  * weight), two for bf16 ones (2^-16), whatever the batch; other types are computed in fp32

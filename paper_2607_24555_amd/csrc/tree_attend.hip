@@ -676,7 +676,7 @@ __global__ __launch_bounds__(64 * RW * TW, kWaves) void tree_kernel(TreeArgs a) 
 #pragma unroll
       for (int w = 0; w < TW; ++w) {
         const float mw = s_m[w][wr * 32 + col];
-        // (a product where the wave has no maximum too: a sum of NaN logits, whose maximum stays -inf, stays NaN)
+        // (a product also where the wave has no maximum: of NaN logits the sum is NaN, the maximum -inf)
         ls += s_l[w][wr * 32 + col] * (mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - mx));
       }
       const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - mx);
@@ -1040,9 +1040,9 @@ void launch_terms(const TreeArgs& a, const Plan& p, hipStream_t st) {
   else launch_one<false, uint16_t, uint16_t, NT, 8, 1, 2, 2>(a, p, st);
 }
 // Terms of a weight, by the output's type alone: three for fp32 (2^-24 of it), two for bf16 (2^-16, a
-// 256th of the output's own rounding).  In one term (2^-8) a bf16 output is as far off again as by its own
-// rounding, 2.3e-3 of it instead of 1.7e-3, and so much depends on the batch's tile where only some tiles have it
-// (ragged trees 304 us in one term, 400 in two, 492 in three; pieces of prompts 447, 605 and 751).
+// 256th of the output's own rounding).  One term (2^-8) puts a bf16 output as far off again as its own
+// rounding does, 2.3e-3 of its norm instead of 1.7e-3 (ragged trees 304 us in one term, 394 in two, 492 in
+// three; pieces of prompts 447, 594 and 751).
 void launch_bf16(const TreeArgs& a, const Plan& p, hipStream_t st) {
   if (a.out_bf16) launch_terms<2>(a, p, st);
   else launch_terms<3>(a, p, st);
